@@ -65,7 +65,9 @@ enum {
   VVS_DEV_BAD_NEIGHBOUR = 4,  /* CSR column outside [0, V) or row_ptr not monotone */
   VVS_DEV_TIMEOUT = 8,        /* a bounded wait on a barrier ran out */
   VVS_DEV_FCACHE_MISS = 16,   /* feature-cache fetch asked for a position not in the ring */
-  VVS_DEV_BAD_ARG = 32        /* n_draft / gamma / n_store outside its documented range */
+  VVS_DEV_BAD_ARG = 32,       /* n_draft / gamma / n_store (and the device arguments of the 8-bit cache and of
+                                 vvs_rotate_axes) outside its documented range */
+  VVS_DEV_NONFINITE = 64      /* vvs_quant_cache_append met an infinity (stored as the largest code) or a NaN (stored as 0) */
 };
 
 typedef struct vvs_ctx vvs_ctx;
@@ -370,6 +372,97 @@ int vvs_select_unverified(vvs_ctx* ctx, const int32_t* paths, const int32_t* pat
                           int32_t n_paths, int32_t max_len, const float* uniforms, int32_t* out_path,
                           int32_t* out_gamma, int32_t* out_tokens, void* stream);
 
+/* ---- 8-bit key / value cache, its attention and eviction; rotary positions with several axes --------------------------
+ * (No counterpart in the paper: what a decoder with long image or video contexts needs next to the verified step.)  The
+ * calls take tensors of one layer and need a context for its storage type T and its status word only; calls on different
+ * streams may share it.  Head sizes of the cache are 64 and 128. */
+
+/* Rows of heads: element (sequence b, row t, head h, i) lies at data + b * seq + t * row + h * head + i (strides in
+ * elements, so that the q, k and v heads of one projection's output need no copy).  data is 16-byte aligned and the
+ * strides are multiples of 16 bytes, except those of dimensions of size one. */
+typedef struct vvs_heads {
+  void* data;
+  int64_t seq;
+  int64_t row;
+  int64_t head;
+} vvs_heads;
+
+/* Rotary positions with several axes: time, row and column of a video token, say.  Pair i of a head is turned by the angle
+ * (float)pos[axis[i]][b][t] * inv_freq[i], a float32 number as in vvs_verify; cosine, sine and the products are float32.
+ * The elements behind the last pair stay as they are. */
+typedef struct vvs_rope_axes {
+  const float* inv_freq; /* device [n_pairs] */
+  const int32_t* axis;   /* device [n_pairs] in 0 .. n_axes - 1; another value sets VVS_DEV_BAD_ARG, its pair is not turned */
+  const int32_t* pos;    /* device [n_axes][n_seqs][n_rows] */
+  int32_t n_axes;
+  int32_t n_pairs;       /* 1 .. head_dim / 2 */
+  int32_t halves;        /* 0: pairs (2i, 2i + 1); 1: pairs (i, i + n_pairs), n_pairs a multiple of 4 */
+} vvs_rope_axes;
+
+/* out = x turned, for the query heads and, with k and k_out, for the key heads of the same rows.  In place where out has
+ * x's address and strides; overlapping otherwise is not allowed.  head_dim is a multiple of 8, at most 256. */
+int vvs_rotate_axes(vvs_ctx* ctx, const vvs_rope_axes* rope, int32_t n_seqs, int32_t n_rows, int32_t n_heads, int32_t n_kv_heads,
+                    int32_t head_dim, const vvs_heads* q, const vvs_heads* q_out, const vvs_heads* k, const vvs_heads* k_out,
+                    void* stream);
+
+/* Keys and values of one layer in e4m3 (4 exponent bits, bias 7, 3 mantissa bits, largest value 448) with one float32 scale
+ * for each block of `block` slots of a head: element = code * scale.  vvs_quant_cache_append writes powers of two, the
+ * smallest (2^-60 at least) by which a block's largest magnitude is at most 448: a scale that has to grow then changes codes
+ * by their exponent, without another rounding of anything but the smallest ones.  vvs_quant_cache_attend takes any positive
+ * scales.  Device memory of the caller; what lies behind a sequence's fill level may be anything. */
+typedef struct vvs_qcache {
+  void* k;          /* e4m3 [n_seqs][n_heads][cap][head_dim], keys after rotation */
+  void* v;
+  float* k_scale;   /* [n_seqs][n_heads][cap / block] */
+  float* v_scale;
+  float* mass;      /* [n_seqs][n_heads][cap] accumulated attention weight of each slot, or NULL */
+  int32_t* age;     /* [n_seqs][n_heads][cap] index of each slot's token in its sequence, or NULL = the slot itself */
+  int32_t n_seqs;
+  int32_t n_heads;
+  int32_t head_dim; /* 64 or 128 */
+  int32_t cap;      /* slots; a multiple of block */
+  int32_t block;    /* 16, 32, 64 or 128 */
+} vvs_qcache;
+
+/* Puts n_rows rows (row_count[b] of them where row_count, device int32 [n_seqs], is given) of k and v behind the
+ * cache_len[b] slots that sequence b holds: slots cache_len[b] .. of every head, mass 0, age next_age[b] + row (next_age:
+ * device int32 [n_seqs]; NULL = cache_len).  With `rope` the keys are turned first, in float32, and so are the q heads
+ * (n_heads of them) into q_out, where q is given.  row_index (device int32 [n_seqs][n_rows], or NULL): row j is source row
+ * row_index[b][j], with its position; after a tree call the rows on the accepted path are put again, at the block's start.
+ * A block's scale starts from its new rows where they begin the block, and else only grows; then the rows before them
+ * are rounded again.  Sequences that do not fit (cache_len + rows > cap) are skipped: VVS_DEV_CACHE_OVERFLOW. */
+int vvs_quant_cache_append(vvs_ctx* ctx, const vvs_qcache* qc, const vvs_heads* k, const vvs_heads* v, const int32_t* cache_len,
+                           int32_t n_rows, const int32_t* row_count, const int32_t* row_index, const int32_t* next_age,
+                           const vvs_rope_axes* rope, int32_t n_heads, const vvs_heads* q, const vvs_heads* q_out, void* stream);
+
+/* Attention of n_rows rows per sequence, already appended (slots cache_len[b] ..), over the cache:
+ * out[b, t, h] = sum_j p_j v_j, p = softmax(scale * q k_j) over the slots that row t sees: first_slot[b] .. cache_len[b] - 1
+ * (first_slot: device int32 [n_seqs], NULL = 0) and of its own block the rows 0 .. t, or those with bit j of visible[b][t]
+ * set (device uint32 [n_seqs][n_rows], a tree's ancestors and the row itself; n_rows <= 32 then).  n_heads is a multiple of
+ * the cache's heads: query head h reads head h / (n_heads / qc->n_heads).  Rows from row_count[b] on, and rows that see
+ * nothing, are zero, their lse -infinity.
+ * lse (float32 [n_seqs][n_rows][n_heads], or NULL): log of the sum of exp(scale * q k_j).
+ * mass_rows > 0: qc->mass[slot] = mass_decay * mass[slot] + the sum of p over the first mass_rows rows and the query heads
+ * of each cached head, for all slots below cache_len + row_count; mass_decay 0 overwrites.  The order of every sum is fixed.
+ * scale <= 0 stands for 1 / sqrt(head_dim).  max_len: an upper bound of cache_len + n_rows that the caller knows, by which
+ * the work is split (results do not depend on its truth, their speed does); 0 = cap. */
+int vvs_quant_cache_attend(vvs_ctx* ctx, const vvs_qcache* qc, const vvs_heads* q, const vvs_heads* out, const int32_t* cache_len,
+                           int32_t n_rows, int32_t n_heads, const int32_t* row_count, const int32_t* first_slot,
+                           const uint32_t* visible, float* lse, float scale, int32_t mass_rows, float mass_decay, int32_t max_len,
+                           void* stream);
+
+/* Brings every sequence to at most `keep` slots: of each head stay the rows of the n_sink first and n_recent last tokens
+ * (age < n_sink, age >= next_age[b] - n_recent; n_sink + n_recent <= keep) and, of the others, those of the largest mass,
+ * the lower slot first among equals (a NaN counts as the least).  Rows that stay and lie in slots below keep stay there; the
+ * others, in the order of their slots, fill the slots that became free.  A block's scale grows to the largest that its new
+ * rows come with.  Reads qc->mass and qc->age (NULL: age = slot), writes them for the new order to mass_out and age_out
+ * (device [n_seqs][n_heads][cap], other memory than qc's; age_out may be NULL): slots from new_len to cache_len become 0
+ * and -1, later ones are not touched.  new_len (device int32 [n_seqs]) = min(cache_len, keep).  kept (device int32
+ * [n_seqs][n_heads][keep]): the slot that each slot's row comes from, -1 behind new_len.  next_age NULL = cache_len.
+ * A sequence whose cache_len is outside 0 .. cap is skipped: VVS_DEV_CACHE_OVERFLOW.  cap <= 131072. */
+int vvs_quant_cache_evict(vvs_ctx* ctx, const vvs_qcache* qc, const int32_t* cache_len, int32_t keep, int32_t n_sink, int32_t n_recent,
+                          const int32_t* next_age, float* mass_out, int32_t* age_out, int32_t* new_len, int32_t* kept, void* stream);
+
 /* Synchronise `stream`, copy the device status word to *out_bits (VVS_DEV_* bits) and clear
  * it.  Returns VVS_ERR_DEVICE_TIMEOUT / VVS_ERR_DEVICE_BOUNDS if such a bit was set. */
 int vvs_device_status(vvs_ctx* ctx, void* stream, int32_t* out_bits);
@@ -382,6 +475,9 @@ int vvs_device_status(vvs_ctx* ctx, void* stream, int32_t* out_bits);
  * the next vvs_device_status returns VVS_ERR_DEVICE_TIMEOUT and clears it), and the context stays
  * usable.  Synchronises `stream`.  Nothing in it can hang: the waits are the bounded ones. */
 int vvs_selftest_bounded_wait(vvs_ctx* ctx, void* stream, int32_t* gave_up);
+
+/* Bytes of an element of the context's storage type T. */
+int vvs_element_bytes(const vvs_ctx* ctx);
 
 /* Number of kernels the last vvs_verify / vvs_epilogue call on this context launched. */
 int vvs_last_launch_count(const vvs_ctx* ctx);

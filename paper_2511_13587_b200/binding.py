@@ -28,7 +28,7 @@ VVS_DTYPE_FP32, VVS_DTYPE_BF16 = 0, 1
 VVS_ROPE_NONE, VVS_ROPE_1D, VVS_ROPE_2D_GRID = 0, 1, 2
 VVS_MODE_STRICT, VVS_MODE_RELAXED = 0, 1
 VVS_DEV_BAD_TOKEN, VVS_DEV_CACHE_OVERFLOW, VVS_DEV_BAD_NEIGHBOUR = 1, 2, 4
-VVS_DEV_TIMEOUT, VVS_DEV_FCACHE_MISS, VVS_DEV_BAD_ARG = 8, 16, 32
+VVS_DEV_TIMEOUT, VVS_DEV_FCACHE_MISS, VVS_DEV_BAD_ARG, VVS_DEV_NONFINITE = 8, 16, 32, 64
 
 
 class vvs_model_desc(C.Structure):
@@ -69,6 +69,20 @@ class vvs_fcache(C.Structure):
                 ("n_rows", C.c_int32), ("cap", C.c_int32)]
 
 
+class vvs_heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("seq", C.c_int64), ("row", C.c_int64), ("head", C.c_int64)]
+
+
+class vvs_rope_axes(C.Structure):
+    _fields_ = [("inv_freq", C.c_void_p), ("axis", C.c_void_p), ("pos", C.c_void_p), ("n_axes", C.c_int32), ("n_pairs", C.c_int32),
+                ("halves", C.c_int32)]
+
+
+class vvs_qcache(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "mass", "age")] + \
+               [(n, C.c_int32) for n in ("n_seqs", "n_heads", "head_dim", "cap", "block")]
+
+
 _P = C.c_void_p
 lib.vvs_create.argtypes = [C.POINTER(vvs_model_desc), C.POINTER(_P)]
 lib.vvs_destroy.argtypes = [_P]
@@ -94,6 +108,13 @@ lib.vvs_skip_decide.argtypes = [_P, _P, _P, C.c_int32, C.c_int32, C.c_int32, _P,
 lib.vvs_skip_decide.restype = C.c_int
 lib.vvs_select_unverified.argtypes = [_P, _P, _P, C.c_int32, C.c_int32, C.c_int32, _P, _P, _P, _P, _P]
 lib.vvs_select_unverified.restype = C.c_int
+lib.vvs_rotate_axes.argtypes = [_P, C.POINTER(vvs_rope_axes)] + [C.c_int32] * 5 + [C.POINTER(vvs_heads)] * 4 + [_P]
+lib.vvs_quant_cache_append.argtypes = [_P, C.POINTER(vvs_qcache), C.POINTER(vvs_heads), C.POINTER(vvs_heads), _P, C.c_int32, _P, _P, _P,
+                                       C.POINTER(vvs_rope_axes), C.c_int32, C.POINTER(vvs_heads), C.POINTER(vvs_heads), _P]
+lib.vvs_quant_cache_attend.argtypes = [_P, C.POINTER(vvs_qcache), C.POINTER(vvs_heads), C.POINTER(vvs_heads), _P, C.c_int32, C.c_int32,
+                                       _P, _P, _P, _P, C.c_float, C.c_int32, C.c_float, C.c_int32, _P]
+lib.vvs_quant_cache_evict.argtypes = [_P, C.POINTER(vvs_qcache), _P, C.c_int32, C.c_int32, C.c_int32, _P, _P, _P, _P, _P, _P]
+lib.vvs_element_bytes.argtypes = [_P]
 lib.vvs_device_status.argtypes = [_P, _P, C.POINTER(C.c_int32)]
 lib.vvs_last_launch_count.argtypes = [_P]
 lib.vvs_profile_enable.argtypes = [_P, C.c_int]
@@ -103,7 +124,8 @@ lib.vvs_strerror.restype = C.c_char_p
 for _n in ("vvs_create", "vvs_destroy", "vvs_workspace_bytes", "vvs_bind_weights",
            "vvs_bind_neighbors", "vvs_verify", "vvs_epilogue", "vvs_feature_cache_reset",
            "vvs_feature_cache_store", "vvs_feature_cache_fetch", "vvs_device_status",
-           "vvs_last_launch_count", "vvs_profile_enable", "vvs_profile_read"):
+           "vvs_last_launch_count", "vvs_profile_enable", "vvs_profile_read", "vvs_rotate_axes", "vvs_quant_cache_append",
+           "vvs_quant_cache_attend", "vvs_quant_cache_evict", "vvs_element_bytes"):
     getattr(lib, _n).restype = C.c_int
 
 
@@ -203,6 +225,10 @@ vvs_feature_cache_store = _native.vvs_feature_cache_store
 vvs_feature_cache_fetch = _native.vvs_feature_cache_fetch
 vvs_skip_decide = _native.vvs_skip_decide
 vvs_select_unverified = _native.vvs_select_unverified
+vvs_rotate_axes = _native.vvs_rotate_axes
+vvs_quant_cache_append = _native.vvs_quant_cache_append
+vvs_quant_cache_attend = _native.vvs_quant_cache_attend
+vvs_quant_cache_evict = _native.vvs_quant_cache_evict
 
 
 def vvs_selftest_bounded_wait(ctx: int, stream=None):
@@ -217,6 +243,29 @@ def make_fcache(feat: torch.Tensor, fpos: torch.Tensor, newest: torch.Tensor) ->
     fc = vvs_fcache(_ptr(feat), _ptr(fpos), _ptr(newest), int(feat.shape[0]), int(feat.shape[1]))
     fc._keep = (feat, fpos, newest)
     return fc
+
+
+def make_rope_axes(inv_freq: torch.Tensor, axis: torch.Tensor, pos: torch.Tensor, halves: bool = False) -> vvs_rope_axes:
+    """inv_freq float32 [n_pairs], axis int32 [n_pairs], pos int32 [n_axes, n_seqs, n_rows] (CUDA tensors)."""
+    r = vvs_rope_axes(_ptr(inv_freq), _ptr(axis), _ptr(pos), int(pos.shape[0]), int(inv_freq.shape[0]), 1 if halves else 0)
+    r._keep = (inv_freq, axis, pos)
+    return r
+
+
+def make_qcache(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, mass: torch.Tensor | None = None,
+                age: torch.Tensor | None = None) -> vvs_qcache:
+    """k, v [n_seqs, n_heads, cap, head_dim] of one byte, k_scale, v_scale float32 [n_seqs, n_heads, cap / block],
+    mass float32 and age int32 [n_seqs, n_heads, cap] (CUDA tensors, contiguous)."""
+    for name, t, shape, size in (("k", k, k.shape, 1), ("v", v, k.shape, 1), ("k_scale", k_scale, k_scale.shape, 4),
+                                 ("v_scale", v_scale, k_scale.shape, 4), ("mass", mass, k.shape[:3], 4), ("age", age, k.shape[:3], 4)):
+        if t is not None and (not t.is_contiguous() or t.shape != shape or t.element_size() != size):
+            raise ValueError(f"{name}: expected a contiguous tensor {tuple(shape)} of {size}-byte elements")
+    if k.dim() != 4 or k_scale.shape[:2] != k.shape[:2] or k_scale.dim() != 3 or k_scale.shape[2] < 1 or k.shape[2] % k_scale.shape[2]:
+        raise ValueError("k_scale: expected [n_seqs, n_heads, cap / block]")
+    qc = vvs_qcache(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), _ptr(mass), _ptr(age), int(k.shape[0]), int(k.shape[1]),
+                    int(k.shape[3]), int(k.shape[2]), int(k.shape[2] // k_scale.shape[2]))
+    qc._keep = (k, v, k_scale, v_scale, mass, age)
+    return qc
 
 
 def vvs_device_status(ctx: int, stream=None, raise_on_error: bool = False) -> int:

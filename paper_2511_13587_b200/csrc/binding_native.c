@@ -10,7 +10,7 @@
 #include "vvs.h"
 
 static PyObject *g_error, *g_raw_stream, *g_get_device;   /* VvsError; torch's current raw stream and device */
-static PyObject *s_data_ptr, *s_shape, *s_cuda_stream;
+static PyObject *s_data_ptr, *s_shape, *s_cuda_stream, *s_stride, *s_element_size;
 
 /* tensor (or integer address, or None) -> address; -1 with an exception set on failure */
 static int to_ptr(PyObject* o, void** out) {
@@ -275,16 +275,17 @@ static int shape_of(PyObject* t, int want, int32_t* dims) {
   Py_DECREF(sh);
   return rc;
 }
-/* the structure behind a ctypes vvs_fcache */
-static int fcache_of(PyObject* o, vvs_fcache* out) {
+/* the structure behind a ctypes object of the given size */
+static int struct_of(PyObject* o, void* out, size_t size, const char* what) {
   Py_buffer b;
   if (PyObject_GetBuffer(o, &b, PyBUF_SIMPLE) < 0) return -1;
-  const int ok = b.len == (Py_ssize_t)sizeof(*out);
-  if (ok) memcpy(out, b.buf, sizeof(*out));
+  const int ok = b.len == (Py_ssize_t)size;
+  if (ok) memcpy(out, b.buf, size);
   PyBuffer_Release(&b);
-  if (!ok) PyErr_SetString(PyExc_TypeError, "expected a vvs_fcache");
+  if (!ok) PyErr_Format(PyExc_TypeError, "expected a %s", what);
   return ok ? 0 : -1;
 }
+static int fcache_of(PyObject* o, vvs_fcache* out) { return struct_of(o, out, sizeof(*out), "vvs_fcache"); }
 
 static PyObject* py_reset(FAST) {
   (void)self;
@@ -331,6 +332,132 @@ static PyObject* py_select(FAST) {
                                                       f.out_gamma, f.out_tokens, f.stream));
 }
 
+/* ---- 8-bit cache and rotation with several axes ------------------------------------------------------------------ */
+typedef struct {
+  vvs_ctx* ctx;
+  PyObject *qc, *rope, *q, *k, *v, *q_out, *k_out, *out;
+  void *cache_len, *row_count, *row_index, *next_age, *first_slot, *visible, *lse, *mass_out, *age_out, *new_len, *kept, *stream;
+  int32_t mass_rows, max_len, keep, n_sink, n_recent;
+  float scale, mass_decay;
+} Frame3;
+#define H(f) offsetof(Frame3, f)
+static Param rotate_params[] = {
+    {"ctx", 'c', 1, H(ctx)}, {"rope", 'o', 1, H(rope)}, {"q", 'o', 1, H(q)}, {"q_out", 'o', 1, H(q_out)}, {"k", 'o', 0, H(k)},
+    {"k_out", 'o', 0, H(k_out)}, {"stream", 's', 0, H(stream)}};
+static Param append_params[] = {
+    {"ctx", 'c', 1, H(ctx)}, {"qc", 'o', 1, H(qc)}, {"k", 'o', 1, H(k)}, {"v", 'o', 1, H(v)}, {"cache_len", 'p', 1, H(cache_len)},
+    {"rope", 'o', 0, H(rope)}, {"q", 'o', 0, H(q)}, {"q_out", 'o', 0, H(q_out)}, {"row_count", 'p', 0, H(row_count)},
+    {"row_index", 'p', 0, H(row_index)}, {"next_age", 'p', 0, H(next_age)}, {"stream", 's', 0, H(stream)}};
+static Param attend_params[] = {
+    {"ctx", 'c', 1, H(ctx)}, {"qc", 'o', 1, H(qc)}, {"q", 'o', 1, H(q)}, {"out", 'o', 1, H(out)}, {"cache_len", 'p', 1, H(cache_len)},
+    {"row_count", 'p', 0, H(row_count)}, {"first_slot", 'p', 0, H(first_slot)}, {"visible", 'p', 0, H(visible)},
+    {"lse", 'p', 0, H(lse)}, {"scale", 'f', 0, H(scale)}, {"mass_rows", 'i', 0, H(mass_rows)}, {"mass_decay", 'f', 0, H(mass_decay)},
+    {"max_len", 'i', 0, H(max_len)}, {"stream", 's', 0, H(stream)}};
+static Param evict_params[] = {
+    {"ctx", 'c', 1, H(ctx)}, {"qc", 'o', 1, H(qc)}, {"cache_len", 'p', 1, H(cache_len)}, {"keep", 'i', 1, H(keep)},
+    {"n_sink", 'i', 1, H(n_sink)}, {"n_recent", 'i', 1, H(n_recent)}, {"next_age", 'p', 1, H(next_age)}, {"mass_out", 'p', 1, H(mass_out)},
+    {"age_out", 'p', 1, H(age_out)}, {"new_len", 'p', 1, H(new_len)}, {"kept", 'p', 1, H(kept)}, {"stream", 's', 0, H(stream)}};
+
+/* a tensor [n_seqs, n_rows, n_heads, head_dim] whose last dimension lies side by side, of the context's type; dims: its sizes, checked where
+ * they are not 0 */
+static int heads_of(PyObject* t, const char* name, const vvs_ctx* ctx, vvs_heads* out, int32_t dims[4]) {
+  int32_t got[4];
+  if (shape_of(t, 4, got) < 0 || to_ptr(t, &out->data) < 0) return -1;
+  for (int i = 0; i < 4; ++i) {
+    if (dims[i] && dims[i] != got[i]) {
+      PyErr_Format(PyExc_ValueError, "%s: dimension %d is %d, expected %d", name, i, got[i], dims[i]);
+      return -1;
+    }
+    dims[i] = got[i];
+  }
+  PyObject* size = PyObject_CallMethodNoArgs(t, s_element_size);
+  if (!size) return -1;
+  const long es = PyLong_AsLong(size);
+  Py_DECREF(size);
+  if (es == -1 && PyErr_Occurred()) return -1;
+  if (ctx && es != vvs_element_bytes(ctx)) {
+    PyErr_Format(PyExc_ValueError, "%s: elements of %ld bytes, the context's have %d", name, es, vvs_element_bytes(ctx));
+    return -1;
+  }
+  PyObject* st = PyObject_CallMethodNoArgs(t, s_stride);
+  if (!st) return -1;
+  long long s[4] = {0, 0, 0, 1};
+  int rc = PyTuple_Check(st) && PyTuple_GET_SIZE(st) == 4 ? 0 : -1;
+  for (int i = 0; i < 4 && rc == 0; ++i) {
+    s[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(st, i));
+    if (s[i] == -1 && PyErr_Occurred()) rc = -1;
+  }
+  Py_DECREF(st);
+  if (rc == 0 && s[3] != 1 && got[3] > 1) {
+    PyErr_Format(PyExc_ValueError, "%s: the elements of a head do not lie side by side", name);
+    rc = -1;
+  }
+  out->seq = s[0];
+  out->row = s[1];
+  out->head = s[2];
+  return rc;
+}
+static int given(PyObject* o) { return o && o != Py_None; }
+
+static PyObject* py_rotate(FAST) {
+  (void)self;
+  Frame3 f = {0};
+  vvs_rope_axes rope;
+  vvs_heads q, q_out, k, k_out;
+  int32_t d[4] = {0}, e[4] = {0};
+  if (PARSE("vvs_rotate_axes", rotate_params, N(rotate_params)) < 0 || struct_of(f.rope, &rope, sizeof(rope), "vvs_rope_axes") < 0 ||
+      heads_of(f.q, "q", f.ctx, &q, d) < 0 || heads_of(f.q_out, "q_out", f.ctx, &q_out, d) < 0)
+    return NULL;
+  const int two = given(f.k), two_out = given(f.k_out);
+  e[0] = d[0], e[1] = d[1], e[3] = d[3];
+  if (two && heads_of(f.k, "k", f.ctx, &k, e) < 0) return NULL;
+  if (two_out && heads_of(f.k_out, "k_out", f.ctx, &k_out, e) < 0) return NULL;
+  CALL("vvs_rotate_axes", vvs_rotate_axes(f.ctx, &rope, d[0], d[1], d[2], e[2], d[3], &q, &q_out, two ? &k : NULL,
+                                          two_out ? &k_out : NULL, f.stream));
+}
+static PyObject* py_append(FAST) {
+  (void)self;
+  Frame3 f = {0};
+  vvs_qcache qc;
+  vvs_rope_axes rope;
+  vvs_heads q, q_out, k, v;
+  if (PARSE("vvs_quant_cache_append", append_params, N(append_params)) < 0 || struct_of(f.qc, &qc, sizeof(qc), "vvs_qcache") < 0)
+    return NULL;
+  int32_t d[4] = {qc.n_seqs, 0, qc.n_heads, qc.head_dim}, e[4] = {0};
+  if (heads_of(f.k, "k", f.ctx, &k, d) < 0 || heads_of(f.v, "v", f.ctx, &v, d) < 0) return NULL;
+  const int turn = given(f.rope), also_q = given(f.q), also_out = given(f.q_out);
+  if (turn && struct_of(f.rope, &rope, sizeof(rope), "vvs_rope_axes") < 0) return NULL;
+  e[0] = d[0], e[1] = d[1], e[3] = d[3];
+  if (also_q && heads_of(f.q, "q", f.ctx, &q, e) < 0) return NULL;
+  if (also_out && heads_of(f.q_out, "q_out", f.ctx, &q_out, e) < 0) return NULL;
+  CALL("vvs_quant_cache_append",
+       vvs_quant_cache_append(f.ctx, &qc, &k, &v, f.cache_len, d[1], f.row_count, f.row_index, f.next_age, turn ? &rope : NULL, e[2],
+                              also_q ? &q : NULL, also_out ? &q_out : NULL, f.stream));
+}
+static PyObject* py_attend(FAST) {
+  (void)self;
+  Frame3 f = {0};
+  vvs_qcache qc;
+  vvs_heads q, out;
+  f.mass_decay = 1.f;
+  if (PARSE("vvs_quant_cache_attend", attend_params, N(attend_params)) < 0 || struct_of(f.qc, &qc, sizeof(qc), "vvs_qcache") < 0)
+    return NULL;
+  int32_t d[4] = {qc.n_seqs, 0, 0, qc.head_dim};
+  if (heads_of(f.q, "q", f.ctx, &q, d) < 0 || heads_of(f.out, "out", f.ctx, &out, d) < 0) return NULL;
+  CALL("vvs_quant_cache_attend",
+       vvs_quant_cache_attend(f.ctx, &qc, &q, &out, f.cache_len, d[1], d[2], f.row_count, f.first_slot, f.visible, f.lse, f.scale,
+                              f.mass_rows, f.mass_decay, f.max_len, f.stream));
+}
+static PyObject* py_evict(FAST) {
+  (void)self;
+  Frame3 f = {0};
+  vvs_qcache qc;
+  if (PARSE("vvs_quant_cache_evict", evict_params, N(evict_params)) < 0 || struct_of(f.qc, &qc, sizeof(qc), "vvs_qcache") < 0)
+    return NULL;
+  CALL("vvs_quant_cache_evict", vvs_quant_cache_evict(f.ctx, &qc, f.cache_len, f.keep, f.n_sink, f.n_recent, f.next_age, f.mass_out,
+                                                      f.age_out, f.new_len, f.kept, f.stream));
+}
+
 /* setup(VvsError, current_raw_stream, current_device) */
 static PyObject* py_setup(PyObject* self, PyObject* args) {
   (void)self;
@@ -362,6 +489,17 @@ static PyMethodDef methods[] = {
     FN("vvs_select_unverified", py_select,
        "Sec. 4.2 / Eq. 3: uniform draw of one candidate path per image, cut to gamma tokens: vvs_select_unverified(ctx, paths, "
        "path_len, uniforms, out_path, out_gamma, out_tokens, stream=None)."),
+    FN("vvs_rotate_axes", py_rotate,
+       "vvs_rotate_axes(ctx, rope, q, q_out, k=None, k_out=None, stream=None): q, k [n_seqs, n_rows, heads, head_dim], any strides of "
+       "whole 16 bytes but the last; rope from make_rope_axes."),
+    FN("vvs_quant_cache_append", py_append,
+       "vvs_quant_cache_append(ctx, qc, k, v, cache_len, rope=None, q=None, q_out=None, row_count=None, row_index=None, next_age=None, "
+       "stream=None): k, v [n_seqs, n_rows, cached heads, head_dim] behind cache_len int32 [n_seqs]; qc from make_qcache."),
+    FN("vvs_quant_cache_attend", py_attend,
+       "vvs_quant_cache_attend(ctx, qc, q, out, cache_len, row_count=None, first_slot=None, visible=None, lse=None, scale=0.0, mass_rows=0, "
+       "mass_decay=1.0, max_len=0, stream=None): q, out [n_seqs, n_rows, heads, head_dim]; scale 0 = 1 / sqrt(head_dim)."),
+    FN("vvs_quant_cache_evict", py_evict,
+       "vvs_quant_cache_evict(ctx, qc, cache_len, keep, n_sink, n_recent, next_age, mass_out, age_out, new_len, kept, stream=None)"),
     {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
@@ -374,9 +512,12 @@ PyMODINIT_FUNC PyInit__native(void) {
   s_data_ptr = PyUnicode_InternFromString("data_ptr");
   s_shape = PyUnicode_InternFromString("shape");
   s_cuda_stream = PyUnicode_InternFromString("cuda_stream");
+  s_stride = PyUnicode_InternFromString("stride");
+  s_element_size = PyUnicode_InternFromString("element_size");
 #define I(ps) intern(ps, N(ps)) < 0
-  if (!s_data_ptr || !s_shape || !s_cuda_stream || I(verify_params) || I(epilogue_params) || I(decide_params) || I(noalloc_params) ||
-      I(reset_params) || I(store_params) || I(fetch_params) || I(skip_params) || I(select_params))
+  if (!s_data_ptr || !s_shape || !s_cuda_stream || !s_stride || !s_element_size || I(verify_params) || I(epilogue_params) || I(decide_params) || I(noalloc_params) ||
+      I(reset_params) || I(store_params) || I(fetch_params) || I(skip_params) || I(select_params) || I(rotate_params) ||
+      I(append_params) || I(attend_params) || I(evict_params))
     return NULL;
   return PyModule_Create(&module);
 }

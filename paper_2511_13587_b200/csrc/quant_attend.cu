@@ -1,0 +1,535 @@
+// Attention of a block's rows over the 8-bit cache, and the weight that every cached key got.
+//
+// With codes c, scales K_b, V_b of the key's block and w_j = 2^(a_j - m), a_j = log2(e) scale q.k_j + log2 V_b, m a running maximum of a:
+//   out = (sum_j w_j cv_j) / (sum_j w_j / V_b),   lse = ln 2 (m + log2 sum_j w_j / V_b)
+// so a value's scale costs one addition per score, and what goes into the second product is at most 2^kShift whatever the blocks' scales
+// are: halves hold it with 11 bits.  Queries are halves too, each row times a power of two that brings its largest element near 2^14:
+// bf16 elements lose nothing but what is 2^-28 of the row's largest.  e4m3 codes are halves exactly.  Float32 contexts split a query
+// into three halves and a weight into two (33 and 22 bits).
+//
+// One pass over the cache.  A (sequence, cached head, tile of rows) is an item of a cluster of CTAs, each of them with a share of the
+// keys; a warp has slices of 16 keys of its own, brought by 16-byte asynchronous copies into a ring of its own, so no barrier is
+// met before the warps' sums are joined: in shared memory first, then over the cluster through distributed shared memory, in rank order.
+// Query rows (rows x query heads of the cached head) are the M side of mma.sync m16n8k16.  The order of a head's elements along K of the
+// first product, and of the output's columns, is the one in which a lane's codes lie side by side in memory: a 16-byte load of a
+// lane is four (keys) or eight (values) operands.
+//
+// The weights' sums need the whole row's maximum and sum: a second walk over the CTA's keys (from L2) with both at hand.
+#include "quant_cache.cuh"
+#include "tc_common.cuh"
+
+namespace vvs {
+
+namespace {
+
+constexpr int kWarps = 4;
+constexpr int kThreads = 32 * kWarps;
+constexpr int kDepth = 4;                       // slices of a warp's ring
+constexpr float kShift = 15.f;                  // weights are at most 2^15: halves keep 11 bits down to 2^-29 of the largest
+constexpr float kLog2e = 1.4426950408889634f;
+
+__device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+  const __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+// 16 bytes, or zeros
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ uint4 lds128(uint32_t at) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t at) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ float lds32(uint32_t at) {
+  float v;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+  return v;
+}
+
+template <int HD, int MT, bool F32>
+struct Layout {
+  static constexpr int kRows = 16 * MT;
+  static constexpr int kSteps = HD / 16;                                    // k-steps of the first product
+  static constexpr int kQ = F32 ? 3 : 1;                                    // halves a query element is split into
+  static constexpr int kP = F32 ? 2 : 1;                                    // ... a weight
+  static constexpr int kTile = 16 * HD;                                     // bytes of 16 keys
+  static constexpr int kSlot = 2 * kTile + 16;                              // keys, values, two scales
+  static constexpr int kRing = kDepth * kSlot;
+  static constexpr int kQBytes = kQ * MT * kSteps * 512;                    // fragments [piece][tile][step][lane] of 16 bytes
+  static constexpr int kPartBytes = kRows * HD * 4;                         // a warp's sums, over its own ring
+  static_assert(kPartBytes <= kRing, "a warp's sums take the place of its ring");
+  static constexpr int kQAt = 0;
+  static constexpr int kRingAt = kQBytes;
+  static constexpr int kMlAt = kRingAt + kWarps * kRing;                    // [kWarps][kRows][2] warps' maxima and sums
+  static constexpr int kTotAt = kMlAt + kWarps * kRows * 8;                 // [kRows][2] the CTA's
+  static constexpr int kLseAt = kTotAt + kRows * 8;                         // [kRows] log2 of the row's sum
+  static constexpr int kFacAt = kLseAt + kRows * 4;                         // [kRows] what a row's queries were divided by
+  static constexpr int kBytes = kFacAt + kRows * 4;
+};
+
+// where 16 bytes `chunk` of key `row` lie in a slice's tile, so that what the eight lanes of a quarter warp load lies in different banks
+template <int HD>
+__device__ __forceinline__ uint32_t key_at(int row, int chunk) {
+  return HD == 128 ? row * 128 + ((chunk ^ ((row & 1) << 2)) << 4) : row * 64 + (chunk << 4);
+}
+template <int HD>
+__device__ __forceinline__ uint32_t value_at(int row, int chunk) {
+  if (HD == 128) return row * 128 + ((chunk ^ (row & 6)) << 4);
+  return (row >> 1) * 128 + (((((row & 1) << 2) | chunk) ^ (row & 6)) << 4);
+}
+
+template <typename T, int HD, int MT>
+__global__ void __launch_bounds__(kThreads) quant_attend_kernel(QAttendArgs a, int tiles_each) {
+  constexpr bool F32 = sizeof(T) == 4;
+  using L = Layout<HD, MT, F32>;
+  extern __shared__ __align__(128) uint8_t smem[];
+  const uint32_t sbase = tc::smem_u32(smem);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
+  const int ranks = gridDim.x, rank = blockIdx.x, head = blockIdx.y % a.c.n_heads, group = blockIdx.y / a.c.n_heads, seq = blockIdx.z;
+  grid_dep_launch();
+  grid_dep_wait();
+
+  const int share = a.n_heads / a.c.n_heads, rows = a.n_rows * share;
+  int len = a.cache_len[seq], n = a.row_count ? a.row_count[seq] : a.n_rows, first = a.first_slot ? a.first_slot[seq] : 0;
+  uint32_t bits = 0;
+  if (n < 0 || n > a.n_rows) { bits |= VVS_DEV_BAD_ARG; n = 0; }
+  if (len < 0 || len > a.c.cap - n) { bits |= VVS_DEV_CACHE_OVERFLOW; len = 0; n = 0; }
+  if (first < 0 || first > len) { bits |= VVS_DEV_BAD_ARG; first = first < 0 ? 0 : len; }
+  if (bits && rank == 0 && blockIdx.y == 0 && tid == 0) atomicOr(a.status, bits);
+  const int end = len + n;
+
+  const size_t item = (size_t)seq * a.c.n_heads + head;
+  const uint8_t* keys = a.c.k + item * a.c.cap * HD;
+  const uint8_t* values = a.c.v + item * a.c.cap * HD;
+  const float* k_scale = a.c.k_scale + item * (a.c.cap >> a.c.block_log2);
+  const float* v_scale = a.c.v_scale + item * (a.c.cap >> a.c.block_log2);
+  // slices of 16 keys: this CTA's are s0 .. s1 - 1, this warp's every kWarps-th of them
+  const int all0 = first >> 4, all1 = (end + 15) >> 4, each = (all1 - all0 + ranks - 1) / ranks;
+  const int s0 = min(all1, all0 + rank * each), s1 = min(all1, s0 + each);
+  const uint32_t ring = sbase + L::kRingAt + warp * L::kRing;
+
+  auto request = [&](int slice, int at, bool with_values) {
+    const uint32_t slot = ring + at * L::kSlot;
+    const int slot0 = slice << 4;
+#pragma unroll
+    for (int i = 0; i < HD / 32; ++i) {
+      const int chunk = i * 32 + lane, row = chunk / (HD / 16), cc = chunk % (HD / 16);
+      const bool there = slot0 + row < end;
+      const size_t off = (size_t)(there ? slot0 + row : slot0) * HD + cc * 16;
+      copy16(slot + key_at<HD>(row, cc), keys + off, there);
+      if (with_values) copy16(slot + L::kTile + value_at<HD>(row, cc), values + off, there);
+    }
+    if (lane < 2) copy4(slot + 2 * L::kTile + 4 * lane, (lane ? v_scale : k_scale) + (slot0 >> a.c.block_log2));
+  };
+
+  for (int tile = group * tiles_each; tile < min((group + 1) * tiles_each, (rows + L::kRows - 1) / L::kRows); ++tile) {
+    const int r0 = tile * L::kRows;
+    // requests of the first slices travel while the queries are laid out
+#pragma unroll
+    for (int d = 0; d < kDepth - 1; ++d) {
+      if (s0 + warp + d * kWarps < s1) request(s0 + warp + d * kWarps, d, true);
+      tc::cp_async_commit();
+    }
+
+    // ---- queries: scaled rows as A fragments -------------------------------------------------------------------------------------
+    for (int r = warp; r < L::kRows; r += kWarps) {
+      const int row = r0 + r, t = row / share, h = head * share + row % share;
+      const bool live = row < rows && t < n;
+      constexpr int kEach = HD / 32;                         // elements of a lane: kEach * lane ..
+      float x[kEach];
+      float top = 0.f;
+      const T* src = static_cast<const T*>(a.q.data) + seq * a.q.seq + (int64_t)t * a.q.row + h * a.q.head;
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) {
+        x[e] = live ? static_cast<float>(src[kEach * lane + e]) : 0.f;
+        top = fmaxf(top, fabsf(x[e]));
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      // a power of two (its biased exponent) that brings the largest element to [2^13, 2^14)
+      const int e_top = (int)(__float_as_uint(top) >> 23);
+      const int up = top > 0.f && e_top < 255 ? min(max(127 + 13 + 127 - e_top, 1), 253) : 127;
+      const float mul = __uint_as_float((uint32_t)up << 23);
+      if (lane == 0) reinterpret_cast<float*>(smem + L::kFacAt)[r] = __uint_as_float((uint32_t)(254 - up) << 23);
+      // element d = 64 h' + 16 c' + 4 s' + e is k-step 4 h' + s', lane column c', register pair e / 2, half e % 2
+#pragma unroll
+      for (int e = 0; e < kEach; e += 2) {
+        const int d = kEach * lane + e, step = (d >> 6) * 4 + ((d >> 2) & 3), col = (d >> 4) & 3, pair = (d >> 1) & 1;
+        const int reg = ((r >> 3) & 1) + 2 * pair, to_lane = (r & 7) * 4 + col;
+        float lo = x[e] * mul, hi = x[e + 1] * mul;
+#pragma unroll
+        for (int piece = 0; piece < L::kQ; ++piece) {
+          const uint32_t w = pack_f16(lo, hi);
+          reinterpret_cast<uint32_t*>(smem + L::kQAt)[(((piece * MT + (r >> 4)) * L::kSteps + step) * 32 + to_lane) * 4 + reg] = w;
+          const float2 f = halves_to_float2(w);
+          lo -= f.x;
+          hi -= f.y;
+        }
+      }
+    }
+    __syncthreads();
+    float fac[MT][2];                       // log2(e) scale / what the row was multiplied by
+    int t_of[MT][2];
+    uint32_t sees[MT][2];                   // rows of the block that a row sees, where they are named
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int r = mt * 16 + g + 8 * i, row = r0 + r, t = row / share;
+        fac[mt][i] = reinterpret_cast<const float*>(smem + L::kFacAt)[r] * a.scale * kLog2e;
+        t_of[mt][i] = row < rows && t < n ? t : -1;
+        sees[mt][i] = a.visible && t_of[mt][i] >= 0 ? a.visible[(size_t)seq * a.n_rows + t] : 0u;
+      }
+    auto visible = [&](int mt, int i, int slot) {
+      const int j = slot - len, t = t_of[mt][i];
+      if (j < 0) return slot >= first && t >= 0;
+      if (j >= n || t < 0) return false;
+      return a.visible ? ((sees[mt][i] >> j) & 1u) != 0u : j <= t;
+    };
+    // scores of a slice, unscaled; s[mt][nt]: keys 8 nt + 2c, + 1 of rows g, g + 8
+    auto scores = [&](uint32_t slot, float (&s)[MT][2][4]) {
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[mt][nt][e] = 0.f;
+#pragma unroll
+      for (int h = 0; h < HD / 64; ++h) {
+        uint4 k4[2];
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt) k4[nt] = lds128(slot + key_at<HD>(8 * nt + g, 4 * h + c));
+#pragma unroll
+        for (int st = 0; st < 4; ++st) {
+          uint32_t b[2][2];
+#pragma unroll
+          for (int nt = 0; nt < 2; ++nt) {
+            const uint32_t w = st == 0 ? k4[nt].x : st == 1 ? k4[nt].y : st == 2 ? k4[nt].z : k4[nt].w;
+            b[nt][0] = from_e4m3x2(w);
+            b[nt][1] = from_e4m3x2(w >> 16);
+          }
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int piece = L::kQ - 1; piece >= 0; --piece) {
+              const uint4 q4 = lds128(sbase + L::kQAt + ((piece * MT + mt) * L::kSteps + 4 * h + st) * 512 + lane * 16);
+              const uint32_t q[4] = {q4.x, q4.y, q4.z, q4.w};
+#pragma unroll
+              for (int nt = 0; nt < 2; ++nt) mma_f16(s[mt][nt], q, b[nt][0], b[nt][1]);
+            }
+        }
+      }
+    };
+
+    // ---- the cache, once -------------------------------------------------------------------------------------------------------------
+    float m[MT][2], l[MT][2], o[MT][HD / 8][4];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) { m[mt][i] = -CUDART_INF_F; l[mt][i] = 0.f; }
+#pragma unroll
+      for (int j = 0; j < HD / 8; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[mt][j][e] = 0.f;
+    }
+    int at = 0;
+    for (int slice = s0 + warp; slice < s1; slice += kWarps) {
+      tc::cp_async_wait<kDepth - 2>();
+      __syncwarp();
+      const uint32_t slot = ring + at * L::kSlot;
+      const float ks = lds32(slot + 2 * L::kTile), vs = lds32(slot + 2 * L::kTile + 4);
+      float s[MT][2][4];
+      scores(slot, s);
+      const float lv = __log2f(vs), inv_vs = 1.f / vs;
+      const int slot0 = slice << 4;
+      const bool whole = slot0 >= first && slot0 + 16 <= len;
+      uint32_t p[L::kP][MT][4];
+      bool same = true;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        float alpha[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float f = fac[mt][i] * ks;
+          float v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            v[e] = fmaf(s[mt][e >> 1][2 * i + (e & 1)], f, lv);
+            if (!whole && !visible(mt, i, slot0 + 8 * (e >> 1) + 2 * c + (e & 1))) v[e] = -CUDART_INF_F;
+          }
+          float mx = fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+          const float m_new = fmaxf(m[mt][i], mx), m_safe = m_new == -CUDART_INF_F ? 0.f : m_new - kShift;
+          alpha[i] = ex2(m[mt][i] - m_new);
+          if (m_new == -CUDART_INF_F) alpha[i] = 1.f;
+          same = same && m_new == m[mt][i];
+          m[mt][i] = m_new;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = ex2(v[e] - m_safe);
+          l[mt][i] = fmaf(l[mt][i], alpha[i], ((v[0] + v[1]) + (v[2] + v[3])) * inv_vs);
+#pragma unroll
+          for (int nt = 0; nt < 2; ++nt) {
+            p[0][mt][i + 2 * nt] = pack_f16(v[2 * nt], v[2 * nt + 1]);
+            if (F32) {
+              const float2 hi = halves_to_float2(p[0][mt][i + 2 * nt]);
+              p[L::kP - 1][mt][i + 2 * nt] = pack_f16(v[2 * nt] - hi.x, v[2 * nt + 1] - hi.y);
+            }
+          }
+        }
+        if (!__all_sync(0xffffffffu, same)) {
+#pragma unroll
+          for (int j = 0; j < HD / 8; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[mt][j][e] *= alpha[e >> 1];
+        }
+      }
+      // values: this lane's keys are 2c, 2c + 1, 8 + 2c, 9 + 2c, its columns g * HD / 8 ..
+      uint32_t w[4][HD / 32];
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) {
+        const int row = (kk >> 1) * 8 + 2 * c + (kk & 1);
+        if (HD == 128) {
+          const uint4 t = lds128(slot + L::kTile + value_at<HD>(row, g));
+          w[kk][0] = t.x; w[kk][1] = t.y; w[kk][HD / 32 - 2] = t.z; w[kk][HD / 32 - 1] = t.w;
+        } else {
+          const uint2 t = lds64(slot + L::kTile + value_at<HD>(row, g >> 1) + (g & 1) * 8);
+          w[kk][0] = t.x; w[kk][1] = t.y;
+        }
+      }
+#pragma unroll
+      for (int wi = 0; wi < HD / 32; ++wi) {
+        uint32_t b[2][4];
+#pragma unroll
+        for (int kp = 0; kp < 2; ++kp) {
+          const uint32_t x = __byte_perm(w[2 * kp][wi], w[2 * kp + 1][wi], 0x5140), y = __byte_perm(w[2 * kp][wi], w[2 * kp + 1][wi], 0x7362);
+          b[kp][0] = from_e4m3x2(x);
+          b[kp][1] = from_e4m3x2(x >> 16);
+          b[kp][2] = from_e4m3x2(y);
+          b[kp][3] = from_e4m3x2(y >> 16);
+        }
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int piece = L::kP - 1; piece >= 0; --piece) mma_f16(o[mt][4 * wi + j], p[piece][mt], b[0][j], b[1][j]);
+      }
+      __syncwarp();
+      if (slice + (kDepth - 1) * kWarps < s1) request(slice + (kDepth - 1) * kWarps, (at + kDepth - 1) % kDepth, true);
+      tc::cp_async_commit();
+      at = (at + 1) % kDepth;
+    }
+    tc::cp_async_wait<0>();
+    __syncwarp();
+
+    // ---- the warps' sums, then the ranks' -----------------------------------------------------------------------------------------------
+    float* part = reinterpret_cast<float*>(smem + L::kRingAt + warp * L::kRing);
+    float* ml = reinterpret_cast<float*>(smem + L::kMlAt);
+    float* tot = reinterpret_cast<float*>(smem + L::kTotAt);
+    float* lse2 = reinterpret_cast<float*>(smem + L::kLseAt);
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        l[mt][i] += __shfl_xor_sync(0xffffffffu, l[mt][i], 1);
+        l[mt][i] += __shfl_xor_sync(0xffffffffu, l[mt][i], 2);
+        const int r = mt * 16 + g + 8 * i;
+        if (c == 0) {
+          ml[(warp * L::kRows + r) * 2] = m[mt][i];
+          ml[(warp * L::kRows + r) * 2 + 1] = l[mt][i];
+        }
+        // columns c * HD / 4 + 0 .. HD / 8 - 1 (elements 0 and 2), + HD / 8 .. (elements 1 and 3)
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int j = 0; j < HD / 8; j += 4)
+            *reinterpret_cast<float4*>(part + r * HD + c * (HD / 4) + half * (HD / 8) + j) =
+                make_float4(o[mt][j][2 * i + half], o[mt][j + 1][2 * i + half], o[mt][j + 2][2 * i + half], o[mt][j + 3][2 * i + half]);
+      }
+    __syncthreads();
+    constexpr int kVecs = L::kRows * HD / 4;
+    for (int v = tid; v < kVecs; v += kThreads) {
+      const int r = v / (HD / 4);
+      float top = -CUDART_INF_F;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) top = fmaxf(top, ml[(w * L::kRows + r) * 2]);
+      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+      float total = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float mw = ml[(w * L::kRows + r) * 2], f = mw == -CUDART_INF_F ? 0.f : ex2(mw - top);
+        const float4 x = reinterpret_cast<const float4*>(smem + L::kRingAt + w * L::kRing)[v];
+        sum.x = fmaf(x.x, f, sum.x); sum.y = fmaf(x.y, f, sum.y); sum.z = fmaf(x.z, f, sum.z); sum.w = fmaf(x.w, f, sum.w);
+        total = fmaf(ml[(w * L::kRows + r) * 2 + 1], f, total);
+      }
+      reinterpret_cast<float4*>(smem + L::kRingAt)[v] = sum;              // (of warp 0's sums this thread reads no other)
+      if (v % (HD / 4) == 0) { tot[2 * r] = top; tot[2 * r + 1] = total; }
+    }
+    if (ranks > 1) tc::cluster_sync(); else __syncthreads();
+    const uint32_t tot_at = sbase + L::kTotAt, sum_at = sbase + L::kRingAt;
+    for (int v = rank * kThreads + tid; v < kVecs; v += ranks * kThreads) {
+      const int r = v / (HD / 4), row = r0 + r;
+      if (row >= rows) break;
+      const int t = row / share, h = head * share + row % share;
+      float top = -CUDART_INF_F;
+      for (int k = 0; k < ranks; ++k) top = fmaxf(top, tc::ld_cluster_f32(tot_at + 8 * r, k));
+      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+      float total = 0.f;
+      for (int k = 0; k < ranks; ++k) {
+        const float mk = tc::ld_cluster_f32(tot_at + 8 * r, k), f = mk == -CUDART_INF_F ? 0.f : ex2(mk - top);
+        const float4 x = tc::ld_cluster_f4(sum_at + 16 * v, k);
+        sum.x = fmaf(x.x, f, sum.x); sum.y = fmaf(x.y, f, sum.y); sum.z = fmaf(x.z, f, sum.z); sum.w = fmaf(x.w, f, sum.w);
+        total = fmaf(tc::ld_cluster_f32(tot_at + 8 * r + 4, k), f, total);
+      }
+      const bool some = t < n && !(total == 0.f);            // (a NaN among the queries is an answer of NaN)
+      const float inv = some ? 1.f / total : 0.f;
+      float x[4] = {sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv};
+      if (!some) x[0] = x[1] = x[2] = x[3] = 0.f;
+      store4(static_cast<T*>(a.out.data) + seq * a.out.seq + (int64_t)t * a.out.row + h * a.out.head + v % (HD / 4) * 4, x);
+      if (a.lse && v % (HD / 4) == 0)
+        a.lse[((size_t)seq * a.n_rows + t) * a.n_heads + h] = some ? (top - kShift + log2f(total)) / kLog2e : -CUDART_INF_F;
+    }
+
+    // ---- weights of this CTA's keys ---------------------------------------------------------------------------------------------------
+    if (a.mass_rows > 0) {
+      if (tid < L::kRows) {
+        float top = -CUDART_INF_F, total = 0.f;
+        for (int k = 0; k < ranks; ++k) top = fmaxf(top, tc::ld_cluster_f32(tot_at + 8 * tid, k));
+        for (int k = 0; k < ranks; ++k) {
+          const float mk = tc::ld_cluster_f32(tot_at + 8 * tid, k);
+          total = fmaf(tc::ld_cluster_f32(tot_at + 8 * tid + 4, k), mk == -CUDART_INF_F ? 0.f : ex2(mk - top), total);
+        }
+        lse2[tid] = total == 0.f ? CUDART_INF_F : top - kShift + log2f(total);
+      }
+    }
+    if (ranks > 1) tc::cluster_sync(); else __syncthreads();              // the other ranks have read this one's sums
+    if (a.mass_rows > 0) {
+      const bool begin = tile == 0;
+      float* mass = a.c.mass + item * a.c.cap;
+      // slots before the first that is seen only lose
+      if (begin && a.mass_decay != 1.f)
+        for (int slot = rank * kThreads + tid; slot < all0 * 16 && slot < end; slot += ranks * kThreads)
+          mass[slot] = a.mass_decay == 0.f ? 0.f : a.mass_decay * mass[slot];
+      float sub[MT][2];
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) sub[mt][i] = t_of[mt][i] >= 0 && t_of[mt][i] < a.mass_rows ? lse2[mt * 16 + g + 8 * i] : CUDART_INF_F;
+#pragma unroll
+      for (int d = 0; d < kDepth - 1; ++d) {
+        if (s0 + warp + d * kWarps < s1) request(s0 + warp + d * kWarps, d, false);
+        tc::cp_async_commit();
+      }
+      at = 0;
+      for (int slice = s0 + warp; slice < s1; slice += kWarps) {
+        tc::cp_async_wait<kDepth - 2>();
+        __syncwarp();
+        const uint32_t slot = ring + at * L::kSlot;
+        const float ks = lds32(slot + 2 * L::kTile);
+        float s[MT][2][4];
+        scores(slot, s);
+        const int slot0 = slice << 4;
+        const bool whole = slot0 >= first && slot0 + 16 <= len;
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const float f = fac[mt][i] * ks;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float w = ex2(fmaf(s[mt][e >> 1][2 * i + (e & 1)], f, -sub[mt][i]));
+              if (sub[mt][i] != CUDART_INF_F && (whole || visible(mt, i, slot0 + 8 * (e >> 1) + 2 * c + (e & 1)))) sum[e] += w;
+            }
+          }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          sum[e] += __shfl_xor_sync(0xffffffffu, sum[e], 4);
+          sum[e] += __shfl_xor_sync(0xffffffffu, sum[e], 8);
+          sum[e] += __shfl_xor_sync(0xffffffffu, sum[e], 16);
+        }
+        if (lane < 4) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int key = slot0 + 8 * (e >> 1) + 2 * c + (e & 1);
+            if (key >= end) continue;
+            const float decay = begin ? a.mass_decay : 1.f;
+            mass[key] = decay == 0.f ? sum[e] : fmaf(decay, mass[key], sum[e]);
+          }
+        }
+        __syncwarp();
+        if (slice + (kDepth - 1) * kWarps < s1) request(slice + (kDepth - 1) * kWarps, (at + kDepth - 1) % kDepth, false);
+        tc::cp_async_commit();
+        at = (at + 1) % kDepth;
+      }
+      tc::cp_async_wait<0>();
+      __syncthreads();
+    }
+  }
+}
+
+template <typename T, int HD, int MT>
+int launch_tiles(const QAttendArgs& a, cudaStream_t s) {
+  using L = Layout<HD, MT, sizeof(T) == 4>;
+  const int rows = a.n_rows * (a.n_heads / a.c.n_heads), tiles = (rows + L::kRows - 1) / L::kRows;
+  // the weights' sums of a key are added by one thread: a CTA goes through all tiles of rows then
+  const int tiles_each = a.mass_rows > 0 ? tiles : 1, groups = (tiles + tiles_each - 1) / tiles_each;
+  const long long items = (long long)a.c.n_seqs * a.c.n_heads * groups;
+  const int slices = ((a.max_len > 0 && a.max_len < a.c.cap ? a.max_len : a.c.cap) + 15) / 16;
+  int ranks = 1;
+  while (ranks < 16 && items * ranks * 2 <= 2LL * a.n_sms && slices >= 2 * ranks * kWarps) ranks *= 2;
+  auto kernel = quant_attend_kernel<T, HD, MT>;
+  if (ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), L::kBytes) != cudaSuccess) return VVS_ERR_CUDA;
+  if (ranks > 8 && cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return VVS_ERR_CUDA;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(ranks, a.c.n_heads * groups, a.c.n_seqs);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = L::kBytes;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = ranks;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, kernel, a, tiles_each) == cudaSuccess ? VVS_OK : VVS_ERR_CUDA;
+}
+
+template <typename T, int HD>
+int launch_hd(const QAttendArgs& a, cudaStream_t s) {
+  const int rows = a.n_rows * (a.n_heads / a.c.n_heads);
+  return rows <= 16 ? launch_tiles<T, HD, 1>(a, s) : launch_tiles<T, HD, 2>(a, s);
+}
+
+}  // namespace
+
+template <typename T>
+int launch_quant_attend(const QAttendArgs& a, cudaStream_t s) {
+  return a.c.hd == 64 ? launch_hd<T, 64>(a, s) : launch_hd<T, 128>(a, s);
+}
+template int launch_quant_attend<float>(const QAttendArgs&, cudaStream_t);
+template int launch_quant_attend<__nv_bfloat16>(const QAttendArgs&, cudaStream_t);
+
+}  // namespace vvs

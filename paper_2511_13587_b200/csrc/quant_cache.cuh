@@ -1,0 +1,199 @@
+// The 8-bit key / value cache (e4m3 codes, one float32 scale for each block of slots and head) and rotary positions with several
+// axes: parameters of the kernels, and what several of them do with a value.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <math_constants.h>
+
+#include "vvs_internal.cuh"
+
+namespace vvs {
+
+// rows of heads as the kernels read them (strides in elements)
+struct HeadRows {
+  void* data;
+  int64_t seq, row, head;
+};
+
+struct RopeAxes {
+  const float* inv_freq;
+  const int32_t* axis;
+  const int32_t* pos;    // [n_axes][n_seqs][n_rows]
+  int n_axes, n_pairs, halves;
+};
+
+struct QCache {
+  uint8_t *k, *v;
+  float *k_scale, *v_scale, *mass;
+  int32_t* age;
+  int n_seqs, n_heads, hd, cap, block_log2;
+};
+
+struct RotateArgs {
+  RopeAxes rope;
+  HeadRows q, q_out, k, k_out;
+  int n_seqs, n_rows, n_heads, n_kv_heads, hd;
+  int32_t* status;
+  int n_sms;
+};
+template <typename T>
+int launch_rotate_axes(const RotateArgs& a, cudaStream_t s);
+
+struct QAppendArgs {
+  QCache c;
+  HeadRows k, v, q, q_out;
+  RopeAxes rope;               // inv_freq null: nothing is turned
+  const int32_t *cache_len, *row_count, *row_index, *next_age;
+  int n_rows, n_heads;         // n_heads 0: no q
+  int32_t* status;
+  int n_sms;
+};
+template <typename T>
+int launch_quant_append(const QAppendArgs& a, cudaStream_t s);
+
+struct QAttendArgs {
+  QCache c;
+  HeadRows q, out;
+  const int32_t *cache_len, *row_count, *first_slot;
+  const uint32_t* visible;
+  float* lse;
+  float scale, mass_decay;
+  int n_rows, n_heads, mass_rows, max_len;
+  int32_t* status;
+  int n_sms;
+};
+template <typename T>
+int launch_quant_attend(const QAttendArgs& a, cudaStream_t s);
+
+struct QEvictArgs {
+  QCache c;
+  const int32_t *cache_len, *next_age;
+  int keep, n_sink, n_recent;
+  float* mass_out;
+  int32_t *age_out, *new_len, *kept;
+  int32_t* status;
+  int n_sms;
+};
+int launch_quant_evict(const QEvictArgs& a, cudaStream_t s);
+
+// ---- eight values of a row, 16 bytes of bf16 or 32 of float32; or two groups of four -----------------------------------
+__device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&x)[8]) {
+  const uint4 t = *reinterpret_cast<const uint4*>(p);
+  const uint32_t w[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(w[i] << 16);
+    x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
+  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+  x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+}
+__device__ __forceinline__ void load4(const __nv_bfloat16* p, float* x) {
+  const uint2 t = *reinterpret_cast<const uint2*>(p);
+  x[0] = __uint_as_float(t.x << 16); x[1] = __uint_as_float(t.x & 0xffff0000u);
+  x[2] = __uint_as_float(t.y << 16); x[3] = __uint_as_float(t.y & 0xffff0000u);
+}
+__device__ __forceinline__ void load4(const float* p, float* x) {
+  const float4 a = *reinterpret_cast<const float4*>(p);
+  x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+}
+__device__ __forceinline__ uint32_t pack_bf16x2(float a, float b) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ void store4(__nv_bfloat16* p, const float* x) {
+  *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
+}
+__device__ __forceinline__ void store4(float* p, const float* x) { *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]); }
+__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&x)[8]) {
+  *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+}
+__device__ __forceinline__ void store8(float* p, const float (&x)[8]) { store4(p, x); store4(p + 4, x + 4); }
+
+// ---- rotation ---------------------------------------------------------------------------------------------------------
+// A head is worked on in units of eight elements.  Neighbouring pairs: unit u is elements 8u .. 8u + 7, pairs 4u .. 4u + 3.
+// Halves: units below n_pairs / 4 are elements 4u .. 4u + 3 and n_pairs + 4u .. n_pairs + 4u + 3, pairs 4u .. 4u + 3; those behind
+// are the elements that stay as they are, 8u .. 8u + 7 (n_pairs is a multiple of four there).
+__device__ __forceinline__ bool unit_split(const RopeAxes& r, int u) { return r.halves && 4 * u < r.n_pairs; }
+
+// cosine and sine of a pair's angle; pairs behind the last and pairs of an unknown axis are not turned
+__device__ __forceinline__ void pair_turn(const RopeAxes& r, int pair, int seq, int row, int n_seqs, int n_rows, int32_t* status, float& c, float& s) {
+  c = 1.f;
+  s = 0.f;
+  if (pair >= r.n_pairs) return;
+  const int ax = r.axis[pair];
+  if (ax < 0 || ax >= r.n_axes) {
+    atomicOr(status, VVS_DEV_BAD_ARG);
+    return;
+  }
+  const float angle = __fmul_rn((float)r.pos[((size_t)ax * n_seqs + seq) * n_rows + row], r.inv_freq[pair]);
+  sincosf(angle, &s, &c);
+}
+
+// products and sum rounded one by one: what a rotation gives does not depend on the kernel that it is part of
+__device__ __forceinline__ void turn(float& x0, float& x1, float c, float s) {
+  const float a = __fsub_rn(__fmul_rn(x0, c), __fmul_rn(x1, s));
+  x1 = __fadd_rn(__fmul_rn(x1, c), __fmul_rn(x0, s));
+  x0 = a;
+}
+// x: a unit's elements as unit_split orders them
+__device__ __forceinline__ void turn_unit(float (&x)[8], bool split, const float* c, const float* s) {
+  if (split) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) turn(x[i], x[4 + i], c[i], s[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) turn(x[2 * i], x[2 * i + 1], c[i], s[i]);
+  }
+}
+template <typename T>
+__device__ __forceinline__ void load_unit(const T* row, int u, bool split, int n_pairs, float (&x)[8]) {
+  if (split) {
+    load4(row + 4 * u, x);
+    load4(row + n_pairs + 4 * u, x + 4);
+  } else {
+    load8(row + 8 * u, x);
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store_unit(T* row, int u, bool split, int n_pairs, const float (&x)[8]) {
+  if (split) {
+    store4(row + 4 * u, x);
+    store4(row + n_pairs + 4 * u, x + 4);
+  } else {
+    store8(row + 8 * u, x);
+  }
+}
+
+// ---- e4m3 -------------------------------------------------------------------------------------------------------------
+// the smallest power of two, 2^-60 at least, by which amax is at most 448 = 1.75 * 2^8
+__device__ __forceinline__ float scale_of(float amax) {
+  const uint32_t b = __float_as_uint(amax);
+  int e = (int)(b >> 23) - 8 + ((b & 0x7fffffu) > 0x600000u ? 1 : 0);      // biased exponent of the scale
+  e = e < 67 ? 67 : e;                                                      // (a subnormal amax has biased exponent 0)
+  return __uint_as_float((uint32_t)e << 23);
+}
+// four values to four codes, to nearest, ties to even, values beyond 448 to 448
+__device__ __forceinline__ uint32_t to_e4m3x4(float a, float b, float c, float d) {
+  uint16_t lo, hi;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(b), "f"(a));
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(d), "f"(c));
+  return (uint32_t)lo | ((uint32_t)hi << 16);
+}
+// two codes (of the low half of w) to two halves
+__device__ __forceinline__ uint32_t from_e4m3x2(uint32_t w) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)w));
+  return r;
+}
+__device__ __forceinline__ float2 halves_to_float2(uint32_t h) { return __half22float2(*reinterpret_cast<const __half2*>(&h)); }
+// four codes times a factor, to codes again
+__device__ __forceinline__ uint32_t rescale_e4m3x4(uint32_t w, float f) {
+  const float2 lo = halves_to_float2(from_e4m3x2(w)), hi = halves_to_float2(from_e4m3x2(w >> 16));
+  return to_e4m3x4(lo.x * f, lo.y * f, hi.x * f, hi.y * f);
+}
+
+}  // namespace vvs

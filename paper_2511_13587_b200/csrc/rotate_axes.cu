@@ -1,0 +1,73 @@
+// Rotary positions with several axes on the query and key heads of a block of rows.  Reads every element once and writes it
+// once: bound by HBM for prompts, by the launch for a step's rows.  A thread has one unit of eight elements of a row, computes its
+// four angles once and goes through a group of heads with them: sines and cosines of float32 angles (some 40 instructions each)
+// cost more than the elements' traffic if every head computes its own.
+#include "quant_cache.cuh"
+
+namespace vvs {
+
+namespace {
+
+constexpr int kThreads = 128;
+constexpr int kFlight = 4;   // heads whose loads are in flight together
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads) rotate_axes_kernel(RotateArgs a, int heads_each) {
+  grid_dep_launch();
+  grid_dep_wait();
+  const int units = a.hd / 8;
+  const long long i = (long long)blockIdx.x * kThreads + threadIdx.x;
+  if (i >= (long long)a.n_seqs * a.n_rows * units) return;
+  const int u = (int)(i % units);
+  const int at = (int)(i / units), row = at % a.n_rows, seq = at / a.n_rows;
+  float c[4], s[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) pair_turn(a.rope, 4 * u + j, seq, row, a.n_seqs, a.n_rows, a.status, c[j], s[j]);
+  const bool split = unit_split(a.rope, u);
+  if (a.rope.halves && !split) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) { c[j] = 1.f; s[j] = 0.f; }
+  }
+  const int heads = a.n_heads + a.n_kv_heads, h0 = blockIdx.y * heads_each, h1 = min(heads, h0 + heads_each);
+  const T* q = static_cast<const T*>(a.q.data) + seq * a.q.seq + row * a.q.row;
+  const T* k = static_cast<const T*>(a.k.data) + seq * a.k.seq + row * a.k.row;
+  T* qo = static_cast<T*>(a.q_out.data) + seq * a.q_out.seq + row * a.q_out.row;
+  T* ko = static_cast<T*>(a.k_out.data) + seq * a.k_out.seq + row * a.k_out.row;
+  for (int h = h0; h < h1; h += kFlight) {
+    float x[kFlight][8];
+#pragma unroll
+    for (int j = 0; j < kFlight; ++j) {
+      const int hh = h + j;
+      if (hh >= h1) break;
+      load_unit(hh < a.n_heads ? q + hh * a.q.head : k + (hh - a.n_heads) * a.k.head, u, split, a.rope.n_pairs, x[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < kFlight; ++j) {
+      const int hh = h + j;
+      if (hh >= h1) break;
+      turn_unit(x[j], split, c, s);
+      store_unit(hh < a.n_heads ? qo + hh * a.q_out.head : ko + (hh - a.n_heads) * a.k_out.head, u, split, a.rope.n_pairs, x[j]);
+    }
+  }
+}
+
+}  // namespace
+
+template <typename T>
+int launch_rotate_axes(const RotateArgs& a, cudaStream_t s) {
+  const long long threads = (long long)a.n_seqs * a.n_rows * (a.hd / 8);
+  const int heads = a.n_heads + a.n_kv_heads;
+  // as many groups of heads as fill the device with threads (2048 an SM)
+  const long long room = (long long)a.n_sms * 2048;
+  int groups = (int)((room + threads - 1) / threads);
+  groups = groups < 1 ? 1 : groups > heads ? heads : groups;
+  const int each = (heads + groups - 1) / groups;
+  const long long blocks = (threads + kThreads - 1) / kThreads;
+  if (blocks > 0x7fffffffLL) return VVS_ERR_SHAPE;
+  const cudaError_t e = launch_kernel(rotate_axes_kernel<T>, dim3((unsigned)blocks, (heads + each - 1) / each), dim3(kThreads), 0, true, s, a, each);
+  return e == cudaSuccess ? VVS_OK : VVS_ERR_CUDA;
+}
+template int launch_rotate_axes<float>(const RotateArgs&, cudaStream_t);
+template int launch_rotate_axes<__nv_bfloat16>(const RotateArgs&, cudaStream_t);
+
+}  // namespace vvs
