@@ -15,6 +15,8 @@
 // lane is four (keys) or eight (values) operands.
 //
 // The weights' sums need the whole row's maximum and sum: a second walk over the CTA's keys (from L2) with both at hand.
+#include <type_traits>
+
 #include "quant_cache.cuh"
 #include "tc_common.cuh"
 
@@ -24,8 +26,11 @@ namespace {
 
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
-constexpr int kDepth = 4;                       // slices of a warp's ring
-constexpr float kShift = 15.f;                  // weights are at most 2^15: halves keep 11 bits down to 2^-29 of the largest
+// The reference m of a row moves only when a score passes it by more than kSlack: weights are 2^kShift at the reference, 2^15 at most, and
+// halves keep 11 bits down to 2^-21 of the reference's.  After a row's first slices its sums are hardly ever scaled again, and no lane
+// has to ask the others for their largest score.
+constexpr float kShift = 7.f, kSlack = 8.f;
+constexpr int kScoreBytes = 20 * 1024;          // of a CTA's shared memory for scores of rows whose weights are summed
 constexpr float kLog2e = 1.4426950408889634f;
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t* a, uint32_t b0, uint32_t b1) {
@@ -42,26 +47,33 @@ __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
   const __half2 h = __floats2half2_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
-// 16 bytes, or zeros
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+// 16 bytes from an address and a constant offset; or `bytes` of them, the rest zeros
+template <int TO, int FROM>
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0 + %2], [%1 + %3], 16;" ::"r"(dst), "l"(src), "n"(TO), "n"(FROM) : "memory");
+}
+__device__ __forceinline__ void copy16_some(uint32_t dst, const void* src, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void copy4(uint32_t dst, const void* src) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
+template <int OFF>
 __device__ __forceinline__ uint4 lds128(uint32_t at) {
   uint4 v;
-  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4 + %5];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at), "n"(OFF) : "memory");
   return v;
 }
+template <int OFF>
 __device__ __forceinline__ uint2 lds64(uint32_t at) {
   uint2 v;
-  asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
+  asm volatile("ld.shared.v2.u32 {%0,%1}, [%2 + %3];" : "=r"(v.x), "=r"(v.y) : "r"(at), "n"(OFF) : "memory");
   return v;
 }
+template <int OFF>
 __device__ __forceinline__ float lds32(uint32_t at) {
   float v;
-  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+  asm volatile("ld.shared.f32 %0, [%1 + %2];" : "=f"(v) : "r"(at), "n"(OFF) : "memory");
   return v;
 }
 
@@ -72,6 +84,7 @@ struct Layout {
   static constexpr int kQ = F32 ? 3 : 1;                                    // halves a query element is split into
   static constexpr int kP = F32 ? 2 : 1;                                    // ... a weight
   static constexpr int kTile = 16 * HD;                                     // bytes of 16 keys
+  static constexpr int kDepth = MT == 2 ? 4 : 3;                            // slices of a warp's ring
   static constexpr int kSlot = 2 * kTile + 16;                              // keys, values, two scales
   static constexpr int kRing = kDepth * kSlot;
   static constexpr int kQBytes = kQ * MT * kSteps * 512;                    // fragments [piece][tile][step][lane] of 16 bytes
@@ -83,7 +96,12 @@ struct Layout {
   static constexpr int kTotAt = kMlAt + kWarps * kRows * 8;                 // [kRows][2] the CTA's
   static constexpr int kLseAt = kTotAt + kRows * 8;                         // [kRows] log2 of the row's sum
   static constexpr int kFacAt = kLseAt + kRows * 4;                         // [kRows] what a row's queries were divided by
-  static constexpr int kBytes = kFacAt + kRows * 4;
+  static constexpr int kScoreAt = kFacAt + kRows * 4;                       // [rows that are summed][keys of the CTA] log2 scores
+  static constexpr int kBytes = kScoreAt;
+  // query fragments stay in registers where they are at most 32 of them
+  static constexpr bool kQRegs = kQ * MT * kSteps * 4 <= 32;
+  // CTAs an SM holds by registers: 64 sums of a lane for heads of 128, twice as many for two tiles of rows
+  static constexpr int kCtas = MT * HD == 256 ? 2 : MT * HD == 128 ? (F32 ? 2 : 3) : 4;
 };
 
 // where 16 bytes `chunk` of key `row` lie in a slice's tile, so that what the eight lanes of a quarter warp load lies in different banks
@@ -98,9 +116,10 @@ __device__ __forceinline__ uint32_t value_at(int row, int chunk) {
 }
 
 template <typename T, int HD, int MT>
-__global__ void __launch_bounds__(kThreads) quant_attend_kernel(QAttendArgs a, int tiles_each) {
+__global__ void __launch_bounds__(kThreads, Layout<HD, MT, sizeof(T) == 4>::kCtas) quant_attend_kernel(QAttendArgs a, int tiles_each, int score_bytes) {
   constexpr bool F32 = sizeof(T) == 4;
   using L = Layout<HD, MT, F32>;
+  constexpr int kDepth = L::kDepth;
   extern __shared__ __align__(128) uint8_t smem[];
   const uint32_t sbase = tc::smem_u32(smem);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
@@ -127,26 +146,58 @@ __global__ void __launch_bounds__(kThreads) quant_attend_kernel(QAttendArgs a, i
   const int s0 = min(all1, all0 + rank * each), s1 = min(all1, s0 + each);
   const uint32_t ring = sbase + L::kRingAt + warp * L::kRing;
 
-  auto request = [&](int slice, int at, bool with_values) {
-    const uint32_t slot = ring + at * L::kSlot;
-    const int slot0 = slice << 4;
+  // a slice is 16 HD bytes side by side; of each 512 of them a lane copies 16
+  const uint32_t key_to = ring + key_at<HD>(lane / (HD / 16), lane % (HD / 16));
+  const uint32_t value_to = ring + L::kTile + value_at<HD>(lane / (HD / 16), lane % (HD / 16));
+  // of heads of 128, 512 bytes are four rows: every other four have their pieces in another order
+  const uint32_t value_odd = HD == 128 ? ring + L::kTile + value_at<HD>(lane / 8 + 4, lane % 8) - 512 : value_to;
+  const uint8_t *keys_at = keys + lane * 16, *values_at = values + lane * 16;
+  const float* scale_at = lane ? v_scale : k_scale;
+  auto request = [&](int slice, uint32_t at, bool with_values) {
+    const size_t from = (size_t)slice * (16 * HD);
+    const int left = end - (slice << 4);
+    if (left >= 16) {
+      copy16<0, 0>(key_to + at, keys_at + from);
+      copy16<512, 512>(key_to + at, keys_at + from);
+      if (HD == 128) {
+        copy16<1024, 1024>(key_to + at, keys_at + from);
+        copy16<1536, 1536>(key_to + at, keys_at + from);
+      }
+      if (with_values) {
+        copy16<0, 0>(value_to + at, values_at + from);
+        copy16<512, 512>(value_odd + at, values_at + from);
+        if (HD == 128) {
+          copy16<1024, 1024>(value_to + at, values_at + from);
+          copy16<1536, 1536>(value_odd + at, values_at + from);
+        }
+      }
+    } else {                                                              // the last slice: zeros behind the last key
 #pragma unroll
-    for (int i = 0; i < HD / 32; ++i) {
-      const int chunk = i * 32 + lane, row = chunk / (HD / 16), cc = chunk % (HD / 16);
-      const bool there = slot0 + row < end;
-      const size_t off = (size_t)(there ? slot0 + row : slot0) * HD + cc * 16;
-      copy16(slot + key_at<HD>(row, cc), keys + off, there);
-      if (with_values) copy16(slot + L::kTile + value_at<HD>(row, cc), values + off, there);
+      for (int i = 0; i < HD / 32; ++i) {
+        const bool there = i * (512 / HD) + lane / (HD / 16) < left;
+        const size_t off = there ? from + i * 512 : from;
+        copy16_some(key_to + at + i * 512, keys_at + off, there ? 16 : 0);
+        if (with_values) copy16_some((i & 1 ? value_odd : value_to) + at + i * 512, values_at + off, there ? 16 : 0);
+      }
     }
-    if (lane < 2) copy4(slot + 2 * L::kTile + 4 * lane, (lane ? v_scale : k_scale) + (slot0 >> a.c.block_log2));
+    if (lane < 2) copy4(ring + at + 2 * L::kTile + 4 * lane, scale_at + (slice >> (a.c.block_log2 - 4)));
   };
+  // where this lane's operands lie in a slice: keys g and 8 + g, pieces c and 4 + c; values 2c, 2c + 1, 8 + 2c, 9 + 2c, piece g
+  const uint32_t k_lane[2] = {ring + key_at<HD>(g, c), HD == 128 ? ring + key_at<HD>(g, 4 + c) : 0u};
+  const uint32_t v_lane = ring + L::kTile + (HD == 128 ? value_at<HD>(2 * c, g) : value_at<HD>(2 * c, g >> 1) + (g & 1) * 8);
+  const uint32_t v_next = HD == 128 ? v_lane + 128 : ring + L::kTile + value_at<HD>(2 * c + 1, g >> 1) + (g & 1) * 8;
+
+  // scores of the rows whose weights are summed stay in shared memory, if those of all of the CTA's keys fit
+  const int score_ld = (((s1 - s0) * 16 + 23) / 32) * 32 + 8;             // 8 more than a multiple of 32 banks
 
   for (int tile = group * tiles_each; tile < min((group + 1) * tiles_each, (rows + L::kRows - 1) / L::kRows); ++tile) {
-    const int r0 = tile * L::kRows;
+    const int r0 = tile * L::kRows, summed = min(L::kRows, min(a.mass_rows, n) * share - r0);      // rows 0 .. summed - 1 of the tile
+    const bool keep_scores = summed > 0 && summed * score_ld * 4 <= score_bytes;
+    float* held = reinterpret_cast<float*>(smem + L::kScoreAt);
     // requests of the first slices travel while the queries are laid out
 #pragma unroll
     for (int d = 0; d < kDepth - 1; ++d) {
-      if (s0 + warp + d * kWarps < s1) request(s0 + warp + d * kWarps, d, true);
+      if (s0 + warp + d * kWarps < s1) request(s0 + warp + d * kWarps, d * L::kSlot, true);
       tc::cp_async_commit();
     }
 
@@ -205,6 +256,15 @@ __global__ void __launch_bounds__(kThreads) quant_attend_kernel(QAttendArgs a, i
       if (j >= n || t < 0) return false;
       return a.visible ? ((sees[mt][i] >> j) & 1u) != 0u : j <= t;
     };
+    uint32_t q_held[L::kQRegs ? MT * L::kSteps : 1][4];
+    if (L::kQRegs) {
+#pragma unroll
+      for (int i = 0; i < MT * L::kSteps; ++i) {
+        const uint4 t = lds128<0>(sbase + L::kQAt + i * 512 + lane * 16);
+        q_held[L::kQRegs ? i : 0][0] = t.x; q_held[L::kQRegs ? i : 0][1] = t.y;
+        q_held[L::kQRegs ? i : 0][2] = t.z; q_held[L::kQRegs ? i : 0][3] = t.w;
+      }
+    }
     // scores of a slice, unscaled; s[mt][nt]: keys 8 nt + 2c, + 1 of rows g, g + 8
     auto scores = [&](uint32_t slot, float (&s)[MT][2][4]) {
 #pragma unroll
@@ -215,9 +275,7 @@ __global__ void __launch_bounds__(kThreads) quant_attend_kernel(QAttendArgs a, i
           for (int e = 0; e < 4; ++e) s[mt][nt][e] = 0.f;
 #pragma unroll
       for (int h = 0; h < HD / 64; ++h) {
-        uint4 k4[2];
-#pragma unroll
-        for (int nt = 0; nt < 2; ++nt) k4[nt] = lds128(slot + key_at<HD>(8 * nt + g, 4 * h + c));
+        const uint4 k4[2] = {lds128<0>(k_lane[h] + slot), lds128<8 * HD>(k_lane[h] + slot)};
 #pragma unroll
         for (int st = 0; st < 4; ++st) {
           uint32_t b[2][2];
@@ -231,8 +289,14 @@ __global__ void __launch_bounds__(kThreads) quant_attend_kernel(QAttendArgs a, i
           for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
             for (int piece = L::kQ - 1; piece >= 0; --piece) {
-              const uint4 q4 = lds128(sbase + L::kQAt + ((piece * MT + mt) * L::kSteps + 4 * h + st) * 512 + lane * 16);
-              const uint32_t q[4] = {q4.x, q4.y, q4.z, q4.w};
+              uint32_t q[4];
+              if (L::kQRegs) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) q[e] = q_held[L::kQRegs ? mt * L::kSteps + 4 * h + st : 0][e];
+              } else {
+                const uint4 t = lds128<0>(sbase + L::kQAt + ((piece * MT + mt) * L::kSteps + 4 * h + st) * 512 + lane * 16);
+                q[0] = t.x; q[1] = t.y; q[2] = t.z; q[3] = t.w;
+              }
 #pragma unroll
               for (int nt = 0; nt < 2; ++nt) mma_f16(s[mt][nt], q, b[nt][0], b[nt][1]);
             }
@@ -251,42 +315,72 @@ __global__ void __launch_bounds__(kThreads) quant_attend_kernel(QAttendArgs a, i
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[mt][j][e] = 0.f;
     }
-    int at = 0;
-    for (int slice = s0 + warp; slice < s1; slice += kWarps) {
-      tc::cp_async_wait<kDepth - 2>();
-      __syncwarp();
-      const uint32_t slot = ring + at * L::kSlot;
-      const float ks = lds32(slot + 2 * L::kTile), vs = lds32(slot + 2 * L::kTile + 4);
-      float s[MT][2][4];
-      scores(slot, s);
-      const float lv = __log2f(vs), inv_vs = 1.f / vs;
+    // the weights of a slice's scores, in place of them; MASKED: some row does not see some key
+    auto weights = [&](auto masked, int slice, float ks, float lv, float inv_vs, float (&s)[MT][2][4], uint32_t (&p)[L::kP][MT][4]) {
+      constexpr bool MASKED = decltype(masked)::value;
       const int slot0 = slice << 4;
-      const bool whole = slot0 >= first && slot0 + 16 <= len;
-      uint32_t p[L::kP][MT][4];
-      bool same = true;
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
-        float alpha[2];
+        if (keep_scores) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            if (mt * 16 + g + 8 * i >= summed) continue;
+            const float f = fac[mt][i] * ks;
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt) {
+              float x[2] = {s[mt][nt][2 * i] * f, s[mt][nt][2 * i + 1] * f};
+              if (MASKED) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                  if (!visible(mt, i, slot0 + 8 * nt + 2 * c + e)) x[e] = -CUDART_INF_F;
+              }
+              *reinterpret_cast<float2*>(held + (mt * 16 + g + 8 * i) * score_ld + (slice - s0) * 16 + 8 * nt + 2 * c) = make_float2(x[0], x[1]);
+            }
+          }
+        }
+        // log2 of the weights at the row's reference; a row that sees nothing yet has none
+        bool passes = false;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const float f = fac[mt][i] * ks;
-          float v[4];
+          const float f = fac[mt][i] * ks, by = lv + kShift - (m[mt][i] == -CUDART_INF_F ? 0.f : m[mt][i]);
+          float top = -CUDART_INF_F;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            v[e] = fmaf(s[mt][e >> 1][2 * i + (e & 1)], f, lv);
-            if (!whole && !visible(mt, i, slot0 + 8 * (e >> 1) + 2 * c + (e & 1))) v[e] = -CUDART_INF_F;
+            float& v = s[mt][e >> 1][2 * i + (e & 1)];
+            v = fmaf(v, f, by);
+            if (MASKED && !visible(mt, i, slot0 + 8 * (e >> 1) + 2 * c + (e & 1))) v = -CUDART_INF_F;
+            top = fmaxf(top, v);
           }
-          float mx = fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]));
-          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-          const float m_new = fmaxf(m[mt][i], mx), m_safe = m_new == -CUDART_INF_F ? 0.f : m_new - kShift;
-          alpha[i] = ex2(m[mt][i] - m_new);
-          if (m_new == -CUDART_INF_F) alpha[i] = 1.f;
-          same = same && m_new == m[mt][i];
-          m[mt][i] = m_new;
+          passes = passes || top > kShift + kSlack || (m[mt][i] == -CUDART_INF_F && top > -CUDART_INF_F);
+        }
+        if (__any_sync(0xffffffffu, passes)) {               // some row's reference moves up to the slice's largest score
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = ex2(v[e] - m_safe);
-          l[mt][i] = fmaf(l[mt][i], alpha[i], ((v[0] + v[1]) + (v[2] + v[3])) * inv_vs);
+          for (int i = 0; i < 2; ++i) {
+            float top = fmaxf(fmaxf(s[mt][0][2 * i], s[mt][0][2 * i + 1]), fmaxf(s[mt][1][2 * i], s[mt][1][2 * i + 1]));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            const bool none = m[mt][i] == -CUDART_INF_F;
+            const float up = none ? top - kShift : fmaxf(top - kShift, 0.f);       // what the reference rises by (from 0 where there was none)
+            if (up == -CUDART_INF_F) continue;
+            const float alpha = none ? 0.f : ex2(-up);
+            m[mt][i] = none ? up : m[mt][i] + up;
+            l[mt][i] *= alpha;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[mt][e >> 1][2 * i + (e & 1)] -= up;
+#pragma unroll
+            for (int j = 0; j < HD / 8; ++j) {
+              o[mt][j][2 * i] *= alpha;
+              o[mt][j][2 * i + 1] *= alpha;
+            }
+          }
+          __syncwarp();
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          float v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = ex2(s[mt][e >> 1][2 * i + (e & 1)]);
+          l[mt][i] = fmaf((v[0] + v[1]) + (v[2] + v[3]), inv_vs, l[mt][i]);
 #pragma unroll
           for (int nt = 0; nt < 2; ++nt) {
             p[0][mt][i + 2 * nt] = pack_f16(v[2 * nt], v[2 * nt + 1]);
@@ -296,25 +390,33 @@ __global__ void __launch_bounds__(kThreads) quant_attend_kernel(QAttendArgs a, i
             }
           }
         }
-        if (!__all_sync(0xffffffffu, same)) {
-#pragma unroll
-          for (int j = 0; j < HD / 8; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[mt][j][e] *= alpha[e >> 1];
-        }
       }
+    };
+    uint32_t at = 0, ahead = (kDepth - 1) * L::kSlot;
+    for (int slice = s0 + warp; slice < s1; slice += kWarps) {
+      tc::cp_async_wait<kDepth - 2>();
+      __syncwarp();
+      const float ks = lds32<2 * L::kTile>(ring + at), vs = lds32<2 * L::kTile + 4>(ring + at);
+      float s[MT][2][4];
+      scores(at, s);
+      const float lv = __log2f(vs), inv_vs = __frcp_rn(vs);
+      uint32_t p[L::kP][MT][4];
+      if ((slice << 4) >= first && (slice << 4) + 16 <= len)
+        weights(std::false_type{}, slice, ks, lv, inv_vs, s, p);
+      else
+        weights(std::true_type{}, slice, ks, lv, inv_vs, s, p);
       // values: this lane's keys are 2c, 2c + 1, 8 + 2c, 9 + 2c, its columns g * HD / 8 ..
       uint32_t w[4][HD / 32];
+      if (HD == 128) {
+        const uint4 t[4] = {lds128<0>(v_lane + at), lds128<0>(v_next + at), lds128<8 * HD>(v_lane + at), lds128<8 * HD>(v_next + at)};
 #pragma unroll
-      for (int kk = 0; kk < 4; ++kk) {
-        const int row = (kk >> 1) * 8 + 2 * c + (kk & 1);
-        if (HD == 128) {
-          const uint4 t = lds128(slot + L::kTile + value_at<HD>(row, g));
-          w[kk][0] = t.x; w[kk][1] = t.y; w[kk][HD / 32 - 2] = t.z; w[kk][HD / 32 - 1] = t.w;
-        } else {
-          const uint2 t = lds64(slot + L::kTile + value_at<HD>(row, g >> 1) + (g & 1) * 8);
-          w[kk][0] = t.x; w[kk][1] = t.y;
+        for (int kk = 0; kk < 4; ++kk) {
+          w[kk][0] = t[kk].x; w[kk][1] = t[kk].y; w[kk][HD / 32 - 2] = t[kk].z; w[kk][HD / 32 - 1] = t[kk].w;
         }
+      } else {
+        const uint2 t[4] = {lds64<0>(v_lane + at), lds64<0>(v_next + at), lds64<8 * HD>(v_lane + at), lds64<8 * HD>(v_next + at)};
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) { w[kk][0] = t[kk].x; w[kk][1] = t[kk].y; }
       }
 #pragma unroll
       for (int wi = 0; wi < HD / 32; ++wi) {
@@ -335,9 +437,10 @@ __global__ void __launch_bounds__(kThreads) quant_attend_kernel(QAttendArgs a, i
             for (int piece = L::kP - 1; piece >= 0; --piece) mma_f16(o[mt][4 * wi + j], p[piece][mt], b[0][j], b[1][j]);
       }
       __syncwarp();
-      if (slice + (kDepth - 1) * kWarps < s1) request(slice + (kDepth - 1) * kWarps, (at + kDepth - 1) % kDepth, true);
+      if (slice + (kDepth - 1) * kWarps < s1) request(slice + (kDepth - 1) * kWarps, ahead, true);
       tc::cp_async_commit();
-      at = (at + 1) % kDepth;
+      ahead = at;
+      at = at == (kDepth - 1) * L::kSlot ? 0u : at + L::kSlot;
     }
     tc::cp_async_wait<0>();
     __syncwarp();
@@ -430,6 +533,20 @@ __global__ void __launch_bounds__(kThreads) quant_attend_kernel(QAttendArgs a, i
       if (begin && a.mass_decay != 1.f)
         for (int slot = rank * kThreads + tid; slot < all0 * 16 && slot < end; slot += ranks * kThreads)
           mass[slot] = a.mass_decay == 0.f ? 0.f : a.mass_decay * mass[slot];
+      const float decay = begin ? a.mass_decay : 1.f;
+      if (keep_scores || summed <= 0) {
+        for (int key = tid; (begin || summed > 0) && key < (s1 - s0) * 16 && s0 * 16 + key < end; key += kThreads) {
+          float sum = 0.f;
+          for (int r = 0; r < summed; ++r) {
+            const float w = ex2(held[r * score_ld + key] - lse2[r]);
+            sum += lse2[r] == CUDART_INF_F ? 0.f : w;
+          }
+          float* at = mass + s0 * 16 + key;
+          *at = decay == 0.f ? sum : fmaf(decay, *at, sum);
+        }
+        __syncthreads();
+        continue;
+      }
       float sub[MT][2];
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt)
@@ -437,20 +554,25 @@ __global__ void __launch_bounds__(kThreads) quant_attend_kernel(QAttendArgs a, i
         for (int i = 0; i < 2; ++i) sub[mt][i] = t_of[mt][i] >= 0 && t_of[mt][i] < a.mass_rows ? lse2[mt * 16 + g + 8 * i] : CUDART_INF_F;
 #pragma unroll
       for (int d = 0; d < kDepth - 1; ++d) {
-        if (s0 + warp + d * kWarps < s1) request(s0 + warp + d * kWarps, d, false);
+        if (s0 + warp + d * kWarps < s1) request(s0 + warp + d * kWarps, d * L::kSlot, false);
         tc::cp_async_commit();
       }
       at = 0;
+      ahead = (kDepth - 1) * L::kSlot;
       for (int slice = s0 + warp; slice < s1; slice += kWarps) {
         tc::cp_async_wait<kDepth - 2>();
         __syncwarp();
-        const uint32_t slot = ring + at * L::kSlot;
-        const float ks = lds32(slot + 2 * L::kTile);
+        const float ks = lds32<2 * L::kTile>(ring + at);
         float s[MT][2][4];
-        scores(slot, s);
+        scores(at, s);
         const int slot0 = slice << 4;
         const bool whole = slot0 >= first && slot0 + 16 <= len;
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        float sum[4] = {0.f, 0.f, 0.f, 0.f}, was[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int key = slot0 + 8 * (e >> 1) + 2 * c + (e & 1);
+          was[e] = lane < 4 && key < end && decay != 0.f ? mass[key] : 0.f;
+        }
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -472,15 +594,14 @@ __global__ void __launch_bounds__(kThreads) quant_attend_kernel(QAttendArgs a, i
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int key = slot0 + 8 * (e >> 1) + 2 * c + (e & 1);
-            if (key >= end) continue;
-            const float decay = begin ? a.mass_decay : 1.f;
-            mass[key] = decay == 0.f ? sum[e] : fmaf(decay, mass[key], sum[e]);
+            if (key < end) mass[key] = decay == 0.f ? sum[e] : fmaf(decay, was[e], sum[e]);
           }
         }
         __syncwarp();
-        if (slice + (kDepth - 1) * kWarps < s1) request(slice + (kDepth - 1) * kWarps, (at + kDepth - 1) % kDepth, false);
+        if (slice + (kDepth - 1) * kWarps < s1) request(slice + (kDepth - 1) * kWarps, ahead, false);
         tc::cp_async_commit();
-        at = (at + 1) % kDepth;
+        ahead = at;
+        at = at == (kDepth - 1) * L::kSlot ? 0u : at + L::kSlot;
       }
       tc::cp_async_wait<0>();
       __syncthreads();
@@ -498,13 +619,24 @@ int launch_tiles(const QAttendArgs& a, cudaStream_t s) {
   const int slices = ((a.max_len > 0 && a.max_len < a.c.cap ? a.max_len : a.c.cap) + 15) / 16;
   int ranks = 1;
   while (ranks < 16 && items * ranks * 2 <= 2LL * a.n_sms && slices >= 2 * ranks * kWarps) ranks *= 2;
+  // shared memory for the scores of summed rows: what a CTA's keys need, if that is little enough with some number of ranks
+  const int mass_rows = a.mass_rows < a.n_rows ? a.mass_rows : a.n_rows;
+  const int summed = mass_rows * (a.n_heads / a.c.n_heads) < L::kRows ? mass_rows * (a.n_heads / a.c.n_heads) : L::kRows;
+  auto scores_of = [&](int r) { return summed * ((((slices + r - 1) / r * 16 + 23) / 32) * 32 + 8) * 4; };
+  int more = ranks;
+  while (more < 16 && scores_of(more) > kScoreBytes) more *= 2;
+  int score_bytes = 0;
+  if (summed > 0 && scores_of(more) <= kScoreBytes) {
+    ranks = more;
+    score_bytes = scores_of(ranks);
+  }
   auto kernel = quant_attend_kernel<T, HD, MT>;
-  if (ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), L::kBytes) != cudaSuccess) return VVS_ERR_CUDA;
+  if (ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), L::kBytes + kScoreBytes) != cudaSuccess) return VVS_ERR_CUDA;
   if (ranks > 8 && cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return VVS_ERR_CUDA;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(ranks, a.c.n_heads * groups, a.c.n_seqs);
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = L::kBytes;
+  cfg.dynamicSmemBytes = L::kBytes + score_bytes;
   cfg.stream = s;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -514,7 +646,7 @@ int launch_tiles(const QAttendArgs& a, cudaStream_t s) {
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, kernel, a, tiles_each) == cudaSuccess ? VVS_OK : VVS_ERR_CUDA;
+  return cudaLaunchKernelEx(&cfg, kernel, a, tiles_each, score_bytes) == cudaSuccess ? VVS_OK : VVS_ERR_CUDA;
 }
 
 template <typename T, int HD>
