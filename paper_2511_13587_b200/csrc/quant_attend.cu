@@ -30,7 +30,7 @@ constexpr int kThreads = 32 * kWarps;
 // halves keep 11 bits down to 2^-21 of the reference's.  After a row's first slices its sums are hardly ever scaled again, and no lane
 // has to ask the others for their largest score.
 constexpr float kShift = 7.f, kSlack = 8.f;
-constexpr int kScoreBytes = 20 * 1024;          // of a CTA's shared memory for scores of rows whose weights are summed
+constexpr int kScoreBytes = 40 * 1024;          // of a CTA's shared memory for scores of rows whose weights are summed
 constexpr float kLog2e = 1.4426950408889634f;
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t* a, uint32_t b0, uint32_t b1) {
@@ -535,14 +535,26 @@ __global__ void __launch_bounds__(kThreads, Layout<HD, MT, sizeof(T) == 4>::kCta
           mass[slot] = a.mass_decay == 0.f ? 0.f : a.mass_decay * mass[slot];
       const float decay = begin ? a.mass_decay : 1.f;
       if (keep_scores || summed <= 0) {
-        for (int key = tid; (begin || summed > 0) && key < (s1 - s0) * 16 && s0 * 16 + key < end; key += kThreads) {
-          float sum = 0.f;
-          for (int r = 0; r < summed; ++r) {
-            const float w = ex2(held[r * score_ld + key] - lse2[r]);
-            sum += lse2[r] == CUDART_INF_F ? 0.f : w;
+        const int n_keys = begin || summed > 0 ? min((s1 - s0) * 16, end - s0 * 16) : 0;
+        constexpr int kTogether = 8;                                      // keys of a thread whose weights so far travel together
+        for (int key0 = tid; key0 < n_keys; key0 += kTogether * kThreads) {
+          float was[kTogether], sum[kTogether];
+#pragma unroll
+          for (int j = 0; j < kTogether; ++j) {
+            const int key = key0 + j * kThreads;
+            was[j] = decay != 0.f && key < n_keys ? mass[s0 * 16 + key] : 0.f;
+            sum[j] = 0.f;
           }
-          float* at = mass + s0 * 16 + key;
-          *at = decay == 0.f ? sum : fmaf(decay, *at, sum);
+          for (int r = 0; r < summed; ++r) {
+            const float by = lse2[r];
+            if (by == CUDART_INF_F) continue;
+#pragma unroll
+            for (int j = 0; j < kTogether; ++j)
+              if (key0 + j * kThreads < n_keys) sum[j] += ex2(held[r * score_ld + key0 + j * kThreads] - by);
+          }
+#pragma unroll
+          for (int j = 0; j < kTogether; ++j)
+            if (key0 + j * kThreads < n_keys) mass[s0 * 16 + key0 + j * kThreads] = decay == 0.f ? sum[j] : fmaf(decay, was[j], sum[j]);
         }
         __syncthreads();
         continue;
@@ -619,17 +631,13 @@ int launch_tiles(const QAttendArgs& a, cudaStream_t s) {
   const int slices = ((a.max_len > 0 && a.max_len < a.c.cap ? a.max_len : a.c.cap) + 15) / 16;
   int ranks = 1;
   while (ranks < 16 && items * ranks * 2 <= 2LL * a.n_sms && slices >= 2 * ranks * kWarps) ranks *= 2;
-  // shared memory for the scores of summed rows: what a CTA's keys need, if that is little enough with some number of ranks
-  const int mass_rows = a.mass_rows < a.n_rows ? a.mass_rows : a.n_rows;
-  const int summed = mass_rows * (a.n_heads / a.c.n_heads) < L::kRows ? mass_rows * (a.n_heads / a.c.n_heads) : L::kRows;
-  auto scores_of = [&](int r) { return summed * ((((slices + r - 1) / r * 16 + 23) / 32) * 32 + 8) * 4; };
-  int more = ranks;
-  while (more < 16 && scores_of(more) > kScoreBytes) more *= 2;
-  int score_bytes = 0;
-  if (summed > 0 && scores_of(more) <= kScoreBytes) {
-    ranks = more;
-    score_bytes = scores_of(ranks);
-  }
+  // shared memory for the scores of summed rows, where all of a CTA's keys fit (a call that says less of its lengths than they are walks
+  // the keys again).  More ranks than the device has room for, to make them fit, cost more than the second walk: 32 sequences of nine
+  // rows behind 900 to 2380 keys 179 us so, 347 with sixteen ranks in the place of one.
+  const int mass_rows = a.mass_rows < a.n_rows ? a.mass_rows : a.n_rows, share = a.n_heads / a.c.n_heads;
+  const long long summed = (long long)mass_rows * share < L::kRows ? mass_rows * share : L::kRows;
+  const long long want = summed * ((((slices + ranks - 1) / ranks * 16 + 23) / 32) * 32 + 8) * 4;
+  const int score_bytes = want <= kScoreBytes ? (int)want : 0;
   auto kernel = quant_attend_kernel<T, HD, MT>;
   if (ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), L::kBytes + kScoreBytes) != cudaSuccess) return VVS_ERR_CUDA;
   if (ranks > 8 && cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return VVS_ERR_CUDA;
