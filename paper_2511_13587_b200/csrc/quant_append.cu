@@ -25,39 +25,43 @@ __device__ __forceinline__ void put_rows(const QAppendArgs& a, const HeadRows& s
   const T* base = static_cast<const T*>(src.data) + seq * src.seq + head * src.head;
   float* scale = scales + ((size_t)seq * a.c.n_heads + head) * (a.c.cap >> a.c.block_log2) + block;
   const float old = live > 0 ? *scale : 0.f;
-  float x[PASSES][8];
-#pragma unroll
-  for (int p = 0; p < PASSES; ++p) {
-    const int t = t0 + p * kRows + r;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[p][e] = 0.f;
-    if (t < t1) {
-      const int from = a.row_index ? a.row_index[(size_t)seq * a.n_rows + t] : t;
-      if (from >= 0 && from < a.n_rows) load_unit(base + from * src.row, u, split, n_pairs, x[p]);
-      else atomicOr(a.status, VVS_DEV_BAD_ARG);
-    }
-  }
-  float amax = 0.f;
+  // the rows as they are stored; they are turned twice, for the maximum and for the codes, which takes fewer registers than one turned
+  // copy (bf16: half, and 80 of a thread in the place of 213)
+  Unit<T> raw[PASSES];
 #pragma unroll
   for (int p = 0; p < PASSES; ++p) {
     const int t = t0 + p * kRows + r;
     if (t >= t1) continue;
-    if (turned && (split || !a.rope.halves)) {
-      const float2* cs = table + (size_t)(t - t0) * (HD / 2) + 4 * u;
+    const int from = a.row_index ? a.row_index[(size_t)seq * a.n_rows + t] : t;
+    if (from >= 0 && from < a.n_rows) {
+      raw[p] = load_unit_raw(base + from * src.row, u, split, n_pairs);
+    } else {
+      raw[p] = Unit<T>{};
+      atomicOr(a.status, VVS_DEV_BAD_ARG);
+    }
+  }
+  const bool mine = turned && (split || !a.rope.halves);
+  auto value = [&](int p, float (&x)[8]) {
+    widen_unit(raw[p], x);
+    if (mine) {
+      const float2* cs = table + (size_t)(p * kRows + r) * (HD / 2) + 4 * u;
       float c[4], s[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) { c[j] = cs[j].x; s[j] = cs[j].y; }
-      turn_unit(x[p], split, c, s);
+      turn_unit(x, split, c, s);
     }
+  };
+  float amax = 0.f;
+#pragma unroll
+  for (int p = 0; p < PASSES; ++p) {
+    if (t0 + p * kRows + r >= t1) continue;
+    float x[8];
+    value(p, x);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float m = fabsf(x[p][e]);
-      if (m < CUDART_INF_F) {
-        amax = fmaxf(amax, m);
-      } else {                                 // an infinity becomes the largest code, a NaN zero
-        odd = true;
-        if (m != m) x[p][e] = 0.f;
-      }
+      const float m = fabsf(x[e]);
+      if (m < CUDART_INF_F) amax = fmaxf(amax, m);
+      else odd = true;                         // an infinity becomes the largest code, a NaN zero
     }
   }
 #pragma unroll
@@ -74,8 +78,11 @@ __device__ __forceinline__ void put_rows(const QAppendArgs& a, const HeadRows& s
     const int t = t0 + p * kRows + r;
     if (t >= t1) continue;
     uint8_t* at = rows + (size_t)(live + t - t0) * HD;
-    const uint32_t lo = to_e4m3x4(x[p][0] * inv, x[p][1] * inv, x[p][2] * inv, x[p][3] * inv);
-    const uint32_t hi = to_e4m3x4(x[p][4] * inv, x[p][5] * inv, x[p][6] * inv, x[p][7] * inv);
+    float x[8];
+    value(p, x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = x[e] == x[e] ? x[e] * inv : 0.f;
+    const uint32_t lo = to_e4m3x4(x[0], x[1], x[2], x[3]), hi = to_e4m3x4(x[4], x[5], x[6], x[7]);
     if (split) {
       *reinterpret_cast<uint32_t*>(at + 4 * u) = lo;
       *reinterpret_cast<uint32_t*>(at + n_pairs + 4 * u) = hi;
@@ -145,22 +152,25 @@ __global__ void __launch_bounds__(kThreads) quant_append_kernel(QAppendArgs a, i
       constexpr int kUnits = HD / 8, kRows = kPassRows<HD>;
       const int u = tid % kUnits, r = tid / kUnits;
       const bool split = turned && unit_split(a.rope, u);
-      float x[PASSES][8];
+      const bool mine = turned && (split || !a.rope.halves);
+      Unit<T> raw[PASSES];
 #pragma unroll
       for (int p = 0; p < PASSES; ++p)
-        if (t0 + p * kRows + r < t1) load_unit(from + (t0 + p * kRows + r) * a.q.row, u, split, a.rope.n_pairs, x[p]);
+        if (t0 + p * kRows + r < t1) raw[p] = load_unit_raw(from + (t0 + p * kRows + r) * a.q.row, u, split, a.rope.n_pairs);
 #pragma unroll
       for (int p = 0; p < PASSES; ++p) {
         const int t = t0 + p * kRows + r;
         if (t >= t1) continue;
-        if (turned && (split || !a.rope.halves)) {
+        float x[8];
+        widen_unit(raw[p], x);
+        if (mine) {
           const float2* cs = table + (size_t)(t - t0) * (HD / 2) + 4 * u;
           float c[4], s[4];
 #pragma unroll
           for (int j = 0; j < 4; ++j) { c[j] = cs[j].x; s[j] = cs[j].y; }
-          turn_unit(x[p], split, c, s);
+          turn_unit(x, split, c, s);
         }
-        store_unit(to + t * a.q_out.row, u, split, a.rope.n_pairs, x[p]);
+        store_unit(to + t * a.q_out.row, u, split, a.rope.n_pairs, x);
       }
     }
   }
@@ -172,8 +182,9 @@ int launch_passes(const QAppendArgs& a, cudaStream_t s) {
   const int blk = 1 << a.c.block_log2, rows = a.n_rows < blk ? a.n_rows : blk;
   const int chunks = (a.n_rows + blk - 2) / blk + 1, items = 2 * a.c.n_heads + a.n_heads;
   const size_t smem = a.rope.inv_freq ? (size_t)rows * (HD / 2) * sizeof(float2) : 0;
-  // as many groups of heads as keep every SM busy with eight CTAs; beyond that a CTA's sines serve several heads
-  const long long room = 8LL * a.n_sms, each_head = (long long)chunks * a.c.n_seqs;
+  // as many groups of heads as keep every SM busy with eight CTAs (four of long blocks, whose sines cost more than their elements'
+  // traffic unless they serve several heads)
+  const long long room = (rows > 32 ? 4LL : 8LL) * a.n_sms, each_head = (long long)chunks * a.c.n_seqs;
   long long groups = (room + each_head - 1) / each_head;
   groups = groups > items ? items : groups;
   const int each = (int)((items + groups - 1) / groups);

@@ -78,28 +78,6 @@ struct QEvictArgs {
 int launch_quant_evict(const QEvictArgs& a, cudaStream_t s);
 
 // ---- eight values of a row, 16 bytes of bf16 or 32 of float32; or two groups of four -----------------------------------
-__device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&x)[8]) {
-  const uint4 t = *reinterpret_cast<const uint4*>(p);
-  const uint32_t w[4] = {t.x, t.y, t.z, t.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = __uint_as_float(w[i] << 16);
-    x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-  }
-}
-__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
-  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-  x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-}
-__device__ __forceinline__ void load4(const __nv_bfloat16* p, float* x) {
-  const uint2 t = *reinterpret_cast<const uint2*>(p);
-  x[0] = __uint_as_float(t.x << 16); x[1] = __uint_as_float(t.x & 0xffff0000u);
-  x[2] = __uint_as_float(t.y << 16); x[3] = __uint_as_float(t.y & 0xffff0000u);
-}
-__device__ __forceinline__ void load4(const float* p, float* x) {
-  const float4 a = *reinterpret_cast<const float4*>(p);
-  x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-}
 __device__ __forceinline__ uint32_t pack_bf16x2(float a, float b) {
   const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&h);
@@ -149,14 +127,36 @@ __device__ __forceinline__ void turn_unit(float (&x)[8], bool split, const float
     for (int i = 0; i < 4; ++i) turn(x[2 * i], x[2 * i + 1], c[i], s[i]);
   }
 }
+// as they are stored
 template <typename T>
-__device__ __forceinline__ void load_unit(const T* row, int u, bool split, int n_pairs, float (&x)[8]) {
-  if (split) {
-    load4(row + 4 * u, x);
-    load4(row + n_pairs + 4 * u, x + 4);
-  } else {
-    load8(row + 8 * u, x);
+struct Unit;
+template <>
+struct Unit<__nv_bfloat16> {
+  uint2 a, b;
+};
+template <>
+struct Unit<float> {
+  float4 a, b;
+};
+__device__ __forceinline__ Unit<__nv_bfloat16> load_unit_raw(const __nv_bfloat16* row, int u, bool split, int n_pairs) {
+  if (split) return {*reinterpret_cast<const uint2*>(row + 4 * u), *reinterpret_cast<const uint2*>(row + n_pairs + 4 * u)};
+  const uint4 t = *reinterpret_cast<const uint4*>(row + 8 * u);
+  return {make_uint2(t.x, t.y), make_uint2(t.z, t.w)};
+}
+__device__ __forceinline__ Unit<float> load_unit_raw(const float* row, int u, bool split, int n_pairs) {
+  const float* p = row + (split ? 4 : 8) * u;
+  return {*reinterpret_cast<const float4*>(p), *reinterpret_cast<const float4*>(split ? row + n_pairs + 4 * u : p + 4)};
+}
+__device__ __forceinline__ void widen_unit(const Unit<__nv_bfloat16>& r, float (&x)[8]) {
+  const uint32_t w[4] = {r.a.x, r.a.y, r.b.x, r.b.y};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(w[i] << 16);
+    x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
   }
+}
+__device__ __forceinline__ void widen_unit(const Unit<float>& r, float (&x)[8]) {
+  x[0] = r.a.x; x[1] = r.a.y; x[2] = r.a.z; x[3] = r.a.w; x[4] = r.b.x; x[5] = r.b.y; x[6] = r.b.z; x[7] = r.b.w;
 }
 template <typename T>
 __device__ __forceinline__ void store_unit(T* row, int u, bool split, int n_pairs, const float (&x)[8]) {

@@ -9,7 +9,7 @@ namespace vvs {
 namespace {
 
 constexpr int kThreads = 128;
-constexpr int kFlight = 4;   // heads whose loads are in flight together
+constexpr int kFlight = 4;   // heads whose elements are on their way together
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads) rotate_axes_kernel(RotateArgs a, int heads_each) {
@@ -20,33 +20,34 @@ __global__ void __launch_bounds__(kThreads) rotate_axes_kernel(RotateArgs a, int
   if (i >= (long long)a.n_seqs * a.n_rows * units) return;
   const int u = (int)(i % units);
   const int at = (int)(i / units), row = at % a.n_rows, seq = at / a.n_rows;
-  float c[4], s[4];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) pair_turn(a.rope, 4 * u + j, seq, row, a.n_seqs, a.n_rows, a.status, c[j], s[j]);
   const bool split = unit_split(a.rope, u);
-  if (a.rope.halves && !split) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) { c[j] = 1.f; s[j] = 0.f; }
-  }
   const int heads = a.n_heads + a.n_kv_heads, h0 = blockIdx.y * heads_each, h1 = min(heads, h0 + heads_each);
   const T* q = static_cast<const T*>(a.q.data) + seq * a.q.seq + row * a.q.row;
   const T* k = static_cast<const T*>(a.k.data) + seq * a.k.seq + row * a.k.row;
   T* qo = static_cast<T*>(a.q_out.data) + seq * a.q_out.seq + row * a.q_out.row;
   T* ko = static_cast<T*>(a.k_out.data) + seq * a.k_out.seq + row * a.k_out.row;
+  auto request = [&](int h, Unit<T> (&x)[kFlight]) {
+#pragma unroll
+    for (int j = 0; j < kFlight; ++j)
+      if (h + j < h1) x[j] = load_unit_raw(h + j < a.n_heads ? q + (h + j) * a.q.head : k + (h + j - a.n_heads) * a.k.head, u, split, a.rope.n_pairs);
+  };
+  // the first heads travel beside the angles, the next ones beside the turning
+  Unit<T> x[kFlight];
+  request(h0, x);
+  float c[4], s[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) pair_turn(a.rope, 4 * u + j, seq, row, a.n_seqs, a.n_rows, a.status, c[j], s[j]);
   for (int h = h0; h < h1; h += kFlight) {
-    float x[kFlight][8];
+    Unit<T> next[kFlight];
+    request(h + kFlight, next);
 #pragma unroll
     for (int j = 0; j < kFlight; ++j) {
-      const int hh = h + j;
-      if (hh >= h1) break;
-      load_unit(hh < a.n_heads ? q + hh * a.q.head : k + (hh - a.n_heads) * a.k.head, u, split, a.rope.n_pairs, x[j]);
-    }
-#pragma unroll
-    for (int j = 0; j < kFlight; ++j) {
-      const int hh = h + j;
-      if (hh >= h1) break;
-      turn_unit(x[j], split, c, s);
-      store_unit(hh < a.n_heads ? qo + hh * a.q_out.head : ko + (hh - a.n_heads) * a.k_out.head, u, split, a.rope.n_pairs, x[j]);
+      if (h + j >= h1) break;
+      float v[8];
+      widen_unit(x[j], v);
+      turn_unit(v, split, c, s);
+      store_unit(h + j < a.n_heads ? qo + (h + j) * a.q_out.head : ko + (h + j - a.n_heads) * a.k_out.head, u, split, a.rope.n_pairs, v);
+      x[j] = next[j];
     }
   }
 }
