@@ -1,8 +1,10 @@
 // Appends a block's keys and values to the 8-bit cache: rotation, one scale for each (block of slots, head), e4m3 codes; the query
-// heads of the same rows are rotated in the same launch.  Every input is read once and every output written once: bound by HBM for
-// prompts, by the launch and one round trip for a step's rows.  A CTA has the rows that fall into one block of slots, and some of the
-// heads: a head's rows stay in registers between the maximum that fixes the scale and the rounding.  Cosines and sines of the CTA's rows
-// are computed once, into shared memory, for all of its heads.
+// heads of the same rows are rotated too.  Every input is read once and every output written once: bound by HBM for prompts, by the
+// launch and a few round trips for a step's rows.  A CTA has the rows that fall into one block of slots, and some of the heads;
+// cosines and sines of its rows are computed once, into shared memory.  A head's rows stay in registers, as they are stored, between
+// the maximum that fixes the scale and the rounding.
+// Few rows: a warp has a head, so that nothing but the table of sines is waited for by a whole CTA, and queries are heads like others.
+// Prompts: a CTA has a head.
 #include "quant_cache.cuh"
 
 namespace vvs {
@@ -12,51 +14,63 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 
-// rows of a pass: 32 of 64, 16 of 128 elements; a block has at most 128
-template <int HD>
-constexpr int kPassRows = kThreads / (HD / 8);
+// rows of a pass of a warp and of a CTA: 4 and 32 of 64 elements, 2 and 16 of 128
+template <int HD, bool WARP>
+constexpr int kPassRows = (WARP ? 32 : kThreads) / (HD / 8);
+constexpr int kFewPasses = 8;                  // of a warp: 32 rows of 64 elements, 16 of 128
 
-template <typename T, int HD, int PASSES>
-__device__ __forceinline__ void put_rows(const QAppendArgs& a, const HeadRows& src, bool turned, uint8_t* codes, float* scales, int seq, int head,
-                                         int block, int live, int t0, int t1, const float2* table, float* red, bool& odd) {
-  constexpr int kUnits = HD / 8, kRows = kPassRows<HD>;
-  const int tid = threadIdx.x, u = tid % kUnits, r = tid / kUnits, n_pairs = a.rope.n_pairs;
-  const bool split = turned && unit_split(a.rope, u);
-  const T* base = static_cast<const T*>(src.data) + seq * src.seq + head * src.head;
-  float* scale = scales + ((size_t)seq * a.c.n_heads + head) * (a.c.cap >> a.c.block_log2) + block;
-  const float old = live > 0 ? *scale : 0.f;
-  // the rows as they are stored; they are turned twice, for the maximum and for the codes, which takes fewer registers than one turned
-  // copy (bf16: half, and 80 of a thread in the place of 213)
-  Unit<T> raw[PASSES];
+// What a CTA works on: rows t0 .. t1 - 1 of the call, those of its k and v t0 .. tk - 1, behind `live` rows of the block of slots.
+struct Chunk {
+  int seq, block, live, t0, t1, tk;
+};
+
+// A thread's pieces of a head's rows, as they are stored; of keys and values the row index picks the rows.
+template <typename T, int HD, int PASSES, bool WARP>
+__device__ __forceinline__ void request_rows(const QAppendArgs& a, const HeadRows& src, const Chunk& ch, int head, int end, bool picked, bool split,
+                                             Unit<T> (&raw)[PASSES]) {
+  const int in = WARP ? threadIdx.x % 32 : threadIdx.x, u = in % (HD / 8), r = in / (HD / 8);
+  const T* base = static_cast<const T*>(src.data) + ch.seq * src.seq + head * src.head;
 #pragma unroll
   for (int p = 0; p < PASSES; ++p) {
-    const int t = t0 + p * kRows + r;
-    if (t >= t1) continue;
-    const int from = a.row_index ? a.row_index[(size_t)seq * a.n_rows + t] : t;
+    const int t = ch.t0 + p * kPassRows<HD, WARP> + r;
+    if (t >= end) continue;
+    const int from = picked ? a.row_index[(size_t)ch.seq * a.n_rows + t] : t;
     if (from >= 0 && from < a.n_rows) {
-      raw[p] = load_unit_raw(base + from * src.row, u, split, n_pairs);
+      raw[p] = load_unit_raw(base + from * src.row, u, split, a.rope.n_pairs);
     } else {
       raw[p] = Unit<T>{};
       atomicOr(a.status, VVS_DEV_BAD_ARG);
     }
   }
-  const bool mine = turned && (split || !a.rope.halves);
-  auto value = [&](int p, float (&x)[8]) {
-    widen_unit(raw[p], x);
-    if (mine) {
-      const float2* cs = table + (size_t)(p * kRows + r) * (HD / 2) + 4 * u;
-      float c[4], s[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) { c[j] = cs[j].x; s[j] = cs[j].y; }
-      turn_unit(x, split, c, s);
-    }
-  };
+}
+
+// A piece's values, turned by its row's angles.
+template <typename T, int HD>
+__device__ __forceinline__ void values_of(const Unit<T>& raw, bool mine, bool split, const float2* table, int row, float (&x)[8]) {
+  widen_unit(raw, x);
+  if (!mine) return;
+  const float4* cs = reinterpret_cast<const float4*>(table + (size_t)row * (HD / 2) + 4 * (threadIdx.x % (HD / 8)));
+  const float4 lo = cs[0], hi = cs[1];
+  const float c[4] = {lo.x, lo.z, hi.x, hi.z}, s[4] = {lo.y, lo.w, hi.y, hi.w};
+  turn_unit(x, split, c, s);
+}
+
+// A head's rows into the cache, by a warp or by the CTA.  They are turned twice, for the maximum and for the codes: that takes fewer registers
+// than one turned copy (bf16 rows of long blocks: 80 of a thread in the place of 213).
+template <typename T, int HD, int PASSES, bool WARP>
+__device__ __forceinline__ void put_rows(const QAppendArgs& a, const Unit<T> (&raw)[PASSES], bool turned, uint8_t* codes, float* scales, const Chunk& ch,
+                                         int head, const float2* table, float* red, bool& odd) {
+  constexpr int kUnits = HD / 8, kRows = kPassRows<HD, WARP>;
+  const int tid = WARP ? threadIdx.x % 32 : threadIdx.x, u = tid % kUnits, r = tid / kUnits, n_pairs = a.rope.n_pairs;
+  const bool split = turned && unit_split(a.rope, u), mine = turned && (split || !a.rope.halves);
+  float* scale = scales + ((size_t)ch.seq * a.c.n_heads + head) * (a.c.cap >> a.c.block_log2) + ch.block;
+  const float old = ch.live > 0 ? *scale : 0.f;
   float amax = 0.f;
 #pragma unroll
   for (int p = 0; p < PASSES; ++p) {
-    if (t0 + p * kRows + r >= t1) continue;
+    if (ch.t0 + p * kRows + r >= ch.tk) continue;
     float x[8];
-    value(p, x);
+    values_of<T, HD>(raw[p], mine, split, table, p * kRows + r, x);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const float m = fabsf(x[e]);
@@ -64,22 +78,25 @@ __device__ __forceinline__ void put_rows(const QAppendArgs& a, const HeadRows& s
       else odd = true;                         // an infinity becomes the largest code, a NaN zero
     }
   }
+  __syncwarp();
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-  if (tid % 32 == 0) red[tid / 32] = amax;
-  __syncthreads();
-  amax = red[0];
+  if (!WARP) {
+    if (tid % 32 == 0) red[tid / 32] = amax;
+    __syncthreads();
+    amax = red[0];
 #pragma unroll
-  for (int w = 1; w < kWarps; ++w) amax = fmaxf(amax, red[w]);
-  const float fresh = scale_of(amax), now = live > 0 ? fmaxf(old, fresh) : fresh, inv = 1.f / now;
-  uint8_t* rows = codes + (((size_t)seq * a.c.n_heads + head) * a.c.cap + ((size_t)block << a.c.block_log2)) * HD;
+    for (int w = 1; w < kWarps; ++w) amax = fmaxf(amax, red[w]);
+  }
+  const float fresh = scale_of(amax), now = ch.live > 0 ? fmaxf(old, fresh) : fresh, inv = 1.f / now;
+  uint8_t* rows = codes + (((size_t)ch.seq * a.c.n_heads + head) * a.c.cap + ((size_t)ch.block << a.c.block_log2)) * HD;
 #pragma unroll
   for (int p = 0; p < PASSES; ++p) {
-    const int t = t0 + p * kRows + r;
-    if (t >= t1) continue;
-    uint8_t* at = rows + (size_t)(live + t - t0) * HD;
+    const int t = ch.t0 + p * kRows + r;
+    if (t >= ch.tk) continue;
+    uint8_t* at = rows + (size_t)(ch.live + t - ch.t0) * HD;
     float x[8];
-    value(p, x);
+    values_of<T, HD>(raw[p], mine, split, table, p * kRows + r, x);
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = x[e] == x[e] ? x[e] * inv : 0.f;
     const uint32_t lo = to_e4m3x4(x[0], x[1], x[2], x[3]), hi = to_e4m3x4(x[4], x[5], x[6], x[7]);
@@ -90,116 +107,146 @@ __device__ __forceinline__ void put_rows(const QAppendArgs& a, const HeadRows& s
       *reinterpret_cast<uint2*>(at + 8 * u) = make_uint2(lo, hi);
     }
   }
-  if (live > 0 && now > old) {                 // the rows before these are rounded again
+  if (ch.live > 0 && now > old) {              // the rows before these are rounded again
     const float f = old / now;
     uint32_t* w = reinterpret_cast<uint32_t*>(rows);
-    for (int i = tid; i < live * (HD / 4); i += kThreads) w[i] = rescale_e4m3x4(w[i], f);
+    for (int i = tid; i < ch.live * (HD / 4); i += WARP ? 32 : kThreads) w[i] = rescale_e4m3x4(w[i], f);
   }
-  if (tid == 0) *scale = now;
+  __syncwarp();
+  if (tid == 0) *scale = now;                  // (every thread has read the old one: by a warp in step, or before the barrier)
 }
 
-template <typename T, int HD, int PASSES>
+// FEW: a chunk's rows fit a warp's passes.
+template <typename T, int HD, bool FEW>
 __global__ void __launch_bounds__(kThreads) quant_append_kernel(QAppendArgs a, int items_each) {
+  constexpr int PASSES = FEW ? kFewPasses : 128 / kPassRows<HD, false>;
   extern __shared__ __align__(16) uint8_t smem[];
   float2* table = reinterpret_cast<float2*>(smem);     // [rows of the chunk][HD / 2] cosine, sine
   __shared__ float red[2][kWarps];
   grid_dep_launch();
   grid_dep_wait();
-  const int seq = blockIdx.z, tid = threadIdx.x, blk = 1 << a.c.block_log2;
-  int base = a.cache_len[seq], n = a.row_count ? a.row_count[seq] : a.n_rows;
-  const int age0 = a.next_age ? a.next_age[seq] : base;
+  const int tid = threadIdx.x, blk = 1 << a.c.block_log2;
+  Chunk ch;
+  ch.seq = blockIdx.z;
+  int base = a.cache_len[ch.seq], n = a.row_count ? a.row_count[ch.seq] : a.n_rows;
+  const int age0 = a.next_age ? a.next_age[ch.seq] : base;
   uint32_t bits = 0;
   if (n < 0 || n > a.n_rows) { bits |= VVS_DEV_BAD_ARG; n = 0; }
   if (base < 0 || base > a.c.cap - n) { bits |= VVS_DEV_CACHE_OVERFLOW; base = 0; n = 0; }
   if (bits && blockIdx.x == 0 && blockIdx.y == 0 && tid == 0) atomicOr(a.status, bits);
-  // rows t0 .. t1 - 1 of the call: those whose slots lie in the blockIdx.x-th block that the call reaches
+  // the rows whose slots lie in the blockIdx.x-th block that the call reaches
   const int in_block = base & (blk - 1), chunk = blockIdx.x;
-  const int t0 = max(0, chunk * blk - in_block), t1 = min(a.n_rows, (chunk + 1) * blk - in_block);
-  if (t0 >= t1) return;
-  const int block = (base >> a.c.block_log2) + chunk, live = chunk == 0 ? in_block : 0, tk = min(t1, n);
-  const int kv = a.c.n_heads, i0 = blockIdx.y * items_each, i1 = min(2 * kv + a.n_heads, i0 + items_each);
-  // items: keys of every head, queries of every head, values of every head
-  const bool turned = a.rope.inv_freq != nullptr;
-  if (turned && i0 < kv + a.n_heads) {
-    for (int i = tid; i < (t1 - t0) * (HD / 2); i += kThreads) {
-      const int t = t0 + i / (HD / 2);
-      int from = t;
-      if (a.row_index && t < tk) from = min(max(a.row_index[(size_t)seq * a.n_rows + t], 0), a.n_rows - 1);
-      float c, s;
-      pair_turn(a.rope, i % (HD / 2), seq, from, a.c.n_seqs, a.n_rows, a.status, c, s);
-      table[i] = make_float2(c, s);
+  ch.t0 = max(0, chunk * blk - in_block);
+  ch.t1 = min(a.n_rows, (chunk + 1) * blk - in_block);
+  if (ch.t0 >= ch.t1) return;
+  ch.tk = min(ch.t1, n);
+  ch.block = (base >> a.c.block_log2) + chunk;
+  ch.live = chunk == 0 ? in_block : 0;
+  // items: keys of every head, queries of every head (few rows), values of every head
+  const int kv = a.c.n_heads, qs = FEW ? a.n_heads : 0, i0 = blockIdx.y * items_each, i1 = min(2 * kv + qs, i0 + items_each);
+  const int mine = FEW ? i0 + tid / 32 : i0, step = FEW ? kWarps : 1;
+  const bool rope = a.rope.inv_freq != nullptr;
+  const int u = tid % (HD / 8), r = (FEW ? tid % 32 : tid) / (HD / 8);
+  auto is_query = [&](int i) { return FEW && i >= kv && i < kv + qs; };
+  auto request = [&](int i, Unit<T> (&raw)[PASSES]) {
+    if (i >= i1) return;
+    const bool query = is_query(i), split = rope && i < kv + qs && unit_split(a.rope, u);
+    request_rows<T, HD, PASSES, FEW>(a, query ? a.q : i < kv ? a.k : a.v, ch, query ? i - kv : i < kv ? i : i - kv - qs, query ? ch.t1 : ch.tk,
+                                     !query && a.row_index, split, raw);
+  };
+  Unit<T> raw[PASSES];
+  request(mine, raw);                          // travels beside the table
+  if (rope && i0 < kv + qs) {
+    // a thread has one pair of every kStep-th row; the positions of several rows travel together
+    constexpr int kStep = kThreads / (HD / 2), kTogether = FEW ? 4 : 8;
+    const int pair = tid % (HD / 2), rows = ch.t1 - ch.t0;
+    const PairAxis pa = pair_axis(a.rope, pair, a.c.n_seqs, a.n_rows, a.status);
+    for (int t0 = tid / (HD / 2); t0 < rows; t0 += kTogether * kStep) {
+      int pos[kTogether];
+#pragma unroll
+      for (int j = 0; j < kTogether; ++j) {
+        const int t = ch.t0 + min(t0 + j * kStep, rows - 1);
+        int from = t;
+        if (a.row_index && t < ch.tk) from = min(max(a.row_index[(size_t)ch.seq * a.n_rows + t], 0), a.n_rows - 1);
+        pos[j] = pa.pos ? pa.pos[(size_t)ch.seq * a.n_rows + from] : 0;
+      }
+#pragma unroll
+      for (int j = 0; j < kTogether; ++j) {
+        const int t = t0 + j * kStep;
+        if (t >= rows) break;
+        float2 cs;
+        sincosf(__fmul_rn((float)pos[j], pa.freq), &cs.y, &cs.x);
+        table[t * (HD / 2) + pair] = cs;
+      }
     }
     __syncthreads();
   }
   bool odd = false;
-  int use = 0;                                 // the sums' room in turns: one barrier a head is enough
-  for (int i = i0; i < i1; ++i) {
-    if (i < kv || i >= kv + a.n_heads) {
-      if (t0 >= tk) continue;
-      const bool key = i < kv;
-      const int head = key ? i : i - kv - a.n_heads;
-      put_rows<T, HD, PASSES>(a, key ? a.k : a.v, key && turned, key ? a.c.k : a.c.v, key ? a.c.k_scale : a.c.v_scale, seq, head, block, live,
-                              t0, tk, table, red[use ^= 1], odd);
-      if (key && tid < tk - t0) {
-        const size_t slot = ((size_t)seq * kv + head) * a.c.cap + base + t0 + tid;
-        if (a.c.mass) a.c.mass[slot] = 0.f;
-        if (a.c.age) a.c.age[slot] = age0 + t0 + tid;
-      }
-    } else {
-      const int head = i - kv;
-      const T* from = static_cast<const T*>(a.q.data) + seq * a.q.seq + head * a.q.head;
-      T* to = static_cast<T*>(a.q_out.data) + seq * a.q_out.seq + head * a.q_out.head;
-      constexpr int kUnits = HD / 8, kRows = kPassRows<HD>;
-      const int u = tid % kUnits, r = tid / kUnits;
-      const bool split = turned && unit_split(a.rope, u);
-      const bool mine = turned && (split || !a.rope.halves);
-      Unit<T> raw[PASSES];
-#pragma unroll
-      for (int p = 0; p < PASSES; ++p)
-        if (t0 + p * kRows + r < t1) raw[p] = load_unit_raw(from + (t0 + p * kRows + r) * a.q.row, u, split, a.rope.n_pairs);
+  int use = 0;                                 // the maxima's room in turns: one barrier a head is enough
+  for (int i = mine; i < i1; i += step) {
+    if (is_query(i)) {
+      const bool split = rope && unit_split(a.rope, u);
 #pragma unroll
       for (int p = 0; p < PASSES; ++p) {
-        const int t = t0 + p * kRows + r;
-        if (t >= t1) continue;
+        const int in = p * kPassRows<HD, FEW> + r, t = ch.t0 + in;
+        if (t >= ch.t1) continue;
         float x[8];
-        widen_unit(raw[p], x);
-        if (mine) {
-          const float2* cs = table + (size_t)(t - t0) * (HD / 2) + 4 * u;
-          float c[4], s[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) { c[j] = cs[j].x; s[j] = cs[j].y; }
-          turn_unit(x, split, c, s);
-        }
-        store_unit(to + t * a.q_out.row, u, split, a.rope.n_pairs, x);
+        values_of<T, HD>(raw[p], rope && (split || !a.rope.halves), split, table, in, x);
+        store_unit(static_cast<T*>(a.q_out.data) + ch.seq * a.q_out.seq + (i - kv) * a.q_out.head + t * a.q_out.row, u, split, a.rope.n_pairs, x);
+      }
+    } else if (ch.t0 < ch.tk) {
+      const bool key = i < kv;
+      const int head = key ? i : i - kv - qs, at = FEW ? tid % 32 : tid;
+      put_rows<T, HD, PASSES, FEW>(a, raw, key && rope, key ? a.c.k : a.c.v, key ? a.c.k_scale : a.c.v_scale, ch, head, table, red[use ^= 1], odd);
+      if (key && at < ch.tk - ch.t0) {         // (few rows are at most 32)
+        const size_t slot = ((size_t)ch.seq * kv + head) * a.c.cap + base + ch.t0 + at;
+        if (a.c.mass) a.c.mass[slot] = 0.f;
+        if (a.c.age) a.c.age[slot] = age0 + ch.t0 + at;
       }
     }
+    __syncwarp();
+    request(i + step, raw);
   }
   if (odd) atomicOr(a.status, VVS_DEV_NONFINITE);
 }
 
-template <typename T, int HD, int PASSES>
-int launch_passes(const QAppendArgs& a, cudaStream_t s) {
+template <typename T, int HD, bool FEW>
+int launch_rows(const QAppendArgs& a, cudaStream_t s) {
   const int blk = 1 << a.c.block_log2, rows = a.n_rows < blk ? a.n_rows : blk;
-  const int chunks = (a.n_rows + blk - 2) / blk + 1, items = 2 * a.c.n_heads + a.n_heads;
+  const int chunks = (a.n_rows + blk - 2) / blk + 1, items = 2 * a.c.n_heads + (FEW ? a.n_heads : 0);
   const size_t smem = a.rope.inv_freq ? (size_t)rows * (HD / 2) * sizeof(float2) : 0;
-  // as many groups of heads as keep every SM busy with eight CTAs (four of long blocks, whose sines cost more than their elements'
-  // traffic unless they serve several heads)
-  const long long room = (rows > 32 ? 4LL : 8LL) * a.n_sms, each_head = (long long)chunks * a.c.n_seqs;
-  long long groups = (room + each_head - 1) / each_head;
-  groups = groups > items ? items : groups;
-  const int each = (int)((items + groups - 1) / groups);
-  auto kernel = quant_append_kernel<T, HD, PASSES>;
+  // Heads of a CTA: few rows, one for each warp (fewer where that leaves SMs without work).  Prompts, as many as leave every SM six
+  // CTAs: the cosines and sines of the rows serve all of them.
+  const long long each_head = (long long)chunks * a.c.n_seqs;
+  int each;
+  if (FEW) {
+    each = kWarps;
+    while (each > 1 && each_head * ((items + each - 1) / each) < a.n_sms) each /= 2;
+  } else {
+    long long groups = (6LL * a.n_sms + each_head - 1) / each_head;
+    groups = groups > items ? items : groups;
+    each = (int)((items + groups - 1) / groups);
+  }
+  auto kernel = quant_append_kernel<T, HD, FEW>;
   if (ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), (int)smem) != cudaSuccess) return VVS_ERR_CUDA;
   const cudaError_t e = launch_kernel(kernel, dim3(chunks, (items + each - 1) / each, a.c.n_seqs), dim3(kThreads), smem, true, s, a, each);
   return e == cudaSuccess ? VVS_OK : VVS_ERR_CUDA;
 }
 
-// a call of few rows, or of small blocks, keeps fewer rows of a head in registers
+// A call of few rows, or of small blocks, is one launch.  Of prompts the queries have a launch of their own, whose threads keep their
+// angles in registers and have no block to wait for.
 template <typename T, int HD>
 int launch_hd(const QAppendArgs& a, cudaStream_t s) {
   const int blk = 1 << a.c.block_log2, rows = a.n_rows < blk ? a.n_rows : blk;
-  if (rows <= kPassRows<HD>) return launch_passes<T, HD, 1>(a, s);
-  return launch_passes<T, HD, 128 / kPassRows<HD>>(a, s);
+  if (rows <= kFewPasses * kPassRows<HD, true>) return launch_rows<T, HD, true>(a, s);
+  if (a.n_heads > 0) {
+    RotateArgs ra{};
+    ra.rope = a.rope; ra.q = a.q; ra.q_out = a.q_out;
+    ra.n_seqs = a.c.n_seqs; ra.n_rows = a.n_rows; ra.n_heads = a.n_heads; ra.hd = HD; ra.status = a.status; ra.n_sms = a.n_sms;
+    const int rc = launch_rotate_axes<T>(ra, s);
+    if (rc != VVS_OK) return rc;
+  }
+  return launch_rows<T, HD, false>(a, s);
 }
 
 }  // namespace

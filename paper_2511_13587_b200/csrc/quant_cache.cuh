@@ -97,18 +97,21 @@ __device__ __forceinline__ void store8(float* p, const float (&x)[8]) { store4(p
 // are the elements that stay as they are, 8u .. 8u + 7 (n_pairs is a multiple of four there).
 __device__ __forceinline__ bool unit_split(const RopeAxes& r, int u) { return r.halves && 4 * u < r.n_pairs; }
 
-// cosine and sine of a pair's angle; pairs behind the last and pairs of an unknown axis are not turned
-__device__ __forceinline__ void pair_turn(const RopeAxes& r, int pair, int seq, int row, int n_seqs, int n_rows, int32_t* status, float& c, float& s) {
-  c = 1.f;
-  s = 0.f;
-  if (pair >= r.n_pairs) return;
+// A pair's positions [n_seqs][n_rows] (null: the pair is not turned, being behind the last or of an unknown axis) and frequency.  Its angle is
+// the float32 product of the two; the cosine and sine of position 0 are those of a pair that stays as it is.
+struct PairAxis {
+  const int32_t* pos;
+  float freq;
+};
+__device__ __forceinline__ PairAxis pair_axis(const RopeAxes& r, int pair, int n_seqs, int n_rows, int32_t* status) {
+  if (pair >= r.n_pairs) return {nullptr, 0.f};
   const int ax = r.axis[pair];
+  const float f = r.inv_freq[pair];
   if (ax < 0 || ax >= r.n_axes) {
     atomicOr(status, VVS_DEV_BAD_ARG);
-    return;
+    return {nullptr, 0.f};
   }
-  const float angle = __fmul_rn((float)r.pos[((size_t)ax * n_seqs + seq) * n_rows + row], r.inv_freq[pair]);
-  sincosf(angle, &s, &c);
+  return {r.pos + (size_t)ax * n_seqs * n_rows, f};
 }
 
 // products and sum rounded one by one: what a rotation gives does not depend on the kernel that it is part of

@@ -12,7 +12,7 @@ constexpr int kThreads = 128;
 constexpr int kFlight = 4;   // heads whose elements are on their way together
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads) rotate_axes_kernel(RotateArgs a, int heads_each) {
+__global__ void __launch_bounds__(kThreads, 7) rotate_axes_kernel(RotateArgs a, int heads_each) {
   grid_dep_launch();
   grid_dep_wait();
   const int units = a.hd / 8;
@@ -35,8 +35,14 @@ __global__ void __launch_bounds__(kThreads) rotate_axes_kernel(RotateArgs a, int
   Unit<T> x[kFlight];
   request(h0, x);
   float c[4], s[4];
+  int pos[4];
+  PairAxis pa[4];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) pair_turn(a.rope, 4 * u + j, seq, row, a.n_seqs, a.n_rows, a.status, c[j], s[j]);
+  for (int j = 0; j < 4; ++j) pa[j] = pair_axis(a.rope, 4 * u + j, a.n_seqs, a.n_rows, a.status);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) pos[j] = pa[j].pos ? pa[j].pos[(size_t)seq * a.n_rows + row] : 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) sincosf(__fmul_rn((float)pos[j], pa[j].freq), &s[j], &c[j]);
   for (int h = h0; h < h1; h += kFlight) {
     Unit<T> next[kFlight];
     request(h + kFlight, next);
