@@ -65,7 +65,7 @@ __device__ __forceinline__ void put_rows(const QAppendArgs& a, const Unit<T> (&r
   const bool split = turned && unit_split(a.rope, u), mine = turned && (split || !a.rope.halves);
   float* scale = scales + ((size_t)ch.seq * a.c.n_heads + head) * (a.c.cap >> a.c.block_log2) + ch.block;
   const float old = ch.live > 0 ? *scale : 0.f;
-  float amax = 0.f;
+  float amax = 0.f, zero = 0.f;                // zero: NaN once an infinity or a NaN has been seen
 #pragma unroll
   for (int p = 0; p < PASSES; ++p) {
     if (ch.t0 + p * kRows + r >= ch.tk) continue;
@@ -73,9 +73,26 @@ __device__ __forceinline__ void put_rows(const QAppendArgs& a, const Unit<T> (&r
     values_of<T, HD>(raw[p], mine, split, table, p * kRows + r, x);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float m = fabsf(x[e]);
-      if (m < CUDART_INF_F) amax = fmaxf(amax, m);
-      else odd = true;                         // an infinity becomes the largest code, a NaN zero
+      amax = fmaxf(amax, fabsf(x[e]));
+      zero = fmaf(x[e], 0.f, zero);
+    }
+  }
+  const bool strange = zero != zero;           // an infinity becomes the largest code, a NaN zero; neither counts for the scale
+  if (strange) {
+    odd = true;
+    amax = 0.f;
+#pragma unroll 1
+    for (int p = 0; p < PASSES; ++p) {
+      if (ch.t0 + p * kRows + r >= ch.tk) continue;
+      Unit<T> piece = raw[0];
+#pragma unroll
+      for (int j = 1; j < PASSES; ++j)
+        if (j == p) piece = raw[j];
+      float x[8];
+      values_of<T, HD>(piece, mine, split, table, p * kRows + r, x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (fabsf(x[e]) < CUDART_INF_F) amax = fmaxf(amax, fabsf(x[e]));
     }
   }
   __syncwarp();
@@ -98,7 +115,11 @@ __device__ __forceinline__ void put_rows(const QAppendArgs& a, const Unit<T> (&r
     float x[8];
     values_of<T, HD>(raw[p], mine, split, table, p * kRows + r, x);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = x[e] == x[e] ? x[e] * inv : 0.f;
+    for (int e = 0; e < 8; ++e) x[e] *= inv;
+    if (strange) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = x[e] == x[e] ? x[e] : 0.f;
+    }
     const uint32_t lo = to_e4m3x4(x[0], x[1], x[2], x[3]), hi = to_e4m3x4(x[4], x[5], x[6], x[7]);
     if (split) {
       *reinterpret_cast<uint32_t*>(at + 4 * u) = lo;
@@ -118,7 +139,7 @@ __device__ __forceinline__ void put_rows(const QAppendArgs& a, const Unit<T> (&r
 
 // FEW: a chunk's rows fit a warp's passes.
 template <typename T, int HD, bool FEW>
-__global__ void __launch_bounds__(kThreads) quant_append_kernel(QAppendArgs a, int items_each) {
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 3 : 1) quant_append_kernel(QAppendArgs a, int items_each) {
   constexpr int PASSES = FEW ? kFewPasses : 128 / kPassRows<HD, false>;
   extern __shared__ __align__(16) uint8_t smem[];
   float2* table = reinterpret_cast<float2*>(smem);     // [rows of the chunk][HD / 2] cosine, sine

@@ -1,10 +1,11 @@
 // Eviction from the 8-bit cache by accumulated attention weight: selection of what stays, then the moves.
 //
-// Selection: the keep-th largest of a head's weights is found digit by digit (four histograms of 256 over order-preserving 32-bit keys; a
-// guarded token's key is above every weight's); a bitmap of what stays follows, with the lower slots first among equals.
-// Moves: what stays in slots behind `keep` goes, in order, into the slots below that became free.  Sources and targets never overlap, so
-// the moves need no order among themselves, and only what fills a hole is read and written.  A cluster of CTAs has a head: every rank
-// selects by itself (the weights come from L2), and has a share of the target blocks.
+// Selection, a cluster of CTAs for a head, each with a range of its slots: order-preserving 32-bit keys of the weights in shared memory (a
+// guarded token's key is above every weight's); the keep-th largest digit by digit, four histograms of 256 summed over the ranks; a bitmap
+// of what stays, the lower slots first among equals; free slots below `keep` and movers behind it counted, and matched through a list.
+// Moves: what stays in slots behind `keep` goes, in order, into the slots below that became free, one CTA for a block of target slots.
+// Sources and targets never overlap, so only what fills a hole is read and written; the one block that holds both, where `keep` lies, is
+// left to a last launch.
 #include "quant_cache.cuh"
 #include "tc_common.cuh"
 
@@ -49,9 +50,12 @@ __device__ __forceinline__ int scan_exclusive(int v, int* warp_sums, int* total)
   return r;
 }
 
-__global__ void __launch_bounds__(1024) quant_evict_kernel(QEvictArgs a) {
+constexpr int kMaxRanks = 8;
+constexpr int kTogether = 4;                                   // slots of a thread whose weights travel together
+
+__global__ void __launch_bounds__(1024) quant_select_kernel(QEvictArgs a, int slots_each) {
   extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ int hist[256], warp_sums[33];
+  __shared__ int hist[2][256], warp_sums[33], counts[4];       // counts: equals, holes, movers of this rank
   __shared__ int digit_found, left_found;
   grid_dep_launch();
   grid_dep_wait();
@@ -84,70 +88,116 @@ __global__ void __launch_bounds__(1024) quant_evict_kernel(QEvictArgs a) {
     }
     return;
   }
-  auto key_at = [&](int slot) {
-    const int t = age ? age[slot] : slot;
-    return t < a.n_sink || t >= end_age - a.n_recent ? 0xffffffffu : key_of(mass[slot]);
+  auto all_sync = [&]() {
+    if (ranks > 1) tc::cluster_sync();
+    else __syncthreads();
   };
+  // this rank's slots s0 .. s1 - 1 and their keys
+  const int s0 = min(len, rank * slots_each), s1 = min(len, s0 + slots_each), n = s1 - s0, words = (n + 31) / 32;
+  uint32_t* keys = reinterpret_cast<uint32_t*>(smem);
+  uint32_t* stays = keys + slots_each;                         // [words]
+  int* before = reinterpret_cast<int*>(stays + slots_each / 32);       // [words] equals, then holes or movers before a word, in this rank
+  for (int i = tid; i < 256; i += blockDim.x) hist[0][i] = hist[1][i] = 0;
+  __syncthreads();
+  for (int i0 = tid; i0 < n; i0 += kTogether * blockDim.x) {
+    float w[kTogether];
+    int t[kTogether];
+#pragma unroll
+    for (int j = 0; j < kTogether; ++j) {
+      const int i = min(i0 + j * (int)blockDim.x, n - 1);
+      w[j] = mass[s0 + i];
+      t[j] = age ? age[s0 + i] : s0 + i;
+    }
+#pragma unroll
+    for (int j = 0; j < kTogether; ++j) {
+      const int i = i0 + j * blockDim.x;
+      if (i >= n) break;
+      const uint32_t k = t[j] < a.n_sink || t[j] >= end_age - a.n_recent ? 0xffffffffu : key_of(w[j]);
+      keys[i] = k;
+      atomicAdd(&hist[0][k >> 24], 1);
+    }
+  }
 
   // ---- the smallest key that stays, and how many of its equals do --------------------------------------------------------------
   uint32_t prefix = 0;
   int left = keep;
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    for (int i = tid; i < 256; i += blockDim.x) hist[i] = 0;
-    __syncthreads();
-    for (int slot = tid; slot < len; slot += blockDim.x) {
-      const uint32_t k = key_at(slot);
-      if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255u], 1);
+  for (int shift = 24, turn = 0; shift >= 0; shift -= 8, turn ^= 1) {
+    if (shift < 24) {
+      __syncthreads();
+      for (int i = tid; i < n; i += blockDim.x) {
+        const uint32_t k = keys[i];
+        if ((k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[turn][(k >> shift) & 255u], 1);
+      }
     }
-    __syncthreads();
+    all_sync();
     if (warp == 0) {                           // lane i has the bins 255 - 8i .. 248 - 8i, from the largest down
-      int mine = 0;
+      int bin[8], mine = 0;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) mine += hist[255 - 8 * lane - j];
+      for (int j = 0; j < 8; ++j) bin[j] = 0;
+      for (int k = 0; k < ranks; ++k)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) bin[j] += ranks > 1 ? tc::ld_cluster_s32(&hist[turn][255 - 8 * lane - j], k) : hist[turn][255 - 8 * lane - j];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) mine += bin[j];
       int upto = mine;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
         const int y = __shfl_up_sync(0xffffffffu, upto, o);
         if (lane >= o) upto += y;
       }
-      int before = upto - mine;
-      if (before < left && upto >= left) {
+      int above = upto - mine;
+      if (above < left && upto >= left) {
+        bool found = false;
+#pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const int n = hist[255 - 8 * lane - j];
-          if (before + n >= left) {
+          if (!found && above + bin[j] >= left) {
             digit_found = 255 - 8 * lane - j;
-            left_found = left - before;
-            break;
+            left_found = left - above;
+            found = true;
           }
-          before += n;
+          above += bin[j];
         }
       }
+    } else {                                   // the other histogram is read by nobody now: the next turn's
+      for (int i = tid - 32; i < 256; i += blockDim.x - 32) hist[turn ^ 1][i] = 0;
     }
     __syncthreads();
     prefix |= (uint32_t)digit_found << shift;
     left = left_found;
-    __syncthreads();
   }
 
   // ---- a bitmap of what stays; free slots below `keep` and movers behind it, counted word by word ---------------------------------
-  const int words = (len + 31) / 32;
-  uint32_t* stays = reinterpret_cast<uint32_t*>(smem);
-  int* movers_before = reinterpret_cast<int*>(stays + words);  // of the words from keep / 32 on
-  int* holes_before = movers_before + words + 1;
   for (int w = warp; w < words; w += n_warps) {
-    const int slot = w * 32 + lane;
-    const uint32_t k = slot < len ? key_at(slot) : 0u;
-    const uint32_t more = __ballot_sync(0xffffffffu, slot < len && k > prefix), equal = __ballot_sync(0xffffffffu, slot < len && k == prefix);
+    const int i = w * 32 + lane;
+    const uint32_t k = i < n ? keys[i] : 0u;
+    const uint32_t more = __ballot_sync(0xffffffffu, i < n && k > prefix), equal = __ballot_sync(0xffffffffu, i < n && k == prefix);
     if (lane == 0) {
       stays[w] = more;
-      holes_before[w] = (int)equal;
+      before[w] = (int)equal;
     }
   }
   __syncthreads();
+  // what lower ranks have of a count, once every rank has said its own
+  auto of_lower = [&](int which, int mine) {
+    if (ranks == 1) return 0;
+    if (tid == 0) counts[which] = mine;
+    all_sync();
+    int sum = 0;
+    for (int k = 0; k < rank; ++k) sum += tc::ld_cluster_s32(&counts[which], k);
+    return sum;
+  };
   int run = 0;
+  if (ranks > 1) {                                             // equals of this rank, so that the ranks above know where theirs begin
+    for (int w0 = 0; w0 < words; w0 += blockDim.x) {
+      int total;
+      scan_exclusive(w0 + tid < words ? __popc((uint32_t)before[w0 + tid]) : 0, warp_sums, &total);
+      run += total;
+    }
+    run = of_lower(0, run);
+  }
   for (int w0 = 0; w0 < words; w0 += blockDim.x) {
     const int w = w0 + tid;
-    uint32_t equal = w < words ? (uint32_t)holes_before[w] : 0u;
+    uint32_t equal = w < words ? (uint32_t)before[w] : 0u;
     int total;
     int take = left - (run + scan_exclusive(__popc(equal), warp_sums, &total));
     run += total;
@@ -161,108 +211,132 @@ __global__ void __launch_bounds__(1024) quant_evict_kernel(QEvictArgs a) {
     }
   }
   __syncthreads();
-  const int keep_word = keep / 32;
-  const uint32_t below = (1u << (keep & 31)) - 1u;             // of the word that keep lies in
+  // free slots and movers of a word of this rank
+  auto free_bits = [&](int w) {
+    const int at = keep - (s0 + w * 32);                       // slots of the word below keep
+    const uint32_t below = at >= 32 ? 0xffffffffu : at <= 0 ? 0u : (1u << at) - 1u;
+    return ~stays[w] & below;
+  };
+  auto move_bits = [&](int w) {
+    const int at = keep - (s0 + w * 32);
+    const uint32_t below = at >= 32 ? 0xffffffffu : at <= 0 ? 0u : (1u << at) - 1u;
+    return stays[w] & ~below;
+  };
   int holes = 0, movers = 0;
-  for (int w0 = 0; w0 < words; w0 += blockDim.x) {
-    const int w = w0 + tid;
-    const uint32_t s = w < words ? stays[w] : 0u;
-    const uint32_t free_bits = w < keep_word ? ~s : w == keep_word ? ~s & below : 0u;
-    const uint32_t move_bits = w > keep_word ? s : w == keep_word ? s & ~below : 0u;
+  for (int w0 = 0; w0 < words; w0 += blockDim.x) {             // a word has free slots or movers to be numbered, but that of keep: movers there
+    const int w = w0 + tid;                                    // are numbered by their own bits again below
     int total;
-    const int h = scan_exclusive(__popc(free_bits), warp_sums, &total) + holes;
+    const int h = scan_exclusive(w < words ? __popc(free_bits(w)) : 0, warp_sums, &total) + holes;
     holes += total;
-    const int m = scan_exclusive(__popc(move_bits), warp_sums, &total) + movers;
+    const int m = scan_exclusive(w < words ? __popc(move_bits(w)) : 0, warp_sums, &total) + movers;
     movers += total;
-    if (w < words) {
-      holes_before[w] = h;
-      movers_before[w] = m;
+    if (w < words) before[w] = s0 + w * 32 < keep ? h : m;
+  }
+  const int holes_lower = of_lower(1, holes), movers_lower = of_lower(2, movers);
+  __syncthreads();
+  // the movers' slots, in order, where the weights' new places will be
+  int32_t* list = reinterpret_cast<int32_t*>(mass_out);
+  for (int w = warp; w < words; w += n_warps) {
+    const uint32_t bits = move_bits(w);
+    if (!bits) continue;
+    // (the word of keep is the first that has movers)
+    const int base = movers_lower + (s0 + w * 32 < keep ? 0 : before[w]);
+    if ((bits >> lane) & 1u) list[base + __popc(bits & ((1u << lane) - 1u))] = s0 + w * 32 + lane;
+  }
+  all_sync();
+  for (int d = s0 + tid; d < min(keep, s1); d += blockDim.x) {
+    const int i = d - s0, w = i >> 5;
+    const uint32_t bits = free_bits(w);
+    kept[d] = (bits >> (i & 31)) & 1u ? list[holes_lower + before[w] + __popc(bits & ((1u << (i & 31)) - 1u))] : d;
+  }
+  all_sync();
+  for (int d0 = s0 + tid; d0 < min(keep, s1); d0 += kTogether * blockDim.x) {
+    int from[kTogether];
+#pragma unroll
+    for (int j = 0; j < kTogether; ++j) from[j] = kept[min(d0 + j * (int)blockDim.x, min(keep, s1) - 1)];
+    float w[kTogether];
+    int t[kTogether];
+#pragma unroll
+    for (int j = 0; j < kTogether; ++j) {
+      w[j] = mass[from[j]];
+      t[j] = age ? age[from[j]] : from[j];
+    }
+#pragma unroll
+    for (int j = 0; j < kTogether; ++j) {
+      const int d = d0 + j * blockDim.x;
+      if (d >= min(keep, s1)) break;
+      mass_out[d] = w[j];
+      if (age_out) age_out[d] = t[j];
     }
   }
-  __syncthreads();
+  if (ranks > 1) tc::cluster_sync();                           // (a rank's counts are read until here)
+}
 
-  // ---- this rank's target blocks: where each slot's row comes from ------------------------------------------------------------------
-  const int blk_log2 = a.c.block_log2, blk = 1 << blk_log2;
-  const int blocks = (keep + blk - 1) >> blk_log2, per = (blocks + ranks - 1) / ranks;
-  const int b0 = min(blocks, rank * per), b1 = min(blocks, b0 + per);
-  float* now = reinterpret_cast<float*>(holes_before + words + 1);      // [per][2] new scales
-  for (int d = (b0 << blk_log2) + tid; d < min(keep, b1 << blk_log2); d += blockDim.x) {
+// One block of target slots: new scales from the old ones, rows that come in or are rounded again into registers, and back once all are read.
+// A block where `keep` lies has sources of its own rows too, and its rows behind keep go with its scale: it is done when all others are.
+template <int HD>
+__global__ void __launch_bounds__(256) quant_move_kernel(QEvictArgs a, int block0) {
+  constexpr int kChunks = HD / 16, kMine = 128 * kChunks / 256;              // 16-byte pieces of a row; of a thread, in blocks of 128
+  __shared__ int from_of[128];
+  __shared__ float top[2][4];
+  grid_dep_launch();
+  grid_dep_wait();
+  const int tid = threadIdx.x, b = block0 + blockIdx.x, head = blockIdx.y, seq = blockIdx.z;
+  const int len = a.cache_len[seq], keep = a.keep, blk_log2 = a.c.block_log2, blk = 1 << blk_log2;
+  if (len <= keep || len > a.c.cap) return;
+  const size_t item = (size_t)seq * a.c.n_heads + head, scale_row = item * (a.c.cap >> blk_log2);
+  const int d0 = b << blk_log2;
+  float ks = 0.f, vs = 0.f;
+  bool moved = false;
+  if (tid < 128) {
+    const int d = d0 + tid;
     int from = d;
-    if (!((stays[d >> 5] >> (d & 31)) & 1u)) {
-      const int r = holes_before[d >> 5] + __popc(~stays[d >> 5] & ((1u << (d & 31)) - 1u));
-      int lo = keep_word, hi = words - 1;                     // the last word with at most r movers before it
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (movers_before[mid] <= r) lo = mid; else hi = mid - 1;
-      }
-      uint32_t s = lo == keep_word ? stays[lo] & ~below : stays[lo];
-      for (int j = r - movers_before[lo]; j > 0; --j) s &= s - 1u;
-      from = lo * 32 + __ffs(s) - 1;
+    if (tid < blk && d < keep) from = a.kept[item * keep + d];
+    from_of[tid] = from;
+    if (from != d) {
+      moved = true;
+      ks = a.c.k_scale[scale_row + (from >> blk_log2)];
+      vs = a.c.v_scale[scale_row + (from >> blk_log2)];
     }
-    kept[d] = from;
-    mass_out[d] = mass[from];
-    if (age_out) age_out[d] = age ? age[from] : from;
-  }
-  __syncthreads();
-
-  // ---- new scales, from the old ones ---------------------------------------------------------------------------------------------------
-  const size_t scale_row = item * (cap >> blk_log2);
-  for (int b = b0 + warp; b < b1; b += n_warps) {
-    float ks = 0.f, vs = 0.f;
-    for (int i = lane; i < blk; i += 32) {
-      const int d = (b << blk_log2) + i;
-      if (d >= keep) break;
-      const int from = kept[d];
-      if (from == d) continue;
-      ks = fmaxf(ks, a.c.k_scale[scale_row + (from >> blk_log2)]);
-      vs = fmaxf(vs, a.c.v_scale[scale_row + (from >> blk_log2)]);
-    }
-    __syncwarp();
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
       ks = fmaxf(ks, __shfl_xor_sync(0xffffffffu, ks, o));
       vs = fmaxf(vs, __shfl_xor_sync(0xffffffffu, vs, o));
     }
-    if (lane == 0) {
-      now[2 * (b - b0)] = fmaxf(ks, a.c.k_scale[scale_row + b]);
-      now[2 * (b - b0) + 1] = fmaxf(vs, a.c.v_scale[scale_row + b]);
+    if (tid % 32 == 0) {
+      top[0][tid / 32] = ks;
+      top[1][tid / 32] = vs;
     }
   }
-  __syncthreads();
-
-  // ---- the moves, 16 bytes a thread; rows that stay in a block whose scale grows are rounded again --------------------------------------
-  const int chunks = a.c.hd / 16;
-  auto rescaled = [](uint4 v, float f) {
-    return make_uint4(rescale_e4m3x4(v.x, f), rescale_e4m3x4(v.y, f), rescale_e4m3x4(v.z, f), rescale_e4m3x4(v.w, f));
-  };
-  for (int i = tid; i < ((b1 - b0) << blk_log2) * chunks; i += blockDim.x) {
-    const int d = (b0 << blk_log2) + i / chunks, cc = i % chunks;
-    if (d >= keep) continue;
-    const int from = kept[d], b = d >> blk_log2;
+  if (!__syncthreads_or(moved)) return;
 #pragma unroll
-    for (int kv = 0; kv < 2; ++kv) {
-      uint4* rows = reinterpret_cast<uint4*>((kv ? a.c.v : a.c.k) + item * cap * a.c.hd);
-      const float was = (kv ? a.c.v_scale : a.c.k_scale)[scale_row + (from >> blk_log2)], f = was / now[2 * (b - b0) + kv];
-      if (from == d && f == 1.f) continue;
-      const uint4 v = rows[(size_t)from * chunks + cc];
-      rows[(size_t)d * chunks + cc] = f == 1.f ? v : rescaled(v, f);
+  for (int kv = 0; kv < 2; ++kv) {
+    float* scales = (kv ? a.c.v_scale : a.c.k_scale) + scale_row;
+    const float old = scales[b], now = fmaxf(fmaxf(fmaxf(top[kv][0], top[kv][1]), fmaxf(top[kv][2], top[kv][3])), old), grown = old / now;
+    uint4* rows = reinterpret_cast<uint4*>((kv ? a.c.v : a.c.k) + item * a.c.cap * HD);
+    uint4 v[kMine];
+    float f[kMine];
+#pragma unroll
+    for (int j = 0; j < kMine; ++j) {
+      const int i = tid + j * 256, r = i / kChunks;
+      f[j] = -1.f;                                             // nothing to write
+      if (r >= blk) continue;
+      const int from = from_of[r];
+      const bool stays = from == d0 + r;
+      f[j] = stays ? grown : scales[from >> blk_log2] / now;
+      if (stays && grown == 1.f) f[j] = -1.f;
+      else v[j] = rows[(size_t)from * kChunks + i % kChunks];
     }
-  }
-  if (ranks > 1) tc::cluster_sync(); else __syncthreads();     // every rank has read the old scales and its sources
-  if (rank == (blocks - 1) / per && (keep & (blk - 1))) {      // the block that keep lies in: the rows behind it go with its scale
-    const int b = blocks - 1;
-    for (int i = tid; i < ((blocks << blk_log2) - keep) * chunks; i += blockDim.x)
+    __syncthreads();
 #pragma unroll
-      for (int kv = 0; kv < 2; ++kv) {
-        uint4* rows = reinterpret_cast<uint4*>((kv ? a.c.v : a.c.k) + item * cap * a.c.hd) + (size_t)keep * chunks;
-        const float f = (kv ? a.c.v_scale : a.c.k_scale)[scale_row + b] / now[2 * (b - b0) + kv];
-        if (f != 1.f) rows[i] = rescaled(rows[i], f);
-      }
-  }
-  __syncthreads();
-  for (int b = b0 + tid; b < b1; b += blockDim.x) {
-    a.c.k_scale[scale_row + b] = now[2 * (b - b0)];
-    a.c.v_scale[scale_row + b] = now[2 * (b - b0) + 1];
+    for (int j = 0; j < kMine; ++j) {
+      const int i = tid + j * 256;
+      if (f[j] < 0.f) continue;
+      uint4 x = v[j];
+      if (f[j] != 1.f) x = make_uint4(rescale_e4m3x4(x.x, f[j]), rescale_e4m3x4(x.y, f[j]), rescale_e4m3x4(x.z, f[j]), rescale_e4m3x4(x.w, f[j]));
+      rows[(size_t)(d0 + i / kChunks) * kChunks + i % kChunks] = x;
+    }
+    if (tid == 0) scales[b] = now;
   }
 }
 
@@ -270,15 +344,16 @@ __global__ void __launch_bounds__(1024) quant_evict_kernel(QEvictArgs a) {
 
 int launch_quant_evict(const QEvictArgs& a, cudaStream_t s) {
   if (a.c.cap > kMaxCap) return VVS_ERR_SHAPE;
-  const int blocks = (a.keep + (1 << a.c.block_log2) - 1) >> a.c.block_log2, words = (a.c.cap + 31) / 32;
+  // a rank for every 4096 slots, while that does not leave more CTAs than SMs
   const long long items = (long long)a.c.n_seqs * a.c.n_heads;
   int ranks = 1;
-  while (ranks < 8 && items * ranks * 2 <= a.n_sms && blocks >= 4 * ranks) ranks *= 2;
-  const size_t smem = (size_t)(3 * words + 2) * 4 + (size_t)((blocks + ranks - 1) / ranks) * 8;
-  if (ensure_dynamic_smem(reinterpret_cast<const void*>(quant_evict_kernel), (int)smem) != cudaSuccess) return VVS_ERR_CUDA;
+  while (ranks < kMaxRanks && (a.c.cap > 16384 * ranks || (items * ranks * 2 <= a.n_sms && a.c.cap >= 8192 * ranks))) ranks *= 2;
+  const int slots = ((a.c.cap + ranks - 1) / ranks + 31) / 32 * 32;
+  const size_t smem = (size_t)slots * 4 + (size_t)slots / 32 * 8;
+  if (ensure_dynamic_smem(reinterpret_cast<const void*>(quant_select_kernel), (int)smem) != cudaSuccess) return VVS_ERR_CUDA;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(ranks, a.c.n_heads, a.c.n_seqs);
-  cfg.blockDim = dim3(a.c.cap <= 2048 ? 256 : 1024);
+  cfg.blockDim = dim3(slots <= 1024 ? 256 : slots <= 2048 ? 512 : 1024);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
   cudaLaunchAttribute attr[2];
@@ -289,7 +364,12 @@ int launch_quant_evict(const QEvictArgs& a, cudaStream_t s) {
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, quant_evict_kernel, a) == cudaSuccess ? VVS_OK : VVS_ERR_CUDA;
+  if (cudaLaunchKernelEx(&cfg, quant_select_kernel, a, slots) != cudaSuccess) return VVS_ERR_CUDA;
+  const int whole = a.keep >> a.c.block_log2, part = a.keep & ((1 << a.c.block_log2) - 1);
+  auto move = a.c.hd == 64 ? quant_move_kernel<64> : quant_move_kernel<128>;
+  if (whole > 0 && launch_kernel(move, dim3(whole, a.c.n_heads, a.c.n_seqs), dim3(256), 0, true, s, a, 0) != cudaSuccess) return VVS_ERR_CUDA;
+  if (part > 0 && launch_kernel(move, dim3(1, a.c.n_heads, a.c.n_seqs), dim3(256), 0, true, s, a, whole) != cudaSuccess) return VVS_ERR_CUDA;
+  return VVS_OK;
 }
 
 }  // namespace vvs
