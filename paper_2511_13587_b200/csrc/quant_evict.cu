@@ -1,7 +1,8 @@
 // Eviction from the 8-bit cache by accumulated attention weight: selection of what stays, then the moves.
 //
 // Selection, a cluster of CTAs for a head, each with a range of its slots: order-preserving 32-bit keys of the weights in shared memory (a
-// guarded token's key is above every weight's); the keep-th largest digit by digit, four histograms of 256 summed over the ranks; a bitmap
+// guarded token's key is above every weight's); the keep-th largest digit by digit,
+// histograms summed over the ranks; a bitmap
 // of what stays, the lower slots first among equals; free slots below `keep` and movers behind it counted, and matched through a list.
 // Moves: what stays in slots behind `keep` goes, in order, into the slots below that became free, one CTA for a block of target slots.
 // Sources and targets never overlap, so only what fills a hole is read and written; the one block that holds both, where `keep` lies, is
@@ -53,14 +54,18 @@ __device__ __forceinline__ int scan_exclusive(int v, int* warp_sums, int* total)
 constexpr int kMaxRanks = 8;
 constexpr int kTogether = 4;                                   // slots of a thread whose weights travel together
 
+// FEW slots: one CTA, digits of 8 bits, four histograms.  Otherwise 1024 threads of one or several CTAs and digits of 11 bits, three
+// histograms: of 8 bits, so many threads would add to the handful of bins that weights' exponents are that the adding costs more.
+template <bool FEW>
 __global__ void __launch_bounds__(1024) quant_select_kernel(QEvictArgs a, int slots_each) {
+  constexpr int BITS = FEW ? 8 : 11, kBins = 1 << BITS, kTurns = FEW ? 4 : 3;
   extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ int hist[2][256], warp_sums[33], counts[4];       // counts: equals, holes, movers of this rank
+  __shared__ int hist[2][kBins], warp_sums[33], counts[3];     // counts: equals, holes, movers of this rank
   __shared__ int digit_found, left_found;
   grid_dep_launch();
   grid_dep_wait();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n_warps = blockDim.x >> 5;
-  const int ranks = gridDim.x, rank = blockIdx.x, head = blockIdx.y, seq = blockIdx.z;
+  const int ranks = FEW ? 1 : gridDim.x, rank = FEW ? 0 : blockIdx.x, head = blockIdx.y, seq = blockIdx.z;
   const int cap = a.c.cap, keep = a.keep, len = a.cache_len[seq];
   if (len < 0 || len > cap) {                                  // (the same for every rank)
     if (rank == 0 && head == 0 && tid == 0) atomicOr(a.status, VVS_DEV_CACHE_OVERFLOW);
@@ -97,7 +102,7 @@ __global__ void __launch_bounds__(1024) quant_select_kernel(QEvictArgs a, int sl
   uint32_t* keys = reinterpret_cast<uint32_t*>(smem);
   uint32_t* stays = keys + slots_each;                         // [words]
   int* before = reinterpret_cast<int*>(stays + slots_each / 32);       // [words] equals, then holes or movers before a word, in this rank
-  for (int i = tid; i < 256; i += blockDim.x) hist[0][i] = hist[1][i] = 0;
+  for (int i = tid; i < kBins; i += blockDim.x) hist[0][i] = hist[1][i] = 0;
   __syncthreads();
   for (int i0 = tid; i0 < n; i0 += kTogether * blockDim.x) {
     float w[kTogether];
@@ -114,56 +119,83 @@ __global__ void __launch_bounds__(1024) quant_select_kernel(QEvictArgs a, int sl
       if (i >= n) break;
       const uint32_t k = t[j] < a.n_sink || t[j] >= end_age - a.n_recent ? 0xffffffffu : key_of(w[j]);
       keys[i] = k;
-      atomicAdd(&hist[0][k >> 24], 1);
+      atomicAdd(&hist[0][k >> (32 - BITS)], 1);
     }
   }
 
   // ---- the smallest key that stays, and how many of its equals do --------------------------------------------------------------
   uint32_t prefix = 0;
   int left = keep;
-  for (int shift = 24, turn = 0; shift >= 0; shift -= 8, turn ^= 1) {
-    if (shift < 24) {
-      __syncthreads();
+#pragma unroll 1
+  for (int turn = 0, above_bit = 32; turn < kTurns; ++turn, above_bit -= BITS) {
+    const int shift = max(0, above_bit - BITS);
+    int* bins = hist[turn & 1];
+    if (turn > 0) {
       for (int i = tid; i < n; i += blockDim.x) {
         const uint32_t k = keys[i];
-        if ((k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[turn][(k >> shift) & 255u], 1);
+        if ((k >> above_bit) == (prefix >> above_bit)) atomicAdd(&bins[(k >> shift) & ((1 << (above_bit - shift)) - 1)], 1);
       }
     }
     all_sync();
-    if (warp == 0) {                           // lane i has the bins 255 - 8i .. 248 - 8i, from the largest down
-      int bin[8], mine = 0;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) bin[j] = 0;
-      for (int k = 0; k < ranks; ++k)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) bin[j] += ranks > 1 ? tc::ld_cluster_s32(&hist[turn][255 - 8 * lane - j], k) : hist[turn][255 - 8 * lane - j];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) mine += bin[j];
-      int upto = mine;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, upto, o);
-        if (lane >= o) upto += y;
-      }
-      int above = upto - mine;
-      if (above < left && upto >= left) {
-        bool found = false;
+    if (FEW) {                                 // a warp's sums, bins 255 - 8 lane and down; the others clear the next turn's
+      if (warp == 0) {
+        int bin[8], mine = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          if (!found && above + bin[j] >= left) {
-            digit_found = 255 - 8 * lane - j;
-            left_found = left - above;
-            found = true;
-          }
-          above += bin[j];
+          bin[j] = bins[255 - 8 * lane - j];
+          mine += bin[j];
+        }
+        int upto = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int y = __shfl_up_sync(0xffffffffu, upto, o);
+          if (lane >= o) upto += y;
+        }
+        int above = upto - mine;
+        if (above < left && upto >= left) {
+          int j = 0;
+#pragma unroll
+          for (int q = 0; q < 7; ++q)
+            if (j == q && above + bin[q] < left) {
+              above += bin[q];
+              ++j;
+            }
+          digit_found = 255 - 8 * lane - j;
+          left_found = left - above;
+        }
+      } else {
+        for (int i = tid - 32; i < kBins; i += blockDim.x - 32) hist[(turn & 1) ^ 1][i] = 0;
+      }
+    } else {                                   // bins 2047 - 2 tid and the one below, of all ranks
+      const int at = 2046 - 2 * tid;
+      int hi = 0, lo = 0, total;
+      if (ranks == 1) {
+        hi = bins[at + 1];
+        lo = bins[at];
+      } else {
+        int c[2 * kMaxRanks];
+#pragma unroll
+        for (int k = 0; k < kMaxRanks; ++k) {
+          c[2 * k] = k < ranks ? tc::ld_cluster_s32(&bins[at + 1], k) : 0;
+          c[2 * k + 1] = k < ranks ? tc::ld_cluster_s32(&bins[at], k) : 0;
+        }
+#pragma unroll
+        for (int k = 0; k < kMaxRanks; ++k) {
+          hi += c[2 * k];
+          lo += c[2 * k + 1];
         }
       }
-    } else {                                   // the other histogram is read by nobody now: the next turn's
-      for (int i = tid - 32; i < 256; i += blockDim.x - 32) hist[turn ^ 1][i] = 0;
+      const int above = scan_exclusive(hi + lo, warp_sums, &total);
+      if (above < left && above + hi + lo >= left) {
+        digit_found = above + hi >= left ? at + 1 : at;
+        left_found = left - above - (above + hi >= left ? 0 : hi);
+      }
+      for (int i = tid; i < kBins; i += blockDim.x) hist[(turn & 1) ^ 1][i] = 0;
     }
     __syncthreads();
     prefix |= (uint32_t)digit_found << shift;
     left = left_found;
+    __syncthreads();
   }
 
   // ---- a bitmap of what stays; free slots below `keep` and movers behind it, counted word by word ---------------------------------
@@ -177,15 +209,6 @@ __global__ void __launch_bounds__(1024) quant_select_kernel(QEvictArgs a, int sl
     }
   }
   __syncthreads();
-  // what lower ranks have of a count, once every rank has said its own
-  auto of_lower = [&](int which, int mine) {
-    if (ranks == 1) return 0;
-    if (tid == 0) counts[which] = mine;
-    all_sync();
-    int sum = 0;
-    for (int k = 0; k < rank; ++k) sum += tc::ld_cluster_s32(&counts[which], k);
-    return sum;
-  };
   int run = 0;
   if (ranks > 1) {                                             // equals of this rank, so that the ranks above know where theirs begin
     for (int w0 = 0; w0 < words; w0 += blockDim.x) {
@@ -193,7 +216,10 @@ __global__ void __launch_bounds__(1024) quant_select_kernel(QEvictArgs a, int sl
       scan_exclusive(w0 + tid < words ? __popc((uint32_t)before[w0 + tid]) : 0, warp_sums, &total);
       run += total;
     }
-    run = of_lower(0, run);
+    if (tid == 0) counts[0] = run;
+    tc::cluster_sync();
+    run = 0;
+    for (int k = 0; k < rank; ++k) run += tc::ld_cluster_s32(&counts[0], k);
   }
   for (int w0 = 0; w0 < words; w0 += blockDim.x) {
     const int w = w0 + tid;
@@ -223,37 +249,54 @@ __global__ void __launch_bounds__(1024) quant_select_kernel(QEvictArgs a, int sl
     return stays[w] & ~below;
   };
   int holes = 0, movers = 0;
-  for (int w0 = 0; w0 < words; w0 += blockDim.x) {             // a word has free slots or movers to be numbered, but that of keep: movers there
-    const int w = w0 + tid;                                    // are numbered by their own bits again below
+  for (int w0 = 0; w0 < words; w0 += blockDim.x) {             // (both counts in one sum: a rank has at most 2^14 slots)
+    const int w = w0 + tid;
     int total;
-    const int h = scan_exclusive(w < words ? __popc(free_bits(w)) : 0, warp_sums, &total) + holes;
-    holes += total;
-    const int m = scan_exclusive(w < words ? __popc(move_bits(w)) : 0, warp_sums, &total) + movers;
-    movers += total;
-    if (w < words) before[w] = s0 + w * 32 < keep ? h : m;
+    const int both = scan_exclusive(w < words ? __popc(free_bits(w)) << 16 | __popc(move_bits(w)) : 0, warp_sums, &total);
+    // free slots or movers before the word, as it lies below keep or not; of the word of keep, free slots: its movers are the first
+    if (w < words) before[w] = s0 + w * 32 < keep ? (both >> 16) + holes : (both & 0xffff) + movers;
+    holes += total >> 16;
+    movers += total & 0xffff;
   }
-  const int holes_lower = of_lower(1, holes), movers_lower = of_lower(2, movers);
+  // the movers' slots, in order: of one rank in the place of the keys, of several where the weights' new places will be
+  int holes_lower = 0, movers_lower = 0;
+  if (ranks > 1) {
+    if (tid == 0) {
+      counts[1] = holes;
+      counts[2] = movers;
+    }
+    tc::cluster_sync();
+    for (int k = 0; k < rank; ++k) {
+      holes_lower += tc::ld_cluster_s32(&counts[1], k);
+      movers_lower += tc::ld_cluster_s32(&counts[2], k);
+    }
+  }
   __syncthreads();
-  // the movers' slots, in order, where the weights' new places will be
-  int32_t* list = reinterpret_cast<int32_t*>(mass_out);
+  int32_t* list = ranks > 1 ? reinterpret_cast<int32_t*>(mass_out) : reinterpret_cast<int32_t*>(keys);
   for (int w = warp; w < words; w += n_warps) {
     const uint32_t bits = move_bits(w);
     if (!bits) continue;
-    // (the word of keep is the first that has movers)
     const int base = movers_lower + (s0 + w * 32 < keep ? 0 : before[w]);
     if ((bits >> lane) & 1u) list[base + __popc(bits & ((1u << lane) - 1u))] = s0 + w * 32 + lane;
   }
   all_sync();
-  for (int d = s0 + tid; d < min(keep, s1); d += blockDim.x) {
+  auto source_of = [&](int d) {
     const int i = d - s0, w = i >> 5;
     const uint32_t bits = free_bits(w);
-    kept[d] = (bits >> (i & 31)) & 1u ? list[holes_lower + before[w] + __popc(bits & ((1u << (i & 31)) - 1u))] : d;
+    return (bits >> (i & 31)) & 1u ? list[holes_lower + before[w] + __popc(bits & ((1u << (i & 31)) - 1u))] : d;
+  };
+  const int e1 = min(keep, s1);
+  if (ranks > 1) {                                             // (the list has to be read before the weights' places are written)
+    for (int d = s0 + tid; d < e1; d += blockDim.x) kept[d] = source_of(d);
+    tc::cluster_sync();
   }
-  all_sync();
-  for (int d0 = s0 + tid; d0 < min(keep, s1); d0 += kTogether * blockDim.x) {
+  for (int d0 = s0 + tid; d0 < e1; d0 += kTogether * blockDim.x) {
     int from[kTogether];
 #pragma unroll
-    for (int j = 0; j < kTogether; ++j) from[j] = kept[min(d0 + j * (int)blockDim.x, min(keep, s1) - 1)];
+    for (int j = 0; j < kTogether; ++j) {
+      const int d = min(d0 + j * (int)blockDim.x, e1 - 1);
+      from[j] = ranks > 1 ? kept[d] : source_of(d);
+    }
     float w[kTogether];
     int t[kTogether];
 #pragma unroll
@@ -264,7 +307,8 @@ __global__ void __launch_bounds__(1024) quant_select_kernel(QEvictArgs a, int sl
 #pragma unroll
     for (int j = 0; j < kTogether; ++j) {
       const int d = d0 + j * blockDim.x;
-      if (d >= min(keep, s1)) break;
+      if (d >= e1) break;
+      if (ranks == 1) kept[d] = from[j];
       mass_out[d] = w[j];
       if (age_out) age_out[d] = t[j];
     }
@@ -344,16 +388,19 @@ __global__ void __launch_bounds__(256) quant_move_kernel(QEvictArgs a, int block
 
 int launch_quant_evict(const QEvictArgs& a, cudaStream_t s) {
   if (a.c.cap > kMaxCap) return VVS_ERR_SHAPE;
-  // a rank for every 4096 slots, while that does not leave more CTAs than SMs
+  // a rank for every 4096 slots, while that does not leave more CTAs than SMs (32 heads of 32K slots: 81 us with four ranks, 140 with
+  // eight, whose clusters do not fit all at once)
   const long long items = (long long)a.c.n_seqs * a.c.n_heads;
   int ranks = 1;
   while (ranks < kMaxRanks && (a.c.cap > 16384 * ranks || (items * ranks * 2 <= a.n_sms && a.c.cap >= 8192 * ranks))) ranks *= 2;
   const int slots = ((a.c.cap + ranks - 1) / ranks + 31) / 32 * 32;
   const size_t smem = (size_t)slots * 4 + (size_t)slots / 32 * 8;
-  if (ensure_dynamic_smem(reinterpret_cast<const void*>(quant_select_kernel), (int)smem) != cudaSuccess) return VVS_ERR_CUDA;
+  const bool few = ranks == 1 && slots <= 2048;
+  auto select = few ? quant_select_kernel<true> : quant_select_kernel<false>;
+  if (ensure_dynamic_smem(reinterpret_cast<const void*>(select), (int)smem) != cudaSuccess) return VVS_ERR_CUDA;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(ranks, a.c.n_heads, a.c.n_seqs);
-  cfg.blockDim = dim3(slots <= 1024 ? 256 : slots <= 2048 ? 512 : 1024);
+  cfg.blockDim = dim3(!few ? 1024 : slots <= 1024 ? 256 : 512);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
   cudaLaunchAttribute attr[2];
@@ -364,7 +411,7 @@ int launch_quant_evict(const QEvictArgs& a, cudaStream_t s) {
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  if (cudaLaunchKernelEx(&cfg, quant_select_kernel, a, slots) != cudaSuccess) return VVS_ERR_CUDA;
+  if (cudaLaunchKernelEx(&cfg, select, a, slots) != cudaSuccess) return VVS_ERR_CUDA;
   const int whole = a.keep >> a.c.block_log2, part = a.keep & ((1 << a.c.block_log2) - 1);
   auto move = a.c.hd == 64 ? quant_move_kernel<64> : quant_move_kernel<128>;
   if (whole > 0 && launch_kernel(move, dim3(whole, a.c.n_heads, a.c.n_seqs), dim3(256), 0, true, s, a, 0) != cudaSuccess) return VVS_ERR_CUDA;
