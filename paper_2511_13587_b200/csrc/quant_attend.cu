@@ -156,7 +156,7 @@ __global__ void __launch_bounds__(kThreads, Layout<HD, MT, sizeof(T) == 4>::kCta
   auto request = [&](int slice, uint32_t at, bool with_values) {
     const size_t from = (size_t)slice * (16 * HD);
     const int left = end - (slice << 4);
-    if (left >= 16) {
+    if (left >= 16 && (slice << 4) >= first) {
       copy16<0, 0>(key_to + at, keys_at + from);
       copy16<512, 512>(key_to + at, keys_at + from);
       if (HD == 128) {
@@ -171,10 +171,11 @@ __global__ void __launch_bounds__(kThreads, Layout<HD, MT, sizeof(T) == 4>::kCta
           copy16<1536, 1536>(value_odd + at, values_at + from);
         }
       }
-    } else {                                                              // the last slice: zeros behind the last key
+    } else {                                                              // zeros in the place of slots that no row sees
 #pragma unroll
       for (int i = 0; i < HD / 32; ++i) {
-        const bool there = i * (512 / HD) + lane / (HD / 16) < left;
+        const int row = i * (512 / HD) + lane / (HD / 16);
+        const bool there = row < left && (slice << 4) + row >= first;
         const size_t off = there ? from + i * 512 : from;
         copy16_some(key_to + at + i * 512, keys_at + off, there ? 16 : 0);
         if (with_values) copy16_some((i & 1 ? value_odd : value_to) + at + i * 512, values_at + off, there ? 16 : 0);
@@ -660,6 +661,11 @@ int launch_tiles(const QAttendArgs& a, cudaStream_t s) {
 template <typename T, int HD>
 int launch_hd(const QAttendArgs& a, cudaStream_t s) {
   const int rows = a.n_rows * (a.n_heads / a.c.n_heads);
+  // Many rows of bf16 contexts: the kernel with 128 of them a tile.  Two trees of 27 rows x 4 heads behind 31K keys 80 us against 158 here (four
+  // tiles of 32 rows turn every key four times); 36 rows 75 against 101.  Up to 32 rows only where its items are on the device at once: 20
+  // rows, 300 to 500 keys, 140 items 13.0 us against 15.2, 160 items 20.6 against 18.2.  (Rows by 2^32 / share: exact up to 2^20 rows of 4096 heads.)
+  const long long items = (long long)a.c.n_seqs * a.c.n_heads;
+  if (sizeof(T) == 2 && a.mass_rows == 0 && rows / a.n_rows <= 4096 && (rows > 32 || (rows > 16 && items <= a.n_sms))) return launch_quant_attend_rows(a, s);
   return rows <= 16 ? launch_tiles<T, HD, 1>(a, s) : launch_tiles<T, HD, 2>(a, s);
 }
 
