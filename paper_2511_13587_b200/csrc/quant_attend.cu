@@ -7,8 +7,8 @@
 // bf16 elements lose nothing but what is 2^-28 of the row's largest.  e4m3 codes are halves exactly.  Float32 contexts split a query
 // into three halves and a weight into two (33 and 22 bits).
 //
-// One pass over the cache.  A (sequence, cached head, tile of rows) is an item of a cluster of CTAs, each of them with a share of the
-// keys; a warp has slices of 16 keys of its own, brought by 16-byte asynchronous copies into a ring of its own, so no barrier is
+// One pass over the cache.  A (sequence, cached head, tile of rows) is an item of a cluster of CTAs, of four warps or of as many as an SM
+// holds, each of them with a share of the keys; a warp has slices of 16 keys of its own, brought by 16-byte asynchronous copies into a ring of its own, so no barrier is
 // met before the warps' sums are joined: in shared memory first, then over the cluster through distributed shared memory, in rank order.
 // Query rows (rows x query heads of the cached head) are the M side of mma.sync m16n8k16.  The order of a head's elements along K of the
 // first product, and of the output's columns, is the one in which a lane's codes lie side by side in memory: a 16-byte load of a
@@ -24,13 +24,10 @@ namespace vvs {
 
 namespace {
 
-constexpr int kWarps = 4;
-constexpr int kThreads = 32 * kWarps;
 // The reference m of a row moves only when a score passes it by more than kSlack: weights are 2^kShift at the reference, 2^15 at most, and
 // halves keep 11 bits down to 2^-21 of the reference's.  After a row's first slices its sums are hardly ever scaled again, and no lane
 // has to ask the others for their largest score.
 constexpr float kShift = 7.f, kSlack = 8.f;
-constexpr int kScoreBytes = 40 * 1024;          // of a CTA's shared memory for scores of rows whose weights are summed
 constexpr float kLog2e = 1.4426950408889634f;
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t* a, uint32_t b0, uint32_t b1) {
@@ -77,7 +74,7 @@ __device__ __forceinline__ float lds32(uint32_t at) {
   return v;
 }
 
-template <int HD, int MT, bool F32>
+template <int HD, int MT, bool F32, bool WIDE>
 struct Layout {
   static constexpr int kRows = 16 * MT;
   static constexpr int kSteps = HD / 16;                                    // k-steps of the first product
@@ -91,6 +88,10 @@ struct Layout {
   static constexpr int kPartBytes = kRows * HD * 4;                         // a warp's sums, over its own ring
   static_assert(kPartBytes <= kRing, "a warp's sums take the place of its ring");
   static constexpr int kQAt = 0;
+  // CTAs an SM holds by registers: 64 sums of a lane for heads of 128, twice as many for two tiles of rows.  A wide CTA has all of their warps.
+  static constexpr int kFit = MT * HD == 256 ? 2 : MT * HD == 128 ? (F32 ? 2 : 3) : 4;
+  static constexpr int kWarps = WIDE ? 4 * kFit : 4, kThreads = 32 * kWarps, kCtas = WIDE ? 1 : kFit;
+  static constexpr int kScoreBytes = (WIDE ? 56 : 40) * 1024;               // at most, for scores of rows whose weights are summed
   static constexpr int kRingAt = kQBytes;
   static constexpr int kMlAt = kRingAt + kWarps * kRing;                    // [kWarps][kRows][2] warps' maxima and sums
   static constexpr int kTotAt = kMlAt + kWarps * kRows * 8;                 // [kRows][2] the CTA's
@@ -100,8 +101,7 @@ struct Layout {
   static constexpr int kBytes = kScoreAt;
   // query fragments stay in registers where they are at most 32 of them
   static constexpr bool kQRegs = kQ * MT * kSteps * 4 <= 32;
-  // CTAs an SM holds by registers: 64 sums of a lane for heads of 128, twice as many for two tiles of rows
-  static constexpr int kCtas = MT * HD == 256 ? 2 : MT * HD == 128 ? (F32 ? 2 : 3) : 4;
+  static_assert(kCtas * (kBytes + 1024) <= 228 * 1024 && kBytes + kScoreBytes <= 227 * 1024, "shared memory");
 };
 
 // where 16 bytes `chunk` of key `row` lie in a slice's tile, so that what the eight lanes of a quarter warp load lies in different banks
@@ -115,11 +115,11 @@ __device__ __forceinline__ uint32_t value_at(int row, int chunk) {
   return (row >> 1) * 128 + (((((row & 1) << 2) | chunk) ^ (row & 6)) << 4);
 }
 
-template <typename T, int HD, int MT>
-__global__ void __launch_bounds__(kThreads, Layout<HD, MT, sizeof(T) == 4>::kCtas) quant_attend_kernel(QAttendArgs a, int tiles_each, int score_bytes) {
+template <typename T, int HD, int MT, bool WIDE>
+__global__ void __launch_bounds__(Layout<HD, MT, sizeof(T) == 4, WIDE>::kThreads, Layout<HD, MT, sizeof(T) == 4, WIDE>::kCtas) quant_attend_kernel(QAttendArgs a, int tiles_each, int score_bytes) {
   constexpr bool F32 = sizeof(T) == 4;
-  using L = Layout<HD, MT, F32>;
-  constexpr int kDepth = L::kDepth;
+  using L = Layout<HD, MT, F32, WIDE>;
+  constexpr int kDepth = L::kDepth, kWarps = L::kWarps, kThreads = L::kThreads;
   extern __shared__ __align__(128) uint8_t smem[];
   const uint32_t sbase = tc::smem_u32(smem);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
@@ -622,29 +622,22 @@ __global__ void __launch_bounds__(kThreads, Layout<HD, MT, sizeof(T) == 4>::kCta
   }
 }
 
-template <typename T, int HD, int MT>
-int launch_tiles(const QAttendArgs& a, cudaStream_t s) {
-  using L = Layout<HD, MT, sizeof(T) == 4>;
-  const int rows = a.n_rows * (a.n_heads / a.c.n_heads), tiles = (rows + L::kRows - 1) / L::kRows;
-  // the weights' sums of a key are added by one thread: a CTA goes through all tiles of rows then
-  const int tiles_each = a.mass_rows > 0 ? tiles : 1, groups = (tiles + tiles_each - 1) / tiles_each;
-  const long long items = (long long)a.c.n_seqs * a.c.n_heads * groups;
-  const int slices = ((a.max_len > 0 && a.max_len < a.c.cap ? a.max_len : a.c.cap) + 15) / 16;
-  int ranks = 1;
-  while (ranks < 16 && items * ranks * 2 <= 2LL * a.n_sms && slices >= 2 * ranks * kWarps) ranks *= 2;
-  // shared memory for the scores of summed rows, where all of a CTA's keys fit (a call that says less of its lengths than they are walks
+template <typename T, int HD, int MT, bool WIDE>
+int launch_kernel_of(const QAttendArgs& a, int tiles_each, int groups, int ranks, int slices, cudaStream_t s) {
+  using L = Layout<HD, MT, sizeof(T) == 4, WIDE>;
+  // Shared memory for the scores of summed rows, where all of a CTA's keys fit (a call that says less of its lengths than they are walks
   // the keys again).  More ranks than the device has room for, to make them fit, cost more than the second walk: 32 sequences of nine
   // rows behind 900 to 2380 keys 179 us so, 347 with sixteen ranks in the place of one.
   const int mass_rows = a.mass_rows < a.n_rows ? a.mass_rows : a.n_rows, share = a.n_heads / a.c.n_heads;
   const long long summed = (long long)mass_rows * share < L::kRows ? mass_rows * share : L::kRows;
   const long long want = summed * ((((slices + ranks - 1) / ranks * 16 + 23) / 32) * 32 + 8) * 4;
-  const int score_bytes = want <= kScoreBytes ? (int)want : 0;
-  auto kernel = quant_attend_kernel<T, HD, MT>;
-  if (ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), L::kBytes + kScoreBytes) != cudaSuccess) return VVS_ERR_CUDA;
+  const int score_bytes = want <= L::kScoreBytes ? (int)want : 0;
+  auto kernel = quant_attend_kernel<T, HD, MT, WIDE>;
+  if (ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), L::kBytes + L::kScoreBytes) != cudaSuccess) return VVS_ERR_CUDA;
   if (ranks > 8 && cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return VVS_ERR_CUDA;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(ranks, a.c.n_heads * groups, a.c.n_seqs);
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(L::kThreads);
   cfg.dynamicSmemBytes = L::kBytes + score_bytes;
   cfg.stream = s;
   cudaLaunchAttribute attr[2];
@@ -656,6 +649,34 @@ int launch_tiles(const QAttendArgs& a, cudaStream_t s) {
   cfg.attrs = attr;
   cfg.numAttrs = 2;
   return cudaLaunchKernelEx(&cfg, kernel, a, tiles_each, score_bytes) == cudaSuccess ? VVS_OK : VVS_ERR_CUDA;
+}
+
+template <typename T, int HD, int MT>
+int launch_tiles(const QAttendArgs& a, cudaStream_t s) {
+  using L = Layout<HD, MT, sizeof(T) == 4, false>;
+  using W = Layout<HD, MT, sizeof(T) == 4, true>;
+  const int rows = a.n_rows * (a.n_heads / a.c.n_heads), tiles = (rows + L::kRows - 1) / L::kRows;
+  // the weights' sums of a key are added by one thread: a CTA goes through all tiles of rows then
+  const int tiles_each = a.mass_rows > 0 ? tiles : 1, groups = (tiles + tiles_each - 1) / tiles_each;
+  const long long items = (long long)a.c.n_seqs * a.c.n_heads * groups;
+  const int slices = ((a.max_len > 0 && a.max_len < a.c.cap ? a.max_len : a.c.cap) + 15) / 16;
+  int ranks = 1;
+  while (ranks < 16 && items * ranks * 2 <= 2LL * a.n_sms && slices >= 2 * ranks * L::kWarps) ranks *= 2;
+  // Items that the device holds at once: CTAs that fill an SM, as many for an item as lets all items be there together, where an item gets as
+  // many warps so.  A token behind 31K keys: 8 cached heads of 128 43.4 -> 30.0 us, 4 of 64 29.0 -> 13.8; 40 of 64 behind 3K keys 16.3 -> 10.1,
+  // nine rows behind 311 11.4 -> 9.5 (the same number of warps, no cluster).  A slice is enough for a warp: with two at least, a token behind
+  // 900 keys of 16 cached heads of 128 takes 12.1 instead of 10.7.
+  if (items <= a.n_sms && slices >= W::kWarps) {
+    auto kernel = quant_attend_kernel<T, HD, MT, true>;
+    if (ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), W::kBytes + W::kScoreBytes) != cudaSuccess) return VVS_ERR_CUDA;
+    const int* there = resident_clusters(reinterpret_cast<const void*>(kernel), W::kThreads, W::kBytes + W::kScoreBytes);
+    if (!there) return VVS_ERR_CUDA;
+    int wide = 0;
+    for (int c = 1; c <= kMaxCluster && slices >= c * W::kWarps; ++c)
+      if (there[c] >= items) wide = c;
+    if (wide > 0 && wide * W::kWarps >= ranks * L::kWarps) return launch_kernel_of<T, HD, MT, true>(a, tiles_each, groups, wide, slices, s);
+  }
+  return launch_kernel_of<T, HD, MT, false>(a, tiles_each, groups, ranks, slices, s);
 }
 
 template <typename T, int HD>

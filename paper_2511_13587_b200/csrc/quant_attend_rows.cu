@@ -2,7 +2,7 @@
 //
 // The mathematics is that of the kernel for few rows: out = (sum_j w_j cv_j) / (sum_j w_j / V_b), w_j = 2^(a_j - m), queries as halves
 // times a power of two, weights as halves.  A row's reference m moves only when its weights of a tile add up to more than kMost, so that
-// none of them is beyond it: a product with one more row of ones would be the same sum, but a lane has its row's weights anyway.
+// none of them is beyond it: a sum costs less than a maximum beside it.
 //
 // A stream has a tile of 128 rows and a share of the keys, 64 at a time.  Codes arrive by bulk copies.  Two warps turn the keys' into halves,
 // two the values', in the 128-byte swizzled layout of the operands (keys K-major; values, as the same rows, MN-major), and issue
@@ -16,8 +16,6 @@
 // for another; an SM issues in 47 of 100 cycles, its tensor pipe is busy in 27.  Clusters of six CTAs with an SM each are what the
 // device holds for 16 items at once: 96 of 148 SMs work (eight: 15 clusters, one waits for another to end, 124 us).  One CTA with one stream,
 // twice on an SM, is packed on half of the SMs: 135 us.
-#include <map>
-#include <mutex>
 #include <type_traits>
 
 #include "quant_cache.cuh"
@@ -546,28 +544,6 @@ __global__ void __launch_bounds__(kThreads, Layout<HD>::kCtas) quant_attend_rows
   if (tid < 32) tc::tmem_dealloc(*tmem_slot, L::kColumns);
 }
 
-// clusters of 2 .. kMaxRanks CTAs that the device holds at once; null: an error
-const int* resident_clusters(const void* kernel, cudaLaunchConfig_t cfg, cudaLaunchAttribute* attr) {
-  struct Counts { int there[kMaxRanks + 1]; };
-  static std::mutex mu;
-  static std::map<std::pair<int, const void*>, Counts> known;
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return nullptr;
-  std::lock_guard<std::mutex> lock(mu);
-  const auto key = std::make_pair(dev, kernel);
-  const auto it = known.find(key);
-  if (it != known.end()) return it->second.there;
-  Counts got{};
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return nullptr;
-  cfg.numAttrs = 1;
-  for (int c = 2; c <= kMaxRanks; ++c) {
-    attr[0].val.clusterDim.x = c;
-    cfg.gridDim = dim3(c);
-    if (cudaOccupancyMaxActiveClusters(&got.there[c], kernel, &cfg) != cudaSuccess) return nullptr;
-  }
-  return known.emplace(key, got).first->second.there;
-}
-
 template <int HD>
 int launch_hd(const QAttendArgs& a, cudaStream_t s) {
   using L = Layout<HD>;
@@ -588,7 +564,7 @@ int launch_hd(const QAttendArgs& a, cudaStream_t s) {
   attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  const int* there = resident_clusters(reinterpret_cast<const void*>(kernel), cfg, attr);
+  const int* there = resident_clusters(reinterpret_cast<const void*>(kernel), kThreads, L::kBytes);
   if (!there) return VVS_ERR_CUDA;
   // the most CTAs for an item by which all items are there at once: a cluster more than that waits until another one has ended
   int ranks = 1;

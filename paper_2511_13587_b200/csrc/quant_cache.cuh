@@ -6,6 +6,9 @@
 #include <cuda_fp16.h>
 #include <math_constants.h>
 
+#include <map>
+#include <mutex>
+
 #include "vvs_internal.cuh"
 
 namespace vvs {
@@ -77,6 +80,37 @@ struct QEvictArgs {
   int n_sms;
 };
 int launch_quant_evict(const QEvictArgs& a, cudaStream_t s);
+
+// Clusters of 1 .. 16 CTAs of a kernel that the device holds at once, by their CTAs; null: an error.  A cluster's CTAs lie in one group
+// of SMs: of CTAs that fill an SM, the device may hold 33 clusters of four, 15 of eight, 7 of sixteen.
+constexpr int kMaxCluster = 16;
+inline const int* resident_clusters(const void* kernel, int threads, int dynamic_smem) {
+  struct Counts { int there[kMaxCluster + 1]; };
+  static std::mutex mu;
+  static std::map<std::pair<int, const void*>, Counts> known;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return nullptr;
+  std::lock_guard<std::mutex> lock(mu);
+  const auto key = std::make_pair(dev, kernel);
+  const auto it = known.find(key);
+  if (it != known.end()) return it->second.there;
+  Counts got{};
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return nullptr;
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = dynamic_smem;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  for (int c = 1; c <= kMaxCluster; ++c) {
+    attr[0].val.clusterDim.x = c;
+    cfg.gridDim = dim3(c);
+    if (cudaOccupancyMaxActiveClusters(&got.there[c], kernel, &cfg) != cudaSuccess) return nullptr;
+  }
+  return known.emplace(key, got).first->second.there;
+}
 
 // ---- eight values of a row, 16 bytes of bf16 or 32 of float32; or two groups of four -----------------------------------
 __device__ __forceinline__ uint32_t pack_bf16x2(float a, float b) {
