@@ -8,13 +8,21 @@
 // into three halves and a weight into two (33 and 22 bits).
 //
 // One pass over the cache.  A (sequence, cached head, tile of rows) is an item of a cluster of CTAs, of four warps or of as many as an SM
-// holds, each of them with a share of the keys; a warp has slices of 16 keys of its own, brought by 16-byte asynchronous copies into a ring of its own, so no barrier is
-// met before the warps' sums are joined: in shared memory first, then over the cluster through distributed shared memory, in rank order.
+// holds, each of them with a share of the keys; a warp has slices of 16 keys of its own, brought by 16-byte asynchronous copies into a ring
+// of its own, so no barrier is met before the warps' sums are joined: in shared memory first, then over the cluster through distributed
+// shared memory, in rank order.
 // Query rows (rows x query heads of the cached head) are the M side of mma.sync m16n8k16.  The order of a head's elements along K of the
 // first product, and of the output's columns, is the one in which a lane's codes lie side by side in memory: a 16-byte load of a
 // lane is four (keys) or eight (values) operands.
 //
-// The weights' sums need the whole row's maximum and sum: a second walk over the CTA's keys (from L2) with both at hand.
+// The weights' sums need the whole row's maximum and sum: from the scores, kept in shared memory, where those of the CTA's keys fit, else by a
+// second walk over the CTA's keys (from L2).
+//
+// 32 sequences of nine rows behind 900 to 2380 keys, 32 heads of 128: 118 us, 3.8 TB/s, 59 % of a copy's rate.  Every key is turned to halves
+// by the warp that multiplies it, for 16 rows of which nine are there: a slice takes a warp 3400 cycles beside eleven others on its SM,
+// conversions, the two products and the weights in one chain.  Left out, measured: slices of 32 keys (116 where 16 took 107), rings of two, four
+// and five slices (108 and more), eight warps a CTA (138), keys as 8-bit operands of mma.sync (131).  One token of a float32 context: 7 us, the
+// call itself 6; nine rows behind 311 keys, weights summed: 9.5.
 #include <type_traits>
 
 #include "quant_cache.cuh"
@@ -116,7 +124,8 @@ __device__ __forceinline__ uint32_t value_at(int row, int chunk) {
 }
 
 template <typename T, int HD, int MT, bool WIDE>
-__global__ void __launch_bounds__(Layout<HD, MT, sizeof(T) == 4, WIDE>::kThreads, Layout<HD, MT, sizeof(T) == 4, WIDE>::kCtas) quant_attend_kernel(QAttendArgs a, int tiles_each, int score_bytes) {
+__global__ void __launch_bounds__(Layout<HD, MT, sizeof(T) == 4, WIDE>::kThreads, Layout<HD, MT, sizeof(T) == 4, WIDE>::kCtas)
+quant_attend_kernel(QAttendArgs a, int tiles_each, int score_bytes) {
   constexpr bool F32 = sizeof(T) == 4;
   using L = Layout<HD, MT, F32, WIDE>;
   constexpr int kDepth = L::kDepth, kWarps = L::kWarps, kThreads = L::kThreads;
@@ -686,7 +695,8 @@ int launch_hd(const QAttendArgs& a, cudaStream_t s) {
   // tiles of 32 rows turn every key four times); 36 rows 75 against 101.  Up to 32 rows only where its items are on the device at once: 20
   // rows, 300 to 500 keys, 140 items 13.0 us against 15.2, 160 items 20.6 against 18.2.  (Rows by 2^32 / share: exact up to 2^20 rows of 4096 heads.)
   const long long items = (long long)a.c.n_seqs * a.c.n_heads;
-  if (sizeof(T) == 2 && a.mass_rows == 0 && rows / a.n_rows <= 4096 && (rows > 32 || (rows > 16 && items <= a.n_sms))) return launch_quant_attend_rows(a, s);
+  if (sizeof(T) == 2 && a.mass_rows == 0 && rows / a.n_rows <= 4096 && (rows > 32 || (rows > 16 && items <= a.n_sms)))
+    return launch_quant_attend_rows(a, s);
   return rows <= 16 ? launch_tiles<T, HD, 1>(a, s) : launch_tiles<T, HD, 2>(a, s);
 }
 

@@ -58,6 +58,9 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
+__device__ __forceinline__ uint4 halves_of(uint32_t a, uint32_t b) {
+  return make_uint4(from_e4m3x2(a), from_e4m3x2(a >> 16), from_e4m3x2(b), from_e4m3x2(b >> 16));
+}
 // bytes side by side, 16-byte aligned, counted on a barrier
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint64_t* bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
@@ -231,7 +234,8 @@ __global__ void __launch_bounds__(kThreads, Layout<HD>::kCtas) quant_attend_rows
     for (int m = 0; m < kBatch; ++m) {
       top[m] = 0.f;
 #pragma unroll
-      for (int e = 0; e < kEach / 2; ++e) top[m] = fmaxf(top[m], fmaxf(fabsf(__uint_as_float(raw[m][e] << 16)), fabsf(__uint_as_float(raw[m][e] & 0xffff0000u))));
+      for (int e = 0; e < kEach / 2; ++e)
+        top[m] = fmaxf(top[m], fmaxf(fabsf(__uint_as_float(raw[m][e] << 16)), fabsf(__uint_as_float(raw[m][e] & 0xffff0000u))));
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1)
@@ -265,7 +269,8 @@ __global__ void __launch_bounds__(kThreads, Layout<HD>::kCtas) quant_attend_rows
     const int row = HD == 128 ? at / 16 * 2 + ((at >> 2) & 1) : at / kPieces;
     const int piece = HD == 128 ? (((at >> 2) ^ (at >> 3)) & 1) * 4 + (at & 3) : at % kPieces;
     uint8_t* to = smem + stream_at + (of_keys ? 0 : L::kValueAt) + (piece >> 2) * L::kSlab + row * 128;
-    uint8_t *to_lo = to + (((2 * (piece & 3)) ^ (row & 7)) << 4), *to_hi = to + (((2 * (piece & 3) + 1) ^ (row & 7)) << 4);     // (kRowsEach is a multiple of 8)
+    // (kRowsEach is a multiple of 8)
+    uint8_t *to_lo = to + (((2 * (piece & 3)) ^ (row & 7)) << 4), *to_hi = to + (((2 * (piece & 3) + 1) ^ (row & 7)) << 4);
     const bool issues = warp == (of_keys ? kSoft : kSoft + kConv / 2);
     int i = 0;
 #pragma unroll 1
@@ -274,7 +279,8 @@ __global__ void __launch_bounds__(kThreads, Layout<HD>::kCtas) quant_attend_rows
       ok = ok && tc::warp_wait_or_abort(&full[st], (i / kStages) & 1, abort_flag);
       uint4 w[kTimes];
 #pragma unroll
-      for (int x = 0; x < kTimes; ++x) w[x] = *reinterpret_cast<const uint4*>(smem + code_at + st * L::kCodes + (x * kRowsEach + row) * HD + piece * 16);
+      for (int x = 0; x < kTimes; ++x)
+        w[x] = *reinterpret_cast<const uint4*>(smem + code_at + st * L::kCodes + (x * kRowsEach + row) * HD + piece * 16);
       if (!of_keys && (slot0 < first || slot0 + kKeys > end)) {
         // values of slots that no row sees are zeros, whatever lies there
 #pragma unroll
@@ -289,8 +295,8 @@ __global__ void __launch_bounds__(kThreads, Layout<HD>::kCtas) quant_attend_rows
                             : tc::warp_wait_or_abort(&o_done[(i - 1) & 1], ((i - 1) >> 1) & 1, abort_flag));
 #pragma unroll
       for (int x = 0; x < kTimes; ++x) {
-        *reinterpret_cast<uint4*>(to_lo + x * kRowsEach * 128) = make_uint4(from_e4m3x2(w[x].x), from_e4m3x2(w[x].x >> 16), from_e4m3x2(w[x].y), from_e4m3x2(w[x].y >> 16));
-        *reinterpret_cast<uint4*>(to_hi + x * kRowsEach * 128) = make_uint4(from_e4m3x2(w[x].z), from_e4m3x2(w[x].z >> 16), from_e4m3x2(w[x].w), from_e4m3x2(w[x].w >> 16));
+        *reinterpret_cast<uint4*>(to_lo + x * kRowsEach * 128) = halves_of(w[x].x, w[x].y);
+        *reinterpret_cast<uint4*>(to_hi + x * kRowsEach * 128) = halves_of(w[x].z, w[x].w);
       }
       tc::fence_proxy_async();
       // both warps have the same answer, whether to go on: one that gave up comes to this barrier all the same
@@ -306,7 +312,8 @@ __global__ void __launch_bounds__(kThreads, Layout<HD>::kCtas) quant_attend_rows
         constexpr uint32_t idesc = (1u << 4) | ((kKeys >> 3) << 17) | ((kRows >> 4) << 24);
 #pragma unroll
         for (int h = 0; h < HD / 64; ++h)
-          tc::mma_bf16_k64(tmem + (i & 1) * kKeys, tc::desc_lo_sw128(sbase + L::kQAt + h * (kRows * 128)), tc::desc_lo_sw128(sbase + stream_at + h * L::kSlab), idesc, h);
+          tc::mma_bf16_k64(tmem + (i & 1) * kKeys, tc::desc_lo_sw128(sbase + L::kQAt + h * (kRows * 128)),
+                           tc::desc_lo_sw128(sbase + stream_at + h * L::kSlab), idesc, h);      // (the descriptor's types are halves)
         tc::mma_commit_elect(&s_full[i & 1]);
       } else {
         ok = tc::warp_wait_or_abort(&p_full[i & 1], (i >> 1) & 1, abort_flag);

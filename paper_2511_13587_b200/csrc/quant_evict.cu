@@ -1,12 +1,16 @@
 // Eviction from the 8-bit cache by accumulated attention weight: selection of what stays, then the moves.
 //
 // Selection, a cluster of CTAs for a head, each with a range of its slots: order-preserving 32-bit keys of the weights in shared memory (a
-// guarded token's key is above every weight's); the keep-th largest digit by digit,
-// histograms summed over the ranks; a bitmap
-// of what stays, the lower slots first among equals; free slots below `keep` and movers behind it counted, and matched through a list.
+// guarded token's key is above every weight's); the keep-th largest digit by digit, histograms summed over the ranks; a bitmap of what
+// stays, the lower slots first among equals; free slots below `keep` and movers behind it counted, and matched through a list.
 // Moves: what stays in slots behind `keep` goes, in order, into the slots below that became free, one CTA for a block of target slots.
 // Sources and targets never overlap, so only what fills a hole is read and written; the one block that holds both, where `keep` lies, is
 // left to a last launch.
+//
+// 32 heads of 128, 32K slots of which 24.6K stay: 82 us.  The selection is 32 of them (three passes over 8192 keys in shared memory, the
+// barriers of four ranks between them); the moves 49, for 150 MB of rows that fill holes and 250 MB of rows that are rounded again because
+// their block's scale grew: nearly every block takes in some row of a larger scale.  40 heads of 640 slots: 11 us, two launches of some
+// round trips each.
 #include "quant_cache.cuh"
 #include "tc_common.cuh"
 
@@ -54,7 +58,7 @@ __device__ __forceinline__ int scan_exclusive(int v, int* warp_sums, int* total)
 constexpr int kMaxRanks = 8;
 constexpr int kTogether = 4;                                   // slots of a thread whose weights travel together
 
-// FEW slots: one CTA, digits of 8 bits, four histograms.  Otherwise 1024 threads of one or several CTAs and digits of 11 bits, three
+// FEW threads: one CTA, digits of 8 bits, four histograms.  Otherwise 1024 threads of one or several CTAs and digits of 11 bits, three
 // histograms: of 8 bits, so many threads would add to the handful of bins that weights' exponents are that the adding costs more.
 template <bool FEW>
 __global__ void __launch_bounds__(1024) quant_select_kernel(QEvictArgs a, int slots_each) {
@@ -395,12 +399,14 @@ int launch_quant_evict(const QEvictArgs& a, cudaStream_t s) {
   while (ranks < kMaxRanks && (a.c.cap > 16384 * ranks || (items * ranks * 2 <= a.n_sms && a.c.cap >= 8192 * ranks))) ranks *= 2;
   const int slots = ((a.c.cap + ranks - 1) / ranks + 31) / 32 * 32;
   const size_t smem = (size_t)slots * 4 + (size_t)slots / 32 * 8;
-  const bool few = ranks == 1 && slots <= 2048;
+  // Heads that have an SM each are selected by 1024 threads, more heads by CTAs of fewer threads, several on an SM: 40 heads of 640 slots 11.2
+  // us against 13.9, 640 heads 52 against 28; 160 heads of 2048 slots 34 against 27, of 8192 slots 83 against 80.
+  const bool few = ranks == 1 && items > a.n_sms && slots <= 8192;
   auto select = few ? quant_select_kernel<true> : quant_select_kernel<false>;
   if (ensure_dynamic_smem(reinterpret_cast<const void*>(select), (int)smem) != cudaSuccess) return VVS_ERR_CUDA;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(ranks, a.c.n_heads, a.c.n_seqs);
-  cfg.blockDim = dim3(!few ? 1024 : slots <= 1024 ? 256 : 512);
+  cfg.blockDim = dim3(!few ? 1024 : slots <= 1024 && items > 2LL * a.n_sms ? 256 : 512);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
   cudaLaunchAttribute attr[2];
