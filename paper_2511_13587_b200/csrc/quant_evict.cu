@@ -3,14 +3,14 @@
 // Selection, a cluster of CTAs for a head, each with a range of its slots: order-preserving 32-bit keys of the weights in shared memory (a
 // guarded token's key is above every weight's); the keep-th largest digit by digit, histograms summed over the ranks; a bitmap of what
 // stays, the lower slots first among equals; free slots below `keep` and movers behind it counted, and matched through a list.
-// Moves: what stays in slots behind `keep` goes, in order, into the slots below that became free, one CTA for a block of target slots.
+// Moves: what stays in slots behind `keep` goes, in order, into the slots below that became free.
 // Sources and targets never overlap, so only what fills a hole is read and written; the one block that holds both, where `keep` lies, is
 // left to a last launch.
 //
-// 32 heads of 128, 32K slots of which 24.6K stay: 82 us.  The selection is 32 of them (three passes over 8192 keys in shared memory, the
-// barriers of four ranks between them); the moves 49, for 150 MB of rows that fill holes and 250 MB of rows that are rounded again because
-// their block's scale grew: nearly every block takes in some row of a larger scale.  40 heads of 640 slots: 11 us, two launches of some
-// round trips each.
+// 32 heads of 128, 32K slots of which 24.6K stay, scales that grow no more: 67 us for 98 MB of rows that fill holes (15 us at a copy's rate).  The
+// selection is 32 of them: three passes over 8192 keys in shared memory, and the barriers of four ranks between them.  The moves, 128 slots a
+// CTA, are a chain of four round trips each.  With a CTA for a block, keys and values in turn, 82, and 214 where blocks are of 16 slots
+// (68 now).  40 heads of 640 slots: 10 us, two launches of some round trips each.
 #include "quant_cache.cuh"
 #include "tc_common.cuh"
 
@@ -320,71 +320,75 @@ __global__ void __launch_bounds__(1024) quant_select_kernel(QEvictArgs a, int sl
   if (ranks > 1) tc::cluster_sync();                           // (a rank's counts are read until here)
 }
 
-// One block of target slots: new scales from the old ones, rows that come in or are rounded again into registers, and back once all are read.
-// A block where `keep` lies has sources of its own rows too, and its rows behind keep go with its scale: it is done when all others are.
+// The blocks of 128 target slots below `end`, their keys or their values: new scales from the old ones, rows that come in or are rounded again
+// through a list, so that no thread is left without one, into registers, and back once all are read.  The block where `keep` lies
+// has sources of its own rows too, and its rows behind keep go with its scale: it is done when all others are.
 template <int HD>
-__global__ void __launch_bounds__(256) quant_move_kernel(QEvictArgs a, int block0) {
-  constexpr int kChunks = HD / 16, kMine = 128 * kChunks / 256;              // 16-byte pieces of a row; of a thread, in blocks of 128
-  __shared__ int from_of[128];
-  __shared__ float top[2][4];
+__global__ void __launch_bounds__(256) quant_move_kernel(QEvictArgs a, int begin, int end) {
+  constexpr int kChunks = HD / 16, kMine = 128 * kChunks / 256;              // 16-byte pieces of a row; of a thread
+  __shared__ int from_of[128], list[128];
+  __shared__ float factor_of[128], top[4];
+  __shared__ uint32_t touched[4];
   grid_dep_launch();
   grid_dep_wait();
-  const int tid = threadIdx.x, b = block0 + blockIdx.x, head = blockIdx.y, seq = blockIdx.z;
+  const int tid = threadIdx.x, d0 = begin + 128 * (blockIdx.x / 2), head = blockIdx.y, seq = blockIdx.z;
   const int len = a.cache_len[seq], keep = a.keep, blk_log2 = a.c.block_log2, blk = 1 << blk_log2;
   if (len <= keep || len > a.c.cap) return;
-  const size_t item = (size_t)seq * a.c.n_heads + head, scale_row = item * (a.c.cap >> blk_log2);
-  const int d0 = b << blk_log2;
-  float ks = 0.f, vs = 0.f;
-  bool moved = false;
-  if (tid < 128) {
-    const int d = d0 + tid;
-    int from = d;
-    if (tid < blk && d < keep) from = a.kept[item * keep + d];
-    from_of[tid] = from;
-    if (from != d) {
-      moved = true;
-      ks = a.c.k_scale[scale_row + (from >> blk_log2)];
-      vs = a.c.v_scale[scale_row + (from >> blk_log2)];
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      ks = fmaxf(ks, __shfl_xor_sync(0xffffffffu, ks, o));
-      vs = fmaxf(vs, __shfl_xor_sync(0xffffffffu, vs, o));
-    }
-    if (tid % 32 == 0) {
-      top[0][tid / 32] = ks;
-      top[1][tid / 32] = vs;
-    }
+  const bool keys = blockIdx.x % 2 == 0;
+  const size_t item = (size_t)seq * a.c.n_heads + head;
+  float* scales = (keys ? a.c.k_scale : a.c.v_scale) + item * (a.c.cap >> blk_log2);
+  uint4* rows = reinterpret_cast<uint4*>((keys ? a.c.k : a.c.v) + item * a.c.cap * HD);
+  // of each slot: where its row comes from, and the scale there
+  const int d = d0 + tid;
+  const bool mine = tid < 128 && d < end;
+  int from = d;
+  if (mine && d < keep) from = a.kept[item * keep + d];
+  const bool moved = from != d;
+  float old = 0.f, there = 0.f;
+  if (mine) {
+    old = scales[d >> blk_log2];
+    if (moved) there = scales[from >> blk_log2];
   }
+  float most = there;                                          // of the rows that come into the slot's block
+  for (int o = blk < 32 ? blk >> 1 : 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+  if (tid < 128 && tid % 32 == 0) top[tid / 32] = most;
   if (!__syncthreads_or(moved)) return;
+  if (tid < 128) {
+    for (int w = 0; w < 4; ++w)
+      if (blk > 32 && ((w * 32) ^ tid) < blk) most = fmaxf(most, top[w]);
+    const float now = fmaxf(most, old), grown = old / now;
+    const uint32_t mask = __ballot_sync(0xffffffffu, mine && (moved || grown != 1.f));
+    if (tid % 32 == 0) touched[tid / 32] = mask;
+    from_of[tid] = from;
+    factor_of[tid] = moved ? there / now : grown;
+    if (mine && (tid & (blk - 1)) == 0) scales[d >> blk_log2] = now;
+  }
+  __syncthreads();
+  int n = 0;
 #pragma unroll
-  for (int kv = 0; kv < 2; ++kv) {
-    float* scales = (kv ? a.c.v_scale : a.c.k_scale) + scale_row;
-    const float old = scales[b], now = fmaxf(fmaxf(fmaxf(top[kv][0], top[kv][1]), fmaxf(top[kv][2], top[kv][3])), old), grown = old / now;
-    uint4* rows = reinterpret_cast<uint4*>((kv ? a.c.v : a.c.k) + item * a.c.cap * HD);
-    uint4 v[kMine];
-    float f[kMine];
+  for (int w = 0; w < 4; ++w) {
+    const uint32_t mask = touched[w];
+    if (tid / 32 == w && (mask >> (tid % 32)) & 1u) list[n + __popc(mask & ((1u << (tid % 32)) - 1u))] = tid;
+    n += __popc(mask);
+  }
+  __syncthreads();
+  uint4 v[kMine];
 #pragma unroll
-    for (int j = 0; j < kMine; ++j) {
-      const int i = tid + j * 256, r = i / kChunks;
-      f[j] = -1.f;                                             // nothing to write
-      if (r >= blk) continue;
-      const int from = from_of[r];
-      const bool stays = from == d0 + r;
-      f[j] = stays ? grown : scales[from >> blk_log2] / now;
-      if (stays && grown == 1.f) f[j] = -1.f;
-      else v[j] = rows[(size_t)from * kChunks + i % kChunks];
-    }
-    __syncthreads();
+  for (int j = 0; j < kMine; ++j) {
+    const int i = tid + j * 256;
+    if (i >= n * kChunks) break;
+    v[j] = rows[(size_t)from_of[list[i / kChunks]] * kChunks + i % kChunks];
+  }
+  __syncthreads();
 #pragma unroll
-    for (int j = 0; j < kMine; ++j) {
-      const int i = tid + j * 256;
-      if (f[j] < 0.f) continue;
-      uint4 x = v[j];
-      if (f[j] != 1.f) x = make_uint4(rescale_e4m3x4(x.x, f[j]), rescale_e4m3x4(x.y, f[j]), rescale_e4m3x4(x.z, f[j]), rescale_e4m3x4(x.w, f[j]));
-      rows[(size_t)(d0 + i / kChunks) * kChunks + i % kChunks] = x;
-    }
-    if (tid == 0) scales[b] = now;
+  for (int j = 0; j < kMine; ++j) {
+    const int i = tid + j * 256;
+    if (i >= n * kChunks) break;
+    const int r = list[i / kChunks];
+    const float f = factor_of[r];
+    uint4 x = v[j];
+    if (f != 1.f) x = make_uint4(rescale_e4m3x4(x.x, f), rescale_e4m3x4(x.y, f), rescale_e4m3x4(x.z, f), rescale_e4m3x4(x.w, f));
+    rows[(size_t)(d0 + r) * kChunks + i % kChunks] = x;
   }
 }
 
@@ -399,8 +403,8 @@ int launch_quant_evict(const QEvictArgs& a, cudaStream_t s) {
   while (ranks < kMaxRanks && (a.c.cap > 16384 * ranks || (items * ranks * 2 <= a.n_sms && a.c.cap >= 8192 * ranks))) ranks *= 2;
   const int slots = ((a.c.cap + ranks - 1) / ranks + 31) / 32 * 32;
   const size_t smem = (size_t)slots * 4 + (size_t)slots / 32 * 8;
-  // Heads that have an SM each are selected by 1024 threads, more heads by CTAs of fewer threads, several on an SM: 40 heads of 640 slots 11.2
-  // us against 13.9, 640 heads 52 against 28; 160 heads of 2048 slots 34 against 27, of 8192 slots 83 against 80.
+  // Heads that have an SM each are selected by 1024 threads, more heads by CTAs of fewer threads, several on an SM: 40 heads of 640 slots 10.3
+  // us against 13, 640 heads 52 against 28; 160 heads of 2048 slots 34 against 27, of 8192 slots 83 against 80.
   const bool few = ranks == 1 && items > a.n_sms && slots <= 8192;
   auto select = few ? quant_select_kernel<true> : quant_select_kernel<false>;
   if (ensure_dynamic_smem(reinterpret_cast<const void*>(select), (int)smem) != cudaSuccess) return VVS_ERR_CUDA;
@@ -418,10 +422,13 @@ int launch_quant_evict(const QEvictArgs& a, cudaStream_t s) {
   cfg.attrs = attr;
   cfg.numAttrs = 2;
   if (cudaLaunchKernelEx(&cfg, select, a, slots) != cudaSuccess) return VVS_ERR_CUDA;
-  const int whole = a.keep >> a.c.block_log2, part = a.keep & ((1 << a.c.block_log2) - 1);
+  const int whole = a.keep >> a.c.block_log2 << a.c.block_log2, next = whole + (1 << a.c.block_log2);
   auto move = a.c.hd == 64 ? quant_move_kernel<64> : quant_move_kernel<128>;
-  if (whole > 0 && launch_kernel(move, dim3(whole, a.c.n_heads, a.c.n_seqs), dim3(256), 0, true, s, a, 0) != cudaSuccess) return VVS_ERR_CUDA;
-  if (part > 0 && launch_kernel(move, dim3(1, a.c.n_heads, a.c.n_seqs), dim3(256), 0, true, s, a, whole) != cudaSuccess) return VVS_ERR_CUDA;
+  auto launch_move = [&](int begin, int end) {
+    return launch_kernel(move, dim3(2 * ((end - begin + 127) / 128), a.c.n_heads, a.c.n_seqs), dim3(256), 0, true, s, a, begin, end) == cudaSuccess;
+  };
+  if (whole > 0 && !launch_move(0, whole)) return VVS_ERR_CUDA;
+  if (a.keep > whole && !launch_move(whole, next)) return VVS_ERR_CUDA;
   return VVS_OK;
 }
 
