@@ -332,6 +332,7 @@ __global__ void __launch_bounds__(kThreads, Layout<HD>::kCtas) quant_attend_rows
       }
       if (at == 0)
         for (int x = i; x < min(nt, i + kStages); ++x) tc::mbar_wait(&full[x % kStages], (x / kStages) & 1);
+      __syncwarp();
     }
   } else {                                                      // ---- scores to weights, sums
     const int mine = warp * 32 + lane, row = r0 + mine, t = t_row(row);     // this lane's row of the tile
