@@ -691,11 +691,14 @@ int launch_tiles(const QAttendArgs& a, cudaStream_t s) {
 template <typename T, int HD>
 int launch_hd(const QAttendArgs& a, cudaStream_t s) {
   const int rows = a.n_rows * (a.n_heads / a.c.n_heads);
-  // Many rows of bf16 contexts: the kernel with 128 of them a tile.  Two trees of 27 rows x 4 heads behind 31K keys 80 us against 158 here (four
-  // tiles of 32 rows turn every key four times); 36 rows 75 against 101.  Up to 32 rows only where its items are on the device at once: 20
-  // rows, 300 to 500 keys, 140 items 13.0 us against 15.2, 160 items 20.6 against 18.2.  (Rows by 2^32 / share: exact up to 2^20 rows of 4096 heads.)
-  const long long items = (long long)a.c.n_seqs * a.c.n_heads;
-  if (sizeof(T) == 2 && a.mass_rows == 0 && rows / a.n_rows <= 4096 && (rows > 32 || (rows > 16 && items <= a.n_sms)))
+  // Many rows of bf16 contexts: the kernel with 128 of them a tile.  Two trees of 27 rows x 4 heads behind 31K keys 79 us against 158 here (four
+  // tiles of 32 rows turn every key four times), with their first rows' weights summed 167 against 447; 36 rows 75 against 101.  Up to 32 rows
+  // only where its items are on the device at once and no weights are summed: 20 rows, 300 to 500 keys, 140 items 13.0 us against 15.2,
+  // 160 items 20.6 against 18.2; 100 items behind 300 keys, weights summed, 17.8 against 13.5.  Summed rows have to lie in its first
+  // tile.  (Rows by 2^32 / share: exact up to 2^20 rows of 4096 heads.)
+  const long long items = (long long)a.c.n_seqs * a.c.n_heads, share = rows / a.n_rows;
+  const long long summed = (a.mass_rows < a.n_rows ? a.mass_rows : a.n_rows) * share;
+  if (sizeof(T) == 2 && summed <= 128 && share <= 4096 && (rows > 32 || (rows > 16 && items <= a.n_sms && a.mass_rows == 0)))
     return launch_quant_attend_rows(a, s);
   return rows <= 16 ? launch_tiles<T, HD, 1>(a, s) : launch_tiles<T, HD, 2>(a, s);
 }

@@ -11,8 +11,11 @@
 // its own keys and tensor memory, and one copy of the queries; a cluster's CTAs have more shares.  The shares' sums are joined
 // through distributed shared memory, in their order.
 //
+// Weights summed for eviction (of rows of the first tile): with the rows' sums at hand the keys go through the first product once more, and
+// the lanes' weights are added over the rows by shuffles.
+//
 // Two sequences, 27 rows x 4 heads over each of 8 cached heads of 128, 30K to 33K keys: 80 us, 346 TFLOP/s (bytes alone are 20 us, the products
-// 16).  A stream needs 3000 cycles for 64 keys: the row's lane 1200 for its powers, sums and halves, the rest waits of one stage
+// 16); 167 with the first rows' weights summed.  A stream needs 3000 cycles for 64 keys: the row's lane 1200 for its powers, sums and halves, the rest waits of one stage
 // for another; an SM issues in 47 of 100 cycles, its tensor pipe is busy in 27.  Clusters of six CTAs with an SM each are what the
 // device holds for 16 items at once: 96 of 148 SMs work (eight: 15 clusters, one waits for another to end, 124 us).  One CTA with one stream,
 // twice on an SM, is packed on half of the SMs: 135 us.
@@ -127,7 +130,8 @@ struct Layout {
   static constexpr int kStreamBytes = kCodeAt + kStages * 2 * kCodes;
   static constexpr int kTotAt = kStreamAt + kStreams * kStreamBytes;      // [stream][128][2] its rows' references and sums
   static constexpr int kFacAt = kTotAt + kStreams * kRows * 8;  // [128] what scores are multiplied by
-  static constexpr int kBarAt = kFacAt + kRows * 4;
+  static constexpr int kPartAt = kFacAt + kRows * 4;            // [stream][2][4 warps][64] summed weights of a tile's keys
+  static constexpr int kBarAt = kPartAt + kStreams * 2 * kSoft * kKeys * 4;
   static constexpr int kBars = 2 * kStages + 8;                 // of a stream; and one of the queries
   static constexpr int kNeed = kBarAt + (kStreams * kBars + 1) * 8 + 16 + 1024;       // (the base is brought to a multiple of 1024)
   // CTAs on an SM: their tensor memory is all of it, S twice 64 columns and O HD of them for each stream
@@ -138,7 +142,8 @@ struct Layout {
   static_assert(kCtas * (kBytes + 1024) <= 228 * 1024 && (kCtas + 1) * (kBytes + 1024) > 228 * 1024, "that many CTAs an SM");
 };
 
-template <int HD>
+// MASS: weights are summed, of rows of the first tile alone
+template <int HD, bool MASS>
 __global__ void __launch_bounds__(kThreads, Layout<HD>::kCtas) quant_attend_rows_kernel(QAttendArgs a, uint32_t share_inv) {
   using L = Layout<HD>;
   constexpr int kStages = L::kStages;
@@ -197,7 +202,7 @@ __global__ void __launch_bounds__(kThreads, Layout<HD>::kCtas) quant_attend_rows
   uint64_t* full = code_full + (of_keys ? 0 : kStages);
   const uint32_t code_at = stream_at + L::kCodeAt + (of_keys ? 0 : kStages * L::kCodes);
   auto request = [&](int i) {
-    const int slot0 = from + (t0 + i) * kKeys, st = i % kStages;
+    const int slot0 = from + (t0 + (MASS && i >= nt ? i - nt : i)) * kKeys, st = i % kStages;       // (i >= nt: the keys once more)
     const uint32_t bytes = min(kKeys, a.c.cap - slot0) * HD;
     tc::mbar_expect_tx(&full[st], bytes);
     bulk_load(sbase + code_at + st * L::kCodes, codes + (size_t)slot0 * HD, bytes, &full[st]);
@@ -262,59 +267,100 @@ __global__ void __launch_bounds__(kThreads, Layout<HD>::kCtas) quant_attend_rows
     if (lane == 0) tc::mbar_arrive(q_full);
   }
 
+  // This thread's 16 codes (piece of a row) of each kRowsEach rows.  Eight lanes side by side read 16-byte words of eight different groups of
+  // banks and write such: two rows, four pieces each, for heads of 128 of different slabs.
+  constexpr int kPieces = HD / 16, kTimes = kKeys * kPieces / kTurn, kRowsEach = kTurn / kPieces;
+  const int c_row = HD == 128 ? at / 16 * 2 + ((at >> 2) & 1) : at / kPieces;
+  const int c_piece = HD == 128 ? (((at >> 2) ^ (at >> 3)) & 1) * 4 + (at & 3) : at % kPieces;
+  uint8_t* to = smem + stream_at + (of_keys ? 0 : L::kValueAt) + (c_piece >> 2) * L::kSlab + c_row * 128;
+  // (kRowsEach is a multiple of 8)
+  uint8_t *to_lo = to + (((2 * (c_piece & 3)) ^ (c_row & 7)) << 4), *to_hi = to + (((2 * (c_piece & 3) + 1) ^ (c_row & 7)) << 4);
+  const bool issues = warp == (of_keys ? kSoft : kSoft + kConv / 2);
+  // Keys or values of tile i; the next ones' codes are asked for up to tile last - 1.  Both warps of a kind have the same answer, whether to go on:
+  // one that gave up comes to the barrier all the same.
+  auto turn_codes = [&](int i, int last) {
+    const int slot0 = from + (t0 + i) * kKeys, st = i % kStages;
+    ok = ok && tc::warp_wait_or_abort(&full[st], (i / kStages) & 1, abort_flag);
+    uint4 w[kTimes];
+#pragma unroll
+    for (int x = 0; x < kTimes; ++x)
+      w[x] = *reinterpret_cast<const uint4*>(smem + code_at + st * L::kCodes + (x * kRowsEach + c_row) * HD + c_piece * 16);
+    if (!of_keys && (slot0 < first || slot0 + kKeys > end)) {
+      // values of slots that no row sees are zeros, whatever lies there
+#pragma unroll
+      for (int x = 0; x < kTimes; ++x) {
+        const int slot = slot0 + c_row + x * kRowsEach;
+        if (slot < first || slot >= end) w[x] = make_uint4(0, 0, 0, 0);
+      }
+    }
+    // the halves before these have been read: by S, by O of the tile before
+    if (i > 0)
+      ok = ok && (of_keys ? tc::warp_wait_or_abort(&s_full[(i - 1) & 1], ((i - 1) >> 1) & 1, abort_flag)
+                          : tc::warp_wait_or_abort(&o_done[(i - 1) & 1], ((i - 1) >> 1) & 1, abort_flag));
+#pragma unroll
+    for (int x = 0; x < kTimes; ++x) {
+      *reinterpret_cast<uint4*>(to_lo + x * kRowsEach * 128) = halves_of(w[x].x, w[x].y);
+      *reinterpret_cast<uint4*>(to_hi + x * kRowsEach * 128) = halves_of(w[x].z, w[x].w);
+    }
+    tc::fence_proxy_async();
+    ok = tc::named_bar_all(1 + 2 * stream + (of_keys ? 0 : 1), kTurn, ok);
+    if (ok && at == 0 && i + kStages < last) request(i + kStages);
+    return ok;
+  };
+  auto multiply_keys = [&](int i) {
+    tc::tc_fence_after();
+    constexpr uint32_t idesc = (1u << 4) | ((kKeys >> 3) << 17) | ((kRows >> 4) << 24);
+#pragma unroll
+    for (int h = 0; h < HD / 64; ++h)
+      tc::mma_bf16_k64(tmem + (i & 1) * kKeys, tc::desc_lo_sw128(sbase + L::kQAt + h * (kRows * 128)),
+                       tc::desc_lo_sw128(sbase + stream_at + h * L::kSlab), idesc, h);      // (the descriptor's types are halves)
+    tc::mma_commit_elect(&s_full[i & 1]);
+  };
+  // products and copies under way, of tiles i and behind, still read and write
+  auto give_up = [&](int i, int last) {
+    *abort_flag = 1;
+    if (issues) {
+      tc::mma_commit_elect(&drained[of_keys ? 0 : 1]);
+      tc::mbar_wait(&drained[of_keys ? 0 : 1], 0);
+    }
+    if (at == 0)
+      for (int x = i; x < min(last, i + kStages); ++x) tc::mbar_wait(&full[x % kStages], (x / kStages) & 1);
+    __syncwarp();
+  };
+
+  // a row's lane: what it sees, and the tiles' scales
+  const int mine = (warp % kSoft) * 32 + lane, my_t = t_row(r0 + mine);
+  const bool live = r0 + mine < rows && my_t < n;
+  // rows of the block that this one sees: a bit of each, or those up to itself
+  const uint32_t sees = !converts && a.visible && live ? a.visible[(size_t)seq * a.n_rows + my_t] & (n < 32 ? (1u << n) - 1u : 0xffffffffu) : 0u;
+  const int upto = !live ? first : a.visible ? len : len + my_t + 1;
+  // the slots that it sees of 64 from slot0 on: first .. upto - 1, and of the block's those of `sees`
+  auto seen = [&](int slot0) {
+    const int lo = min(max(first - slot0, 0), 64), hi = min(max(upto - slot0, 0), 64), by = len - slot0;
+    uint64_t bits = (hi < 64 ? (1ULL << hi) - 1ULL : ~0ULL) & (lo < 64 ? ~0ULL << lo : 0ULL);
+    if (by > -32 && by < 64) bits |= by >= 0 ? (uint64_t)sees << by : (uint64_t)(sees >> -by);
+    return bits;
+  };
+  const uint32_t t_lane = (uint32_t)((warp % kSoft) * 32) << 16;
+  const float* scale_at = (lane & 4 ? a.c.v_scale : a.c.k_scale) + item * (a.c.cap >> a.c.block_log2);
+  // lanes 0 to 3 have the scales of the keys of a tile's four slices, lanes 4 to 7 those of their values
+  auto scale_of_tile = [&](int i) { return scale_at[min(from + (t0 + i) * kKeys + 16 * (lane & 3), end - 1) >> a.c.block_log2]; };
+  auto scores = [&](uint32_t from_at, float (&s)[kKeys]) {
+    tmem_request32(from_at, s);
+    tmem_request32(from_at + 32, s + 32);
+    tmem_arrived<kKeys>(s);
+  };
+
   if (converts) {                                               // ---- codes to halves, products: two warps for keys and S, two for values and O
-    // This thread's 16 codes (piece of a row) of each kRowsEach rows.  Eight lanes side by side read 16-byte words of eight different groups of
-    // banks and write such: two rows, four pieces each, for heads of 128 of different slabs.
-    constexpr int kPieces = HD / 16, kTimes = kKeys * kPieces / kTurn, kRowsEach = kTurn / kPieces;
-    const int row = HD == 128 ? at / 16 * 2 + ((at >> 2) & 1) : at / kPieces;
-    const int piece = HD == 128 ? (((at >> 2) ^ (at >> 3)) & 1) * 4 + (at & 3) : at % kPieces;
-    uint8_t* to = smem + stream_at + (of_keys ? 0 : L::kValueAt) + (piece >> 2) * L::kSlab + row * 128;
-    // (kRowsEach is a multiple of 8)
-    uint8_t *to_lo = to + (((2 * (piece & 3)) ^ (row & 7)) << 4), *to_hi = to + (((2 * (piece & 3) + 1) ^ (row & 7)) << 4);
-    const bool issues = warp == (of_keys ? kSoft : kSoft + kConv / 2);
     int i = 0;
 #pragma unroll 1
     for (; i < nt; ++i) {
-      const int slot0 = from + (t0 + i) * kKeys, st = i % kStages;
-      ok = ok && tc::warp_wait_or_abort(&full[st], (i / kStages) & 1, abort_flag);
-      uint4 w[kTimes];
-#pragma unroll
-      for (int x = 0; x < kTimes; ++x)
-        w[x] = *reinterpret_cast<const uint4*>(smem + code_at + st * L::kCodes + (x * kRowsEach + row) * HD + piece * 16);
-      if (!of_keys && (slot0 < first || slot0 + kKeys > end)) {
-        // values of slots that no row sees are zeros, whatever lies there
-#pragma unroll
-        for (int x = 0; x < kTimes; ++x) {
-          const int slot = slot0 + row + x * kRowsEach;
-          if (slot < first || slot >= end) w[x] = make_uint4(0, 0, 0, 0);
-        }
-      }
-      // the halves before these have been read: by S, by O of the tile before
-      if (i > 0)
-        ok = ok && (of_keys ? tc::warp_wait_or_abort(&s_full[(i - 1) & 1], ((i - 1) >> 1) & 1, abort_flag)
-                            : tc::warp_wait_or_abort(&o_done[(i - 1) & 1], ((i - 1) >> 1) & 1, abort_flag));
-#pragma unroll
-      for (int x = 0; x < kTimes; ++x) {
-        *reinterpret_cast<uint4*>(to_lo + x * kRowsEach * 128) = halves_of(w[x].x, w[x].y);
-        *reinterpret_cast<uint4*>(to_hi + x * kRowsEach * 128) = halves_of(w[x].z, w[x].w);
-      }
-      tc::fence_proxy_async();
-      // both warps have the same answer, whether to go on: one that gave up comes to this barrier all the same
-      ok = tc::named_bar_all(1 + 2 * stream + (of_keys ? 0 : 1), kTurn, ok);
-      if (!ok) break;
-      if (at == 0 && i + kStages < nt) request(i + kStages);
+      if (!turn_codes(i, nt)) break;
       if (!issues) continue;
       if (of_keys) {                                            // S of tile i, where P of tile i - 2 was
         if (i == 0) ok = tc::warp_wait_or_abort(q_full, 0, abort_flag);
         if (i > 1) ok = tc::warp_wait_or_abort(&o_done[i & 1], ((i - 2) >> 1) & 1, abort_flag);
-        if (!ok) continue;
-        tc::tc_fence_after();
-        constexpr uint32_t idesc = (1u << 4) | ((kKeys >> 3) << 17) | ((kRows >> 4) << 24);
-#pragma unroll
-        for (int h = 0; h < HD / 64; ++h)
-          tc::mma_bf16_k64(tmem + (i & 1) * kKeys, tc::desc_lo_sw128(sbase + L::kQAt + h * (kRows * 128)),
-                           tc::desc_lo_sw128(sbase + stream_at + h * L::kSlab), idesc, h);      // (the descriptor's types are halves)
-        tc::mma_commit_elect(&s_full[i & 1]);
+        if (ok) multiply_keys(i);
       } else {
         ok = tc::warp_wait_or_abort(&p_full[i & 1], (i >> 1) & 1, abort_flag);
         if (!ok) continue;
@@ -324,33 +370,8 @@ __global__ void __launch_bounds__(kThreads, Layout<HD>::kCtas) quant_attend_rows
         tc::mma_commit_elect(&o_done[i & 1]);
       }
     }
-    if (!ok) {                                                  // products and copies under way still read and write
-      *abort_flag = 1;
-      if (issues) {
-        tc::mma_commit_elect(&drained[of_keys ? 0 : 1]);
-        tc::mbar_wait(&drained[of_keys ? 0 : 1], 0);
-      }
-      if (at == 0)
-        for (int x = i; x < min(nt, i + kStages); ++x) tc::mbar_wait(&full[x % kStages], (x / kStages) & 1);
-      __syncwarp();
-    }
+    if (!ok) give_up(i, nt);
   } else {                                                      // ---- scores to weights, sums
-    const int mine = warp * 32 + lane, row = r0 + mine, t = t_row(row);     // this lane's row of the tile
-    const bool live = row < rows && t < n;
-    // rows of the block that this one sees: a bit of each, or those up to itself
-    const uint32_t sees = a.visible && live ? a.visible[(size_t)seq * a.n_rows + t] & (n < 32 ? (1u << n) - 1u : 0xffffffffu) : 0u;
-    const int upto = !live ? first : a.visible ? len : len + t + 1;
-    // the slots that it sees of 64 from slot0 on: first .. upto - 1, and of the block's those of `sees`
-    auto seen = [&](int slot0) {
-      const int lo = min(max(first - slot0, 0), 64), hi = min(max(upto - slot0, 0), 64), by = len - slot0;
-      uint64_t bits = (hi < 64 ? (1ULL << hi) - 1ULL : ~0ULL) & (lo < 64 ? ~0ULL << lo : 0ULL);
-      if (by > -32 && by < 64) bits |= by >= 0 ? (uint64_t)sees << by : (uint64_t)(sees >> -by);
-      return bits;
-    };
-    const uint32_t t_lane = (uint32_t)(warp * 32) << 16;
-    const float* scale_at = (lane & 4 ? a.c.v_scale : a.c.k_scale) + item * (a.c.cap >> a.c.block_log2);
-    // lanes 0 to 3 have the scales of the keys of a tile's four slices, lanes 4 to 7 those of their values
-    auto scale_of_tile = [&](int i) { return scale_at[min(from + (t0 + i) * kKeys + 16 * (lane & 3), end - 1) >> a.c.block_log2]; };
     float next_scale = nt > 0 ? scale_of_tile(0) : 1.f;
     float m = -CUDART_INF_F, l = 0.f;                           // (a row that is not there has neither)
     if (nt > 0) ok = tc::warp_wait_or_abort(q_full, 0, abort_flag);
@@ -395,11 +416,6 @@ __global__ void __launch_bounds__(kThreads, Layout<HD>::kCtas) quant_attend_rows
         by_value = fmaf(part, __shfl_sync(0xffffffffu, inv_vs, 4 + q), by_value);
       }
       return all;
-    };
-    auto scores = [&](uint32_t at, float (&s)[kKeys]) {
-      tmem_request32(at, s);
-      tmem_request32(at + 32, s + 32);
-      tmem_arrived<kKeys>(s);
     };
 #pragma unroll 1
     for (int i = 0; i < nt && ok; ++i) {
@@ -547,12 +563,115 @@ __global__ void __launch_bounds__(kThreads, Layout<HD>::kCtas) quant_attend_rows
     store4(static_cast<__nv_bfloat16*>(a.out.data) + seq * a.out.seq + (int64_t)t * a.out.row + h * a.out.head + piece * 4, x);
     if (a.lse && piece == 0) a.lse[((size_t)seq * a.n_rows + t) * a.n_heads + h] = some ? (top - kShift + log2f(total)) / kLog2e : -CUDART_INF_F;
   }
+  // log2 of a summed row's sum; of other rows, and of one that sees nothing, infinity
+  const int summed = MASS && tile == 0 ? min(kRows, min(a.mass_rows, n) * share) : 0;
+  float sub = CUDART_INF_F;
+  if (MASS && !converts && mine < summed) {
+    float2 ml[kMaxRanks][kStreams];
+    float top = -CUDART_INF_F, total = 0.f;
+#pragma unroll
+    for (int k = 0; k < kMaxRanks; ++k)
+#pragma unroll
+      for (int st = 0; st < kStreams; ++st) {
+        ml[k][st] = make_float2(-CUDART_INF_F, 0.f);
+        if (k < ranks) ml[k][st] = ld_cluster_f2(tot_at + (st * kRows + mine) * 8, k);
+        top = fmaxf(top, ml[k][st].x);
+      }
+#pragma unroll
+    for (int k = 0; k < kMaxRanks; ++k)
+#pragma unroll
+      for (int st = 0; st < kStreams; ++st) total = fmaf(ml[k][st].y, ml[k][st].x == -CUDART_INF_F ? 0.f : ex2(ml[k][st].x - top), total);
+    if (!(total == 0.f)) sub = top - kShift + log2f(total);
+  }
+  if (MASS) tc::fence_proxy_async();                            // codes come where the sums were
   __syncwarp();
   if (ranks > 1) tc::cluster_sync(); else __syncthreads();      // the other ranks have read this one's sums
+
+  // ---- weights of the keys: the keys once more, by the CTAs of the first rows --------------------------------------------------------------------
+  if (MASS && tile == 0 && !failed) {
+    float* mass = a.c.mass + item * a.c.cap;
+    const float decay = a.mass_decay;
+    // slots before the first tile only lose; where no row is summed, all do
+    for (int slot = rank * kThreads + tid; slot < (summed > 0 ? min(from, end) : end); slot += ranks * kThreads)
+      if (decay != 1.f) mass[slot] = decay == 0.f ? 0.f : decay * mass[slot];
+    if (summed > 0) {
+      const int last = 2 * nt;
+      if (converts) {
+        if (of_keys) {
+          if (at == 0)
+            for (int i = nt; i < min(last, nt + kStages); ++i) request(i);
+          int i = nt;
+#pragma unroll 1
+          for (; i < last; ++i) {
+            if (!turn_codes(i, last)) break;
+            if (!issues) continue;
+            if (i >= nt + 2) ok = tc::warp_wait_or_abort(&p_full[i & 1], ((i - 2) >> 1) & 1, abort_flag);      // S of tile i - 2 has been read
+            if (ok) multiply_keys(i);
+          }
+          if (!ok) give_up(i, last);
+        }
+      } else {
+        const int warps = (summed + 31) / 32;                   // that have summed rows
+        const float fac = fac_of[mine];
+        float* part = reinterpret_cast<float*>(smem + L::kPartAt) + stream * 2 * kSoft * kKeys;
+        float next_scale = nt > 0 ? scale_of_tile(0) : 1.f;
+#pragma unroll 1
+        for (int j = 0; j < nt; ++j) {
+          const int i = nt + j, slot0 = from + (t0 + j) * kKeys;
+          const float scale = next_scale;
+          if (j + 1 < nt) next_scale = scale_of_tile(j + 1);
+          float was[2] = {0.f, 0.f};
+          if (warp == 0 && decay != 0.f)
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+              if (slot0 + x * 32 + lane < end) was[x] = mass[slot0 + x * 32 + lane];
+          ok = ok && tc::warp_wait_or_abort(&s_full[i & 1], (i >> 1) & 1, abort_flag);
+          tc::tc_fence_after();
+          if (warp < warps) {
+            float s[kKeys];
+            scores(tmem + t_lane + (i & 1) * kKeys, s);
+            tc::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(&p_full[i & 1]);
+            const uint64_t bits = sub == CUDART_INF_F ? 0ULL : seen(slot0);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const float f = fac * __shfl_sync(0xffffffffu, scale, q);
+              float v[16];
+#pragma unroll
+              for (int e = 0; e < 16; ++e) v[e] = (bits >> (16 * q + e)) & 1 ? ex2(fmaf(s[16 * q + e], f, -sub)) : 0.f;
+              tc::warp_sums<16>(v, lane);
+              if (!(lane & 1)) part[((i & 1) * kSoft + warp) * kKeys + 16 * q + tc::warp_sums_index<16>(lane)] = v[0];
+            }
+            // (of the part's two buffers, this one's were read before the barrier of the tile before)
+            if (warps > 1) tc::named_bar_sync(5 + stream, 32 * warps);
+            else __syncwarp();
+            if (warp == 0) {
+#pragma unroll
+              for (int x = 0; x < 2; ++x) {
+                const int key = x * 32 + lane;
+                float sum = 0.f;
+                for (int w = 0; w < warps; ++w) sum += part[((i & 1) * kSoft + w) * kKeys + key];
+                if (slot0 + key < end && ok) mass[slot0 + key] = decay == 0.f ? sum : fmaf(decay, was[x], sum);
+              }
+              __syncwarp();
+            }
+          } else if (lane == 0) {
+            tc::mbar_arrive(&p_full[i & 1]);
+          }
+          __syncwarp();
+        }
+        if (!ok) *abort_flag = 1;
+      }
+    }
+    __syncthreads();
+    tc::tc_fence_after();
+    if (tid == 0 && *abort_flag) atomicOr(a.status, VVS_DEV_TIMEOUT);
+  }
   if (tid < 32) tc::tmem_dealloc(*tmem_slot, L::kColumns);
 }
 
-template <int HD>
+template <int HD, bool MASS>
 int launch_hd(const QAttendArgs& a, cudaStream_t s) {
   using L = Layout<HD>;
   const int rows = a.n_rows * (a.n_heads / a.c.n_heads), row_tiles = (rows + kRows - 1) / kRows;
@@ -560,7 +679,7 @@ int launch_hd(const QAttendArgs& a, cudaStream_t s) {
   const int tiles = ((a.max_len > 0 && a.max_len < a.c.cap ? a.max_len : a.c.cap) + kKeys - 1) / kKeys;
   const int share = a.n_heads / a.c.n_heads;
   const uint32_t share_inv = share == 1 ? 0u : (uint32_t)(((1ULL << 32) + share - 1) / share);
-  auto kernel = quant_attend_rows_kernel<HD>;
+  auto kernel = quant_attend_rows_kernel<HD, MASS>;
   if (ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), L::kBytes) != cudaSuccess) return VVS_ERR_CUDA;
   cudaLaunchConfig_t cfg = {};
   cfg.blockDim = dim3(kThreads);
@@ -586,6 +705,9 @@ int launch_hd(const QAttendArgs& a, cudaStream_t s) {
 
 }  // namespace
 
-int launch_quant_attend_rows(const QAttendArgs& a, cudaStream_t s) { return a.c.hd == 64 ? launch_hd<64>(a, s) : launch_hd<128>(a, s); }
+int launch_quant_attend_rows(const QAttendArgs& a, cudaStream_t s) {
+  if (a.mass_rows > 0) return a.c.hd == 64 ? launch_hd<64, true>(a, s) : launch_hd<128, true>(a, s);
+  return a.c.hd == 64 ? launch_hd<64, false>(a, s) : launch_hd<128, false>(a, s);
+}
 
 }  // namespace vvs

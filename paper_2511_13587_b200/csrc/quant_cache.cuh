@@ -68,7 +68,7 @@ struct QAttendArgs {
 };
 template <typename T>
 int launch_quant_attend(const QAttendArgs& a, cudaStream_t s);
-int launch_quant_attend_rows(const QAttendArgs& a, cudaStream_t s);        // bf16, many rows, no weights summed
+int launch_quant_attend_rows(const QAttendArgs& a, cudaStream_t s);        // bf16, many rows, 128 summed ones at most
 
 struct QEvictArgs {
   QCache c;

@@ -23,6 +23,8 @@ MANY = [
     (129, 1, 1, 128, 32, [300], None, [33], False, 129, 0.75),
     (43, 6, 2, 64, 16, [2500, 17], None, [0, 1], False, 2, 0.0),
     (5, 40, 1, 128, 128, [3000], [4], [100], True, 5, 1.0),
+    (50, 2, 1, 128, 64, [5000, 77], [50, 49], [0, 3], False, 50, 0.25),
+    (30, 8, 2, 64, 16, [4000], None, [1777], True, 9, 0.0),
 ]
 
 
