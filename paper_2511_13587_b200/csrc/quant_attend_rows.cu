@@ -134,17 +134,17 @@ struct Layout {
   static constexpr int kBarAt = kPartAt + kStreams * 2 * kSoft * kKeys * 4;
   static constexpr int kBars = 2 * kStages + 8;                 // of a stream; and one of the queries
   static constexpr int kNeed = kBarAt + (kStreams * kBars + 1) * 8 + 16 + 1024;       // (the base is brought to a multiple of 1024)
-  // CTAs on an SM: their tensor memory is all of it, S twice 64 columns and O HD of them for each stream
-  static constexpr int kCtas = 2 / kStreams, kAtLeast = (kStreams == 2 ? 120 : 80) * 1024;
-  static constexpr int kBytes = kNeed < kAtLeast ? kAtLeast : kNeed;
-  static constexpr int kColumns = 256 * kStreams, kStreamColumns = 256, kOut = 2 * kKeys;
+  // One CTA on an SM: it has all of the tensor memory, S twice 64 columns and O HD of them for each stream.  And none of another kernel that
+  // multiplies there: two clusters that hold tensor memory on one SM each and wait for it on the other's would wait forever.
+  static constexpr int kBytes = kNeed < 200 * 1024 ? 200 * 1024 : kNeed;
+  static constexpr int kColumns = 512, kStreamColumns = 256, kOut = 2 * kKeys;
   static_assert(kStreamBytes >= kRows * HD * 4, "a stream's sums fit");
-  static_assert(kCtas * (kBytes + 1024) <= 228 * 1024 && (kCtas + 1) * (kBytes + 1024) > 228 * 1024, "that many CTAs an SM");
+  static_assert(kBytes <= 227 * 1024, "shared memory");
 };
 
 // MASS: weights are summed, of rows of the first tile alone
 template <int HD, bool MASS>
-__global__ void __launch_bounds__(kThreads, Layout<HD>::kCtas) quant_attend_rows_kernel(QAttendArgs a, uint32_t share_inv) {
+__global__ void __launch_bounds__(kThreads, 1) quant_attend_rows_kernel(QAttendArgs a, uint32_t share_inv) {
   using L = Layout<HD>;
   constexpr int kStages = L::kStages;
   extern __shared__ __align__(16) uint8_t smem_raw[];
@@ -517,7 +517,7 @@ __global__ void __launch_bounds__(kThreads, Layout<HD>::kCtas) quant_attend_rows
     const int r = v / (HD / 4), piece = v % (HD / 4), row = r0 + r;
     if (row >= rows) break;
     const int t = t_row(row), h = head * share + row - t * share;
-    constexpr int kTogether = 8 / kStreams;
+    constexpr int kTogether = 4;
     float2 ml[kMaxRanks][kStreams];
     float top = -CUDART_INF_F;
 #pragma unroll
