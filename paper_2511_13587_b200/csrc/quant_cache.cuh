@@ -84,7 +84,7 @@ int launch_quant_evict(const QEvictArgs& a, cudaStream_t s);
 // Clusters of 1 .. 16 CTAs of a kernel that the device holds at once, by their CTAs; null: an error.  A cluster's CTAs lie in one group
 // of SMs: of CTAs that fill an SM, the device may hold 33 clusters of four, 15 of eight, 7 of sixteen.
 constexpr int kMaxCluster = 16;
-inline const int* resident_clusters(const void* kernel, int threads, int dynamic_smem) {
+inline const int* resident_clusters(const void* kernel, int threads, int dynamic_smem) try {
   struct Counts { int there[kMaxCluster + 1]; };
   static std::mutex mu;
   static std::map<std::pair<int, const void*>, Counts> known;
@@ -110,6 +110,8 @@ inline const int* resident_clusters(const void* kernel, int threads, int dynamic
     if (cudaOccupancyMaxActiveClusters(&got.there[c], kernel, &cfg) != cudaSuccess) return nullptr;
   }
   return known.emplace(key, got).first->second.there;
+} catch (...) {                                // no memory for the table, no lock
+  return nullptr;
 }
 
 // ---- eight values of a row, 16 bytes of bf16 or 32 of float32; or two groups of four -----------------------------------
