@@ -40,7 +40,7 @@ __device__ __forceinline__ void request_rows(const QAppendArgs& a, const HeadRow
     if (t >= end) continue;
     const int from = picked ? a.row_index[(size_t)ch.seq * a.n_rows + t] : t;
     if (from >= 0 && from < a.n_rows) {
-      raw[p] = load_unit_raw(base + from * src.row, u, split, a.rope.n_pairs);
+      raw[p] = load_unit(base + from * src.row + unit_at(u, split), split, a.rope.n_pairs);
     } else {
       raw[p] = Unit<T>{};
       atomicOr(a.status, VVS_DEV_BAD_ARG);
@@ -48,25 +48,44 @@ __device__ __forceinline__ void request_rows(const QAppendArgs& a, const HeadRow
   }
 }
 
-// A piece's values, turned by its row's angles.
-template <typename T, int HD>
+// Cosines and sines of a piece's four pairs, of a row.
+template <int HD>
+__device__ __forceinline__ void angles_of(const float2* table, int row, float (&c)[4], float (&s)[4]) {
+  const float4* cs = reinterpret_cast<const float4*>(table + (size_t)row * (HD / 2) + 4 * (threadIdx.x % (HD / 8)));
+  const float4 lo = cs[0], hi = cs[1];
+  c[0] = lo.x; s[0] = lo.y; c[1] = lo.z; s[1] = lo.w;
+  c[2] = hi.x; s[2] = hi.y; c[3] = hi.z; s[3] = hi.w;
+}
+// Whether a unit has any pair at all.
+__device__ __forceinline__ bool unit_turns(const RopeAxes& r, int u) { return 4 * u < r.n_pairs; }
+// A piece's values, turned by its row's angles if it is `mine`: all pairs, or (SOME) those that have any.
+template <typename T, int HD, bool SOME>
 __device__ __forceinline__ void values_of(const Unit<T>& raw, bool mine, bool split, const float2* table, int row, float (&x)[8]) {
   widen_unit(raw, x);
   if (!mine) return;
-  const float4* cs = reinterpret_cast<const float4*>(table + (size_t)row * (HD / 2) + 4 * (threadIdx.x % (HD / 8)));
-  const float4 lo = cs[0], hi = cs[1];
-  const float c[4] = {lo.x, lo.z, hi.x, hi.z}, s[4] = {lo.y, lo.w, hi.y, hi.w};
-  turn_unit(x, split, c, s);
+  float c[4], s[4];
+  angles_of<HD>(table, row, c, s);
+  if (SOME) turn_some(x, split, c, s, pairs_of(c));
+  else turn_unit(x, split, c, s);
+}
+// One of a thread's pieces, by an index that is not known where the code is made.
+template <typename T, int PASSES>
+__device__ __forceinline__ Unit<T> piece_of(const Unit<T> (&raw)[PASSES], int p) {
+  Unit<T> piece = raw[0];
+#pragma unroll
+  for (int j = 1; j < PASSES; ++j)
+    if (j == p) piece = raw[j];
+  return piece;
 }
 
 // A head's rows into the cache, by a warp or by the CTA.  They are turned twice, for the maximum and for the codes: that takes fewer registers
 // than one turned copy (bf16 rows of long blocks: 80 of a thread in the place of 213).
 template <typename T, int HD, int PASSES, bool WARP>
-__device__ __forceinline__ void put_rows(const QAppendArgs& a, const Unit<T> (&raw)[PASSES], bool turned, uint8_t* codes, float* scales, const Chunk& ch,
-                                         int head, const float2* table, float* red, bool& odd) {
+__device__ __forceinline__ void put_rows(const QAppendArgs& a, const Unit<T> (&raw)[PASSES], bool turned, uint8_t* codes, float* scales,
+                                         const Chunk& ch, int head, const float2* table, float* red, bool& odd) {
   constexpr int kUnits = HD / 8, kRows = kPassRows<HD, WARP>;
   const int tid = WARP ? threadIdx.x % 32 : threadIdx.x, u = tid % kUnits, r = tid / kUnits, n_pairs = a.rope.n_pairs;
-  const bool split = turned && unit_split(a.rope, u), mine = turned && (split || !a.rope.halves);
+  const bool mine = turned && unit_turns(a.rope, u), split = turned && unit_split(a.rope, u);
   float* scale = scales + ((size_t)ch.seq * a.c.n_heads + head) * (a.c.cap >> a.c.block_log2) + ch.block;
   const float old = ch.live > 0 ? *scale : 0.f;
   float amax = 0.f, zero = 0.f;                // zero: NaN once an infinity or a NaN has been seen
@@ -74,7 +93,7 @@ __device__ __forceinline__ void put_rows(const QAppendArgs& a, const Unit<T> (&r
   for (int p = 0; p < PASSES; ++p) {
     if (ch.t0 + p * kRows + r >= ch.tk) continue;
     float x[8];
-    values_of<T, HD>(raw[p], mine, split, table, p * kRows + r, x);
+    values_of<T, HD, false>(raw[p], mine, split, table, p * kRows + r, x);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       amax = fmaxf(amax, fabsf(x[e]));
@@ -83,20 +102,18 @@ __device__ __forceinline__ void put_rows(const QAppendArgs& a, const Unit<T> (&r
   }
   const bool strange = zero != zero;           // an infinity becomes the largest code, a NaN zero; neither counts for the scale
   if (strange) {
-    odd = true;
     amax = 0.f;
 #pragma unroll 1
     for (int p = 0; p < PASSES; ++p) {
       if (ch.t0 + p * kRows + r >= ch.tk) continue;
-      Unit<T> piece = raw[0];
-#pragma unroll
-      for (int j = 1; j < PASSES; ++j)
-        if (j == p) piece = raw[j];
       float x[8];
-      values_of<T, HD>(piece, mine, split, table, p * kRows + r, x);
+      values_of<T, HD, true>(piece_of(raw, p), mine, split, table, p * kRows + r, x);
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (fabsf(x[e]) < CUDART_INF_F) amax = fmaxf(amax, fabsf(x[e]));
+      for (int e = 0; e < 8; ++e) {
+        const bool fine = fabsf(x[e]) < CUDART_INF_F;
+        if (fine) amax = fmaxf(amax, fabsf(x[e]));
+        odd = odd || !fine;
+      }
     }
   }
   __syncwarp();
@@ -111,25 +128,34 @@ __device__ __forceinline__ void put_rows(const QAppendArgs& a, const Unit<T> (&r
   }
   const float fresh = scale_of(amax), now = ch.live > 0 ? fmaxf(old, fresh) : fresh, inv = 1.f / now;
   uint8_t* rows = codes + (((size_t)ch.seq * a.c.n_heads + head) * a.c.cap + ((size_t)ch.block << a.c.block_log2)) * HD;
-#pragma unroll
-  for (int p = 0; p < PASSES; ++p) {
-    const int t = ch.t0 + p * kRows + r;
-    if (t >= ch.tk) continue;
-    uint8_t* at = rows + (size_t)(ch.live + t - ch.t0) * HD;
-    float x[8];
-    values_of<T, HD>(raw[p], mine, split, table, p * kRows + r, x);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] *= inv;
-    if (strange) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = x[e] == x[e] ? x[e] : 0.f;
-    }
+  auto put_codes = [&](int p, float (&x)[8]) {
+    uint8_t* at = rows + (size_t)(ch.live + p * kRows + r) * HD;
     const uint32_t lo = to_e4m3x4(x[0], x[1], x[2], x[3]), hi = to_e4m3x4(x[4], x[5], x[6], x[7]);
     if (split) {
       *reinterpret_cast<uint32_t*>(at + 4 * u) = lo;
       *reinterpret_cast<uint32_t*>(at + n_pairs + 4 * u) = hi;
     } else {
       *reinterpret_cast<uint2*>(at + 8 * u) = make_uint2(lo, hi);
+    }
+  };
+#pragma unroll
+  for (int p = 0; p < PASSES; ++p) {
+    if (strange || ch.t0 + p * kRows + r >= ch.tk) continue;
+    float x[8];
+    values_of<T, HD, false>(raw[p], mine, split, table, p * kRows + r, x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] *= inv;
+    put_codes(p, x);
+  }
+  if (strange) {
+#pragma unroll 1
+    for (int p = 0; p < PASSES; ++p) {
+      if (ch.t0 + p * kRows + r >= ch.tk) continue;
+      float x[8];
+      values_of<T, HD, true>(piece_of(raw, p), mine, split, table, p * kRows + r, x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = x[e] == x[e] ? x[e] * inv : 0.f;
+      put_codes(p, x);
     }
   }
   if (ch.live > 0 && now > old) {              // the rows before these are rounded again
@@ -201,28 +227,49 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 3 : 1) quant_append
         if (t >= rows) break;
         float2 cs;
         sincosf(__fmul_rn((float)pos[j], pa.freq), &cs.y, &cs.x);
+        if (!pa.pos) cs = make_float2(kStays, CUDART_NAN_F);       // (a piece with such a pair takes the way of the infinities)
         table[t * (HD / 2) + pair] = cs;
       }
     }
     __syncthreads();
   }
+  // of queries: where this thread's pieces lie, and the pairs of them that are turned
+  const bool apart = rope && unit_split(a.rope, u);
+  uint32_t pairs = 0;
+  if (FEW && rope && i0 < kv + qs && unit_turns(a.rope, u)) {
+    float c[4], s[4];
+    angles_of<HD>(table, 0, c, s);
+    pairs = pairs_of(c);
+  }
   bool odd = false;
   int use = 0;                                 // the maxima's room in turns: one barrier a head is enough
   for (int i = mine; i < i1; i += step) {
     if (is_query(i)) {
-      const bool split = rope && unit_split(a.rope, u);
-#pragma unroll
-      for (int p = 0; p < PASSES; ++p) {
+      auto put_query = [&](int p, const Unit<T>& piece, bool some) {
         const int in = p * kPassRows<HD, FEW> + r, t = ch.t0 + in;
-        if (t >= ch.t1) continue;
-        float x[8];
-        values_of<T, HD>(raw[p], rope && (split || !a.rope.halves), split, table, in, x);
-        store_unit(static_cast<T*>(a.q_out.data) + ch.seq * a.q_out.seq + (i - kv) * a.q_out.head + t * a.q_out.row, u, split, a.rope.n_pairs, x);
+        if (t >= ch.t1) return;
+        Unit<T> out = piece;
+        if (pairs) {
+          float c[4], s[4];
+          angles_of<HD>(table, in, c, s);
+          out = some ? turned_some(piece, apart, c, s, pairs) : turned_unit(piece, apart, c, s);
+        }
+        store_unit(static_cast<T*>(a.q_out.data) + ch.seq * a.q_out.seq + (i - kv) * a.q_out.head + t * a.q_out.row +
+                       unit_at(u, apart),
+                   apart, a.rope.n_pairs, out);
+      };
+      if (!pairs || pairs == kAllPairs) {
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) put_query(p, raw[p], false);
+      } else {
+#pragma unroll 1
+        for (int p = 0; p < PASSES; ++p) put_query(p, piece_of(raw, p), true);
       }
     } else if (ch.t0 < ch.tk) {
       const bool key = i < kv;
       const int head = key ? i : i - kv - qs, at = FEW ? tid % 32 : tid;
-      put_rows<T, HD, PASSES, FEW>(a, raw, key && rope, key ? a.c.k : a.c.v, key ? a.c.k_scale : a.c.v_scale, ch, head, table, red[use ^= 1], odd);
+      put_rows<T, HD, PASSES, FEW>(a, raw, key && rope, key ? a.c.k : a.c.v, key ? a.c.k_scale : a.c.v_scale, ch, head, table,
+                                   red[use ^= 1], odd);
       if (key && at < ch.tk - ch.t0) {         // (few rows are at most 32)
         const size_t slot = ((size_t)ch.seq * kv + head) * a.c.cap + base + ch.t0 + at;
         if (a.c.mass) a.c.mass[slot] = 0.f;

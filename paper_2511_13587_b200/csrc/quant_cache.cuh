@@ -114,7 +114,7 @@ inline const int* resident_clusters(const void* kernel, int threads, int dynamic
   return nullptr;
 }
 
-// ---- eight values of a row, 16 bytes of bf16 or 32 of float32; or two groups of four -----------------------------------
+// ---- four values of a row, 8 bytes of bf16 or 16 of float32 -----------------------------------------------------------
 __device__ __forceinline__ uint32_t pack_bf16x2(float a, float b) {
   const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&h);
@@ -123,10 +123,6 @@ __device__ __forceinline__ void store4(__nv_bfloat16* p, const float* x) {
   *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
 }
 __device__ __forceinline__ void store4(float* p, const float* x) { *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]); }
-__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&x)[8]) {
-  *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
-}
-__device__ __forceinline__ void store8(float* p, const float (&x)[8]) { store4(p, x); store4(p + 4, x + 4); }
 
 // ---- rotation ---------------------------------------------------------------------------------------------------------
 // A head is worked on in units of eight elements.  Neighbouring pairs: unit u is elements 8u .. 8u + 7, pairs 4u .. 4u + 3.
@@ -134,8 +130,8 @@ __device__ __forceinline__ void store8(float* p, const float (&x)[8]) { store4(p
 // are the elements that stay as they are, 8u .. 8u + 7 (n_pairs is a multiple of four there).
 __device__ __forceinline__ bool unit_split(const RopeAxes& r, int u) { return r.halves && 4 * u < r.n_pairs; }
 
-// A pair's positions [n_seqs][n_rows] (null: the pair is not turned, being behind the last or of an unknown axis) and frequency.  Its angle is
-// the float32 product of the two; the cosine and sine of position 0 are those of a pair that stays as it is.
+// A pair's positions [n_seqs][n_rows] (null: the pair stays as it is, being behind the last or of an unknown axis) and frequency.  Its angle is
+// the float32 product of the two.
 struct PairAxis {
   const int32_t* pos;
   float freq;
@@ -167,6 +163,28 @@ __device__ __forceinline__ void turn_unit(float (&x)[8], bool split, const float
     for (int i = 0; i < 4; ++i) turn(x[2 * i], x[2 * i + 1], c[i], s[i]);
   }
 }
+// In the place of a cosine: the pair stays as it is.  It is left alone, not turned by an angle of 0: next to an infinity,
+// x * 1 + inf * 0 would be a NaN.  A unit of which only some pairs are turned (the last pair lies in it, or one of an unknown axis) has a
+// path of its own: selections in the loops over whole units cost an append of prompts 83 us in the place of 71.
+constexpr float kStays = 2.f;
+// Which of a unit's four pairs are turned: bit i is pair 4u + i.
+__device__ __forceinline__ uint32_t pairs_of(const float (&c)[4]) {
+  uint32_t pairs = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) pairs |= c[j] != kStays ? 1u << j : 0u;
+  return pairs;
+}
+constexpr uint32_t kAllPairs = 15u;
+// those pairs alone
+__device__ __forceinline__ void turn_some(float (&x)[8], bool split, const float* c, const float* s, uint32_t pairs) {
+  float y[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) y[e] = x[e];
+  turn_unit(y, split, c, s);
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (pairs >> (split ? e % 4 : e / 2) & 1u) x[e] = y[e];
+}
 // as they are stored
 template <typename T>
 struct Unit;
@@ -178,14 +196,15 @@ template <>
 struct Unit<float> {
   float4 a, b;
 };
-__device__ __forceinline__ Unit<__nv_bfloat16> load_unit_raw(const __nv_bfloat16* row, int u, bool split, int n_pairs) {
-  if (split) return {*reinterpret_cast<const uint2*>(row + 4 * u), *reinterpret_cast<const uint2*>(row + n_pairs + 4 * u)};
-  const uint4 t = *reinterpret_cast<const uint4*>(row + 8 * u);
+// where a unit begins in its row; its second half lies n_pairs behind that, or next to the first
+__device__ __forceinline__ int unit_at(int u, bool split) { return (split ? 4 : 8) * u; }
+__device__ __forceinline__ Unit<__nv_bfloat16> load_unit(const __nv_bfloat16* p, bool split, int n_pairs) {
+  if (split) return {*reinterpret_cast<const uint2*>(p), *reinterpret_cast<const uint2*>(p + n_pairs)};
+  const uint4 t = *reinterpret_cast<const uint4*>(p);
   return {make_uint2(t.x, t.y), make_uint2(t.z, t.w)};
 }
-__device__ __forceinline__ Unit<float> load_unit_raw(const float* row, int u, bool split, int n_pairs) {
-  const float* p = row + (split ? 4 : 8) * u;
-  return {*reinterpret_cast<const float4*>(p), *reinterpret_cast<const float4*>(split ? row + n_pairs + 4 * u : p + 4)};
+__device__ __forceinline__ Unit<float> load_unit(const float* p, bool split, int n_pairs) {
+  return {*reinterpret_cast<const float4*>(p), *reinterpret_cast<const float4*>(p + (split ? n_pairs : 4))};
 }
 __device__ __forceinline__ void widen_unit(const Unit<__nv_bfloat16>& r, float (&x)[8]) {
   const uint32_t w[4] = {r.a.x, r.a.y, r.b.x, r.b.y};
@@ -198,14 +217,54 @@ __device__ __forceinline__ void widen_unit(const Unit<__nv_bfloat16>& r, float (
 __device__ __forceinline__ void widen_unit(const Unit<float>& r, float (&x)[8]) {
   x[0] = r.a.x; x[1] = r.a.y; x[2] = r.a.z; x[3] = r.a.w; x[4] = r.b.x; x[5] = r.b.y; x[6] = r.b.z; x[7] = r.b.w;
 }
-template <typename T>
-__device__ __forceinline__ void store_unit(T* row, int u, bool split, int n_pairs, const float (&x)[8]) {
-  if (split) {
-    store4(row + 4 * u, x);
-    store4(row + n_pairs + 4 * u, x + 4);
-  } else {
-    store8(row + 8 * u, x);
+__device__ __forceinline__ Unit<__nv_bfloat16> narrow_unit(const float (&x)[8], const Unit<__nv_bfloat16>&) {
+  return {make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])), make_uint2(pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]))};
+}
+__device__ __forceinline__ Unit<float> narrow_unit(const float (&x)[8], const Unit<float>&) {
+  return {make_float4(x[0], x[1], x[2], x[3]), make_float4(x[4], x[5], x[6], x[7])};
+}
+// what is not turned as it came (rounding to bf16 would give another NaN for a NaN)
+__device__ __forceinline__ void put_back(Unit<__nv_bfloat16>& out, const Unit<__nv_bfloat16>& raw, bool split, uint32_t pairs) {
+  uint32_t* o[4] = {&out.a.x, &out.a.y, &out.b.x, &out.b.y};
+  const uint32_t r[4] = {raw.a.x, raw.a.y, raw.b.x, raw.b.y};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int first = split ? 2 * i % 4 : i, second = split ? 2 * i % 4 + 1 : i;      // pairs of the word's two elements
+    const uint32_t mask = (pairs >> first & 1u ? 0xffffu : 0u) | (pairs >> second & 1u ? 0xffff0000u : 0u);
+    *o[i] = (*o[i] & mask) | (r[i] & ~mask);
   }
+}
+__device__ __forceinline__ void put_back(Unit<float>& out, const Unit<float>& raw, bool split, uint32_t pairs) {
+  float* o[8] = {&out.a.x, &out.a.y, &out.a.z, &out.a.w, &out.b.x, &out.b.y, &out.b.z, &out.b.w};
+  const float r[8] = {raw.a.x, raw.a.y, raw.a.z, raw.a.w, raw.b.x, raw.b.y, raw.b.z, raw.b.w};
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (!(pairs >> (split ? e % 4 : e / 2) & 1u)) *o[e] = r[e];
+}
+template <typename T>
+__device__ __forceinline__ Unit<T> turned_unit(const Unit<T>& raw, bool split, const float* c, const float* s) {
+  float x[8];
+  widen_unit(raw, x);
+  turn_unit(x, split, c, s);
+  return narrow_unit(x, raw);
+}
+template <typename T>
+__device__ __forceinline__ Unit<T> turned_some(const Unit<T>& raw, bool split, const float* c, const float* s, uint32_t pairs) {
+  Unit<T> out = turned_unit(raw, split, c, s);
+  put_back(out, raw, split, pairs);
+  return out;
+}
+__device__ __forceinline__ void store_unit(__nv_bfloat16* p, bool split, int n_pairs, const Unit<__nv_bfloat16>& x) {
+  if (split) {
+    *reinterpret_cast<uint2*>(p) = x.a;
+    *reinterpret_cast<uint2*>(p + n_pairs) = x.b;
+  } else {
+    *reinterpret_cast<uint4*>(p) = make_uint4(x.a.x, x.a.y, x.b.x, x.b.y);
+  }
+}
+__device__ __forceinline__ void store_unit(float* p, bool split, int n_pairs, const Unit<float>& x) {
+  *reinterpret_cast<float4*>(p) = x.a;
+  *reinterpret_cast<float4*>(p + (split ? n_pairs : 4)) = x.b;
 }
 
 // ---- e4m3 -------------------------------------------------------------------------------------------------------------

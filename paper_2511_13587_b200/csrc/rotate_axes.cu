@@ -24,14 +24,14 @@ __global__ void __launch_bounds__(kThreads, 7) rotate_axes_kernel(RotateArgs a, 
   const int at = (int)(i / units), row = at % a.n_rows, seq = at / a.n_rows;
   const bool split = unit_split(a.rope, u);
   const int heads = a.n_heads + a.n_kv_heads, h0 = blockIdx.y * heads_each, h1 = min(heads, h0 + heads_each);
-  const T* q = static_cast<const T*>(a.q.data) + seq * a.q.seq + row * a.q.row;
-  const T* k = static_cast<const T*>(a.k.data) + seq * a.k.seq + row * a.k.row;
-  T* qo = static_cast<T*>(a.q_out.data) + seq * a.q_out.seq + row * a.q_out.row;
-  T* ko = static_cast<T*>(a.k_out.data) + seq * a.k_out.seq + row * a.k_out.row;
+  const T* q = static_cast<const T*>(a.q.data) + seq * a.q.seq + row * a.q.row + unit_at(u, split);
+  const T* k = static_cast<const T*>(a.k.data) + seq * a.k.seq + row * a.k.row + unit_at(u, split);
+  T* qo = static_cast<T*>(a.q_out.data) + seq * a.q_out.seq + row * a.q_out.row + unit_at(u, split);
+  T* ko = static_cast<T*>(a.k_out.data) + seq * a.k_out.seq + row * a.k_out.row + unit_at(u, split);
   auto request = [&](int h, Unit<T> (&x)[kFlight]) {
 #pragma unroll
     for (int j = 0; j < kFlight; ++j)
-      if (h + j < h1) x[j] = load_unit_raw(h + j < a.n_heads ? q + (h + j) * a.q.head : k + (h + j - a.n_heads) * a.k.head, u, split, a.rope.n_pairs);
+      if (h + j < h1) x[j] = load_unit(h + j < a.n_heads ? q + (h + j) * a.q.head : k + (h + j - a.n_heads) * a.k.head, split, a.rope.n_pairs);
   };
   // the first heads travel beside the angles, the next ones beside the turning
   Unit<T> x[kFlight];
@@ -45,16 +45,20 @@ __global__ void __launch_bounds__(kThreads, 7) rotate_axes_kernel(RotateArgs a, 
   for (int j = 0; j < 4; ++j) pos[j] = pa[j].pos ? pa[j].pos[(size_t)seq * a.n_rows + row] : 0;
 #pragma unroll
   for (int j = 0; j < 4; ++j) sincosf(__fmul_rn((float)pos[j], pa[j].freq), &s[j], &c[j]);
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (!pa[j].pos) c[j] = kStays;
+  const bool some = pairs_of(c) != kAllPairs;
+  auto at_out = [&](int h) { return h < a.n_heads ? qo + h * a.q_out.head : ko + (h - a.n_heads) * a.k_out.head; };
   for (int h = h0; h < h1; h += kFlight) {
     Unit<T> next[kFlight];
     request(h + kFlight, next);
 #pragma unroll
     for (int j = 0; j < kFlight; ++j) {
       if (h + j >= h1) break;
-      float v[8];
-      widen_unit(x[j], v);
-      turn_unit(v, split, c, s);
-      store_unit(h + j < a.n_heads ? qo + (h + j) * a.q_out.head : ko + (h + j - a.n_heads) * a.k_out.head, u, split, a.rope.n_pairs, v);
+      Unit<T> out = turned_unit(x[j], split, c, s);
+      if (some) put_back(out, x[j], split, pairs_of(c));
+      store_unit(at_out(h + j), split, a.rope.n_pairs, out);
       x[j] = next[j];
     }
   }
