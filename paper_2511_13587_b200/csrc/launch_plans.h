@@ -4,6 +4,12 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#ifdef __CUDACC__
+#define VVS_HOST_DEVICE __host__ __device__      // (a kernel does the same arithmetic)
+#else
+#define VVS_HOST_DEVICE
+#endif
+
 namespace vvs {
 
 // ---- projections with folded epilogues, proj_tc.cu -----------------------------------------------
@@ -342,5 +348,11 @@ inline int tree_walk_parts(int vocab, int n_images, int n_sms) {
   while (S > 1 && (long long)n_images * S > (S == 8 ? n_sms * 30 / 37 : S == 4 ? n_sms * 33 / 37 : n_sms)) S /= 2;
   return S;
 }
+
+// ---- attention over the 8-bit cache, quant_attend.cu ---------------------------------------------
+// Scores of rows whose weights are summed, kept in shared memory: a row's length in floats, 8 more than a multiple of 32 banks, and the bytes
+// of all of them: up to 32 rows of up to 2^30 keys, more than an int holds.
+VVS_HOST_DEVICE inline int quant_score_ld(int keys) { return (keys + 23) / 32 * 32 + 8; }
+VVS_HOST_DEVICE inline long long quant_score_bytes(int rows, int keys) { return (long long)rows * quant_score_ld(keys) * (long long)sizeof(float); }
 
 }  // namespace vvs

@@ -198,11 +198,11 @@ quant_attend_kernel(QAttendArgs a, int tiles_each, int score_bytes) {
   const uint32_t v_next = HD == 128 ? v_lane + 128 : ring + L::kTile + value_at<HD>(2 * c + 1, g >> 1) + (g & 1) * 8;
 
   // scores of the rows whose weights are summed stay in shared memory, if those of all of the CTA's keys fit
-  const int score_ld = (((s1 - s0) * 16 + 23) / 32) * 32 + 8;             // 8 more than a multiple of 32 banks
+  const int score_ld = quant_score_ld((s1 - s0) * 16);
 
   for (int tile = group * tiles_each; tile < min((group + 1) * tiles_each, (rows + L::kRows - 1) / L::kRows); ++tile) {
     const int r0 = tile * L::kRows, summed = min(L::kRows, min(a.mass_rows, n) * share - r0);      // rows 0 .. summed - 1 of the tile
-    const bool keep_scores = summed > 0 && summed * score_ld * 4 <= score_bytes;
+    const bool keep_scores = summed > 0 && quant_score_bytes(summed, (s1 - s0) * 16) <= score_bytes;
     float* held = reinterpret_cast<float*>(smem + L::kScoreAt);
     // requests of the first slices travel while the queries are laid out
 #pragma unroll
@@ -638,8 +638,8 @@ int launch_kernel_of(const QAttendArgs& a, int tiles_each, int groups, int ranks
   // the keys again).  More ranks than the device has room for, to make them fit, cost more than the second walk: 32 sequences of nine
   // rows behind 900 to 2380 keys 179 us so, 347 with sixteen ranks in the place of one.
   const int mass_rows = a.mass_rows < a.n_rows ? a.mass_rows : a.n_rows, share = a.n_heads / a.c.n_heads;
-  const long long summed = (long long)mass_rows * share < L::kRows ? mass_rows * share : L::kRows;
-  const long long want = summed * ((((slices + ranks - 1) / ranks * 16 + 23) / 32) * 32 + 8) * 4;
+  const int summed = (long long)mass_rows * share < L::kRows ? mass_rows * share : L::kRows;
+  const long long want = quant_score_bytes(summed, (slices + ranks - 1) / ranks * 16);
   const int score_bytes = want <= L::kScoreBytes ? (int)want : 0;
   auto kernel = quant_attend_kernel<T, HD, MT, WIDE>;
   if (ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), L::kBytes + L::kScoreBytes) != cudaSuccess) return VVS_ERR_CUDA;
