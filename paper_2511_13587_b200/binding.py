@@ -78,6 +78,11 @@ class vvs_rope_axes(C.Structure):
                 ("halves", C.c_int32)]
 
 
+class _RopeOfRows(vvs_rope_axes):
+    """What make_rope_axes gives: with the block that its positions are of, which the calls compare with theirs."""
+    _fields_ = [("n_seqs", C.c_int32), ("n_rows", C.c_int32)]
+
+
 class vvs_qcache(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "mass", "age")] + \
                [(n, C.c_int32) for n in ("n_seqs", "n_heads", "head_dim", "cap", "block")]
@@ -215,7 +220,7 @@ def vvs_bind_neighbors(ctx: int, row_ptr: torch.Tensor, col: torch.Tensor) -> No
 
 # The calls a decoding loop makes per step are marshalled natively, csrc/binding_native.c (keyword arguments named as
 # the fields of the C structures, `ctx` first; a call through ctypes costs 6-10 us of host time).
-_native.setup(VvsError, torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice)
+_native.setup(VvsError, torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice, torch.Tensor, _RopeOfRows)
 vvs_verify = _native.vvs_verify
 vvs_epilogue = _native.vvs_epilogue
 vvs_decide = _native.vvs_decide
@@ -225,6 +230,7 @@ vvs_feature_cache_store = _native.vvs_feature_cache_store
 vvs_feature_cache_fetch = _native.vvs_feature_cache_fetch
 vvs_skip_decide = _native.vvs_skip_decide
 vvs_select_unverified = _native.vvs_select_unverified
+make_rope_axes = _native.make_rope_axes
 vvs_rotate_axes = _native.vvs_rotate_axes
 vvs_quant_cache_append = _native.vvs_quant_cache_append
 vvs_quant_cache_attend = _native.vvs_quant_cache_attend
@@ -245,23 +251,21 @@ def make_fcache(feat: torch.Tensor, fpos: torch.Tensor, newest: torch.Tensor) ->
     return fc
 
 
-def make_rope_axes(inv_freq: torch.Tensor, axis: torch.Tensor, pos: torch.Tensor, halves: bool = False) -> vvs_rope_axes:
-    """inv_freq float32 [n_pairs], axis int32 [n_pairs], pos int32 [n_axes, n_seqs, n_rows] (CUDA tensors)."""
-    r = vvs_rope_axes(_ptr(inv_freq), _ptr(axis), _ptr(pos), int(pos.shape[0]), int(inv_freq.shape[0]), 1 if halves else 0)
-    r._keep = (inv_freq, axis, pos)
-    return r
-
-
 def make_qcache(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, mass: torch.Tensor | None = None,
                 age: torch.Tensor | None = None) -> vvs_qcache:
     """k, v [n_seqs, n_heads, cap, head_dim] of one byte, k_scale, v_scale float32 [n_seqs, n_heads, cap / block],
     mass float32 and age int32 [n_seqs, n_heads, cap] (CUDA tensors, contiguous)."""
-    for name, t, shape, size in (("k", k, k.shape, 1), ("v", v, k.shape, 1), ("k_scale", k_scale, k_scale.shape, 4),
-                                 ("v_scale", v_scale, k_scale.shape, 4), ("mass", mass, k.shape[:3], 4), ("age", age, k.shape[:3], 4)):
-        if t is not None and (not t.is_contiguous() or t.shape != shape or t.element_size() != size):
-            raise ValueError(f"{name}: expected a contiguous tensor {tuple(shape)} of {size}-byte elements")
+    f32, i32 = torch.float32, torch.int32
+    for name, t, shape, dtype in (("k", k, k.shape, None), ("v", v, k.shape, None), ("k_scale", k_scale, k_scale.shape, f32),
+                                  ("v_scale", v_scale, k_scale.shape, f32), ("mass", mass, k.shape[:3], f32), ("age", age, k.shape[:3], i32)):
+        if t is None:
+            continue
+        if not t.is_contiguous() or t.shape != shape or (t.dtype != dtype if dtype else t.element_size() != 1):
+            raise ValueError(f"{name}: expected a contiguous tensor {tuple(shape)} of {dtype or 'one-byte elements'}")
     if k.dim() != 4 or k_scale.shape[:2] != k.shape[:2] or k_scale.dim() != 3 or k_scale.shape[2] < 1 or k.shape[2] % k_scale.shape[2]:
         raise ValueError("k_scale: expected [n_seqs, n_heads, cap / block]")
+    if not all(t.is_cuda for t in (k, v, k_scale, v_scale, mass, age) if t is not None):
+        raise ValueError("expected CUDA tensors")
     qc = vvs_qcache(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), _ptr(mass), _ptr(age), int(k.shape[0]), int(k.shape[1]),
                     int(k.shape[3]), int(k.shape[2]), int(k.shape[2] // k_scale.shape[2]))
     qc._keep = (k, v, k_scale, v_scale, mass, age)

@@ -5,12 +5,14 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <stddef.h>
+#include <stdint.h>
+#include <stdio.h>
 #include <string.h>
 
 #include "vvs.h"
 
 static PyObject *g_error, *g_raw_stream, *g_get_device;   /* VvsError; torch's current raw stream and device */
-static PyObject *s_data_ptr, *s_shape, *s_cuda_stream, *s_stride, *s_element_size;
+static PyObject *s_data_ptr, *s_shape, *s_cuda_stream, *s_keep;
 
 /* tensor (or integer address, or None) -> address; -1 with an exception set on failure */
 static int to_ptr(PyObject* o, void** out) {
@@ -333,105 +335,239 @@ static PyObject* py_select(FAST) {
 }
 
 /* ---- 8-bit cache and rotation with several axes ------------------------------------------------------------------ */
+/* What a tensor is, by the C interface that torch.Tensor offers for it (__dlpack_c_exchange_api__ of DLPack 1.3; the layouts are that
+ * standard's).  One call of some 40 ns; each of data_ptr(), shape, stride() and is_contiguous() costs more, and these entry points look at
+ * up to nine tensors of a call that takes 6 us. */
+enum { kInt = 0, kUint = 1, kFloat = 2, kBfloat = 4, kDeviceCuda = 2 };
+typedef struct {
+  void* data;
+  int32_t device, device_id, ndim;
+  uint8_t code, bits;
+  uint16_t lanes;
+  int64_t *shape, *strides;
+  uint64_t byte_offset;
+} TensorView;
+typedef struct {
+  uint32_t major, minor;
+  void *older, *allocate, *managed_from, *managed_to;
+  int (*view)(void* tensor, TensorView* out);
+  void* work_stream;
+} ExchangeApi;
+static const ExchangeApi* g_exchange;
+static PyObject *g_tensor, *g_rope;              /* torch.Tensor; the class of make_rope_axes' results */
+
+static int look(PyObject* o, const char* name, TensorView* v) {
+  if (!PyObject_TypeCheck(o, (PyTypeObject*)g_tensor)) {
+    PyErr_Format(PyExc_TypeError, "%s: expected a tensor", name);
+    return -1;
+  }
+  if (g_exchange->view(o, v) < 0) return -1;
+  v->data = (char*)v->data + v->byte_offset;
+  return 0;
+}
+/* vvs_rope_axes, and of which block its positions are */
+typedef struct {
+  vvs_rope_axes r;
+  int32_t n_seqs, n_rows;                        /* -1: a structure that the caller has made */
+} RopeAxes;
+
 typedef struct {
   vvs_ctx* ctx;
   PyObject *qc, *rope, *q, *k, *v, *q_out, *k_out, *out;
-  void *cache_len, *row_count, *row_index, *next_age, *first_slot, *visible, *lse, *mass_out, *age_out, *new_len, *kept, *stream;
-  int32_t mass_rows, max_len, keep, n_sink, n_recent;
+  PyObject *cache_len, *row_count, *row_index, *next_age, *first_slot, *visible, *lse, *mass_out, *age_out, *new_len, *kept;
+  PyObject *inv_freq, *axis, *pos;
+  void* stream;
+  const char* elsewhere;                         /* a tensor that is not on a CUDA device */
+  int32_t mass_rows, max_len, keep, n_sink, n_recent, halves;
   float scale, mass_decay;
 } Frame3;
+
+/* A contiguous array of 32-bit numbers (kind kInt: with or without a sign, kFloat), or an address that the caller answers for, or nothing: of
+ * as many elements as the dimensions say, or flat and longer (n_dims 0: of any, where the library refuses what the dimensions come from). */
+static int array_of(Frame3* f, PyObject* o, const char* name, int kind, int n_dims, const int64_t* dims, void** out) {
+  if (!o || o == Py_None || PyLong_Check(o)) return o ? to_ptr(o, out) : 0;
+  TensorView v;
+  if (look(o, name, &v) < 0) return -1;
+  const char* type = kind == kFloat ? "float32" : "int32";
+  if (v.bits != 32 || v.lanes != 1 || (kind == kFloat ? v.code != kFloat : v.code != kInt && v.code != kUint)) {
+    PyErr_Format(PyExc_ValueError, "%s: expected %s elements", name, type);
+    return -1;
+  }
+  int64_t count = 1, side = 1;
+  int dense = 1;
+  for (int i = 0; i < n_dims; ++i) count *= dims[i];
+  for (int i = v.ndim - 1; i >= 0; --i) {
+    dense = dense && (v.shape[i] <= 1 || !v.strides || v.strides[i] == side);
+    side *= v.shape[i];
+  }
+  if (n_dims && side != count && !(v.ndim == 1 && side > count)) {
+    char text[128] = "";
+    for (int i = 0, at = 0; i < n_dims && at < 100; ++i) at += snprintf(text + at, sizeof(text) - at, "%s%lld", i ? ", " : "", (long long)dims[i]);
+    PyErr_Format(PyExc_ValueError, "%s: expected %s [%s]", name, type, text);
+    return -1;
+  }
+  if (!dense) {
+    PyErr_Format(PyExc_ValueError, "%s: expected a contiguous tensor", name);
+    return -1;
+  }
+  *out = v.data;
+  if (v.device != kDeviceCuda) f->elsewhere = name;
+  return 0;
+}
+/* asked once all the tensors of a call are known to be what they should be */
+static int all_on_device(const Frame3* f) {
+  if (!f->elsewhere) return 0;
+  PyErr_Format(PyExc_ValueError, "%s: expected a CUDA tensor", f->elsewhere);
+  return -1;
+}
+
 #define H(f) offsetof(Frame3, f)
 static Param rotate_params[] = {
     {"ctx", 'c', 1, H(ctx)}, {"rope", 'o', 1, H(rope)}, {"q", 'o', 1, H(q)}, {"q_out", 'o', 1, H(q_out)}, {"k", 'o', 0, H(k)},
     {"k_out", 'o', 0, H(k_out)}, {"stream", 's', 0, H(stream)}};
 static Param append_params[] = {
-    {"ctx", 'c', 1, H(ctx)}, {"qc", 'o', 1, H(qc)}, {"k", 'o', 1, H(k)}, {"v", 'o', 1, H(v)}, {"cache_len", 'p', 1, H(cache_len)},
-    {"rope", 'o', 0, H(rope)}, {"q", 'o', 0, H(q)}, {"q_out", 'o', 0, H(q_out)}, {"row_count", 'p', 0, H(row_count)},
-    {"row_index", 'p', 0, H(row_index)}, {"next_age", 'p', 0, H(next_age)}, {"stream", 's', 0, H(stream)}};
+    {"ctx", 'c', 1, H(ctx)}, {"qc", 'o', 1, H(qc)}, {"k", 'o', 1, H(k)}, {"v", 'o', 1, H(v)}, {"cache_len", 'o', 1, H(cache_len)},
+    {"rope", 'o', 0, H(rope)}, {"q", 'o', 0, H(q)}, {"q_out", 'o', 0, H(q_out)}, {"row_count", 'o', 0, H(row_count)},
+    {"row_index", 'o', 0, H(row_index)}, {"next_age", 'o', 0, H(next_age)}, {"stream", 's', 0, H(stream)}};
 static Param attend_params[] = {
-    {"ctx", 'c', 1, H(ctx)}, {"qc", 'o', 1, H(qc)}, {"q", 'o', 1, H(q)}, {"out", 'o', 1, H(out)}, {"cache_len", 'p', 1, H(cache_len)},
-    {"row_count", 'p', 0, H(row_count)}, {"first_slot", 'p', 0, H(first_slot)}, {"visible", 'p', 0, H(visible)},
-    {"lse", 'p', 0, H(lse)}, {"scale", 'f', 0, H(scale)}, {"mass_rows", 'i', 0, H(mass_rows)}, {"mass_decay", 'f', 0, H(mass_decay)},
+    {"ctx", 'c', 1, H(ctx)}, {"qc", 'o', 1, H(qc)}, {"q", 'o', 1, H(q)}, {"out", 'o', 1, H(out)}, {"cache_len", 'o', 1, H(cache_len)},
+    {"row_count", 'o', 0, H(row_count)}, {"first_slot", 'o', 0, H(first_slot)}, {"visible", 'o', 0, H(visible)},
+    {"lse", 'o', 0, H(lse)}, {"scale", 'f', 0, H(scale)}, {"mass_rows", 'i', 0, H(mass_rows)}, {"mass_decay", 'f', 0, H(mass_decay)},
     {"max_len", 'i', 0, H(max_len)}, {"stream", 's', 0, H(stream)}};
 static Param evict_params[] = {
-    {"ctx", 'c', 1, H(ctx)}, {"qc", 'o', 1, H(qc)}, {"cache_len", 'p', 1, H(cache_len)}, {"keep", 'i', 1, H(keep)},
-    {"n_sink", 'i', 1, H(n_sink)}, {"n_recent", 'i', 1, H(n_recent)}, {"next_age", 'p', 1, H(next_age)}, {"mass_out", 'p', 1, H(mass_out)},
-    {"age_out", 'p', 1, H(age_out)}, {"new_len", 'p', 1, H(new_len)}, {"kept", 'p', 1, H(kept)}, {"stream", 's', 0, H(stream)}};
+    {"ctx", 'c', 1, H(ctx)}, {"qc", 'o', 1, H(qc)}, {"cache_len", 'o', 1, H(cache_len)}, {"keep", 'i', 1, H(keep)},
+    {"n_sink", 'i', 1, H(n_sink)}, {"n_recent", 'i', 1, H(n_recent)}, {"next_age", 'o', 1, H(next_age)}, {"mass_out", 'o', 1, H(mass_out)},
+    {"age_out", 'o', 1, H(age_out)}, {"new_len", 'o', 1, H(new_len)}, {"kept", 'o', 1, H(kept)}, {"stream", 's', 0, H(stream)}};
+static Param rope_params[] = {{"inv_freq", 'o', 1, H(inv_freq)}, {"axis", 'o', 1, H(axis)}, {"pos", 'o', 1, H(pos)}, {"halves", 'b', 0, H(halves)}};
 
 /* a tensor [n_seqs, n_rows, n_heads, head_dim] whose last dimension lies side by side, of the context's type; dims: its sizes, checked where
  * they are not 0 */
-static int heads_of(PyObject* t, const char* name, const vvs_ctx* ctx, vvs_heads* out, int32_t dims[4]) {
-  int32_t got[4];
-  if (shape_of(t, 4, got) < 0 || to_ptr(t, &out->data) < 0) return -1;
-  for (int i = 0; i < 4; ++i) {
-    if (dims[i] && dims[i] != got[i]) {
-      PyErr_Format(PyExc_ValueError, "%s: dimension %d is %d, expected %d", name, i, got[i], dims[i]);
-      return -1;
-    }
-    dims[i] = got[i];
-  }
-  PyObject* size = PyObject_CallMethodNoArgs(t, s_element_size);
-  if (!size) return -1;
-  const long es = PyLong_AsLong(size);
-  Py_DECREF(size);
-  if (es == -1 && PyErr_Occurred()) return -1;
-  if (ctx && es != vvs_element_bytes(ctx)) {
-    PyErr_Format(PyExc_ValueError, "%s: elements of %ld bytes, the context's have %d", name, es, vvs_element_bytes(ctx));
+static int heads_of(Frame3* f, PyObject* t, const char* name, vvs_heads* out, int32_t dims[4]) {
+  TensorView v;
+  if (look(t, name, &v) < 0) return -1;
+  if (v.ndim != 4) {
+    PyErr_Format(PyExc_ValueError, "%s: expected a tensor of 4 dimensions", name);
     return -1;
   }
-  PyObject* st = PyObject_CallMethodNoArgs(t, s_stride);
-  if (!st) return -1;
-  long long s[4] = {0, 0, 0, 1};
-  int rc = PyTuple_Check(st) && PyTuple_GET_SIZE(st) == 4 ? 0 : -1;
-  for (int i = 0; i < 4 && rc == 0; ++i) {
-    s[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(st, i));
-    if (s[i] == -1 && PyErr_Occurred()) rc = -1;
+  for (int i = 0; i < 4; ++i) {
+    if ((dims[i] && dims[i] != v.shape[i]) || v.shape[i] > INT32_MAX) {
+      PyErr_Format(PyExc_ValueError, "%s: dimension %d is %lld, expected %d", name, i, (long long)v.shape[i], dims[i]);
+      return -1;
+    }
+    dims[i] = (int32_t)v.shape[i];
   }
-  Py_DECREF(st);
-  if (rc == 0 && s[3] != 1 && got[3] > 1) {
+  const int wide = f->ctx && vvs_element_bytes(f->ctx) == 4;
+  if (f->ctx && (v.code != (wide ? kFloat : kBfloat) || v.bits != (wide ? 32 : 16) || v.lanes != 1)) {
+    PyErr_Format(PyExc_ValueError, "%s: expected %s elements, the context's", name, wide ? "float32" : "bfloat16");
+    return -1;
+  }
+  if (v.strides && v.strides[3] != 1 && v.shape[3] > 1) {
     PyErr_Format(PyExc_ValueError, "%s: the elements of a head do not lie side by side", name);
-    rc = -1;
+    return -1;
   }
-  out->seq = s[0];
-  out->row = s[1];
-  out->head = s[2];
-  return rc;
+  out->data = v.data;
+  out->head = v.strides ? v.strides[2] : v.shape[3];
+  out->row = v.strides ? v.strides[1] : out->head * v.shape[2];
+  out->seq = v.strides ? v.strides[0] : out->row * v.shape[1];
+  if (v.device != kDeviceCuda) f->elsewhere = name;
+  return 0;
 }
 static int given(PyObject* o) { return o && o != Py_None; }
+
+/* the structure behind make_rope_axes' result, or one that the caller has made; its positions have to be those of the call's rows */
+static int rope_of(PyObject* o, int32_t n_seqs, int32_t n_rows, RopeAxes* out) {
+  Py_buffer b;
+  if (PyObject_GetBuffer(o, &b, PyBUF_SIMPLE) < 0) return -1;
+  const Py_ssize_t len = b.len;
+  out->n_seqs = out->n_rows = -1;
+  if (len == (Py_ssize_t)sizeof(RopeAxes) || len == (Py_ssize_t)sizeof(vvs_rope_axes)) memcpy(out, b.buf, len);
+  PyBuffer_Release(&b);
+  if (len != (Py_ssize_t)sizeof(RopeAxes) && len != (Py_ssize_t)sizeof(vvs_rope_axes)) {
+    PyErr_SetString(PyExc_TypeError, "expected a vvs_rope_axes");
+    return -1;
+  }
+  if (out->n_rows != -1 && (out->n_seqs != n_seqs || out->n_rows != n_rows)) {
+    PyErr_Format(PyExc_ValueError, "rope: positions of %d sequences and %d rows, the call has %d and %d", out->n_seqs, out->n_rows, n_seqs, n_rows);
+    return -1;
+  }
+  return 0;
+}
+static PyObject* py_rope(FAST) {
+  (void)self;
+  Frame3 f = {0};
+  if (PARSE("make_rope_axes", rope_params, N(rope_params)) < 0) return NULL;
+  TensorView freq, pos;
+  if (look(f.inv_freq, "inv_freq", &freq) < 0 || look(f.pos, "pos", &pos) < 0) return NULL;
+  if (freq.ndim != 1 || pos.ndim != 3 || freq.shape[0] > INT32_MAX || pos.shape[0] > INT32_MAX || pos.shape[1] > INT32_MAX ||
+      pos.shape[2] > INT32_MAX) {
+    PyErr_SetString(PyExc_ValueError, "expected inv_freq [n_pairs], axis [n_pairs] and pos [n_axes, n_seqs, n_rows]");
+    return NULL;
+  }
+  const int64_t pairs[1] = {freq.shape[0]}, where[3] = {pos.shape[0], pos.shape[1], pos.shape[2]};
+  void *p_freq = NULL, *p_axis = NULL, *p_pos = NULL;
+  if (array_of(&f, f.inv_freq, "inv_freq", kFloat, 1, pairs, &p_freq) < 0 || array_of(&f, f.axis, "axis", kInt, 1, pairs, &p_axis) < 0 ||
+      array_of(&f, f.pos, "pos", kInt, 3, where, &p_pos) < 0 || all_on_device(&f) < 0)
+    return NULL;
+  const RopeAxes r = {{p_freq, p_axis, p_pos, (int32_t)where[0], (int32_t)pairs[0], f.halves != 0}, (int32_t)where[1], (int32_t)where[2]};
+  PyObject* made = PyObject_CallNoArgs(g_rope);
+  if (!made) return NULL;
+  Py_buffer b;
+  PyObject* keep = NULL;
+  int rc = PyObject_GetBuffer(made, &b, PyBUF_WRITABLE);
+  if (rc == 0) {
+    if (b.len == (Py_ssize_t)sizeof(r)) memcpy(b.buf, &r, sizeof(r));
+    else rc = -1, PyErr_SetString(PyExc_SystemError, "the class of make_rope_axes' results has another layout");
+    PyBuffer_Release(&b);
+  }
+  if (rc == 0) {
+    keep = PyTuple_Pack(3, f.inv_freq, f.axis, f.pos);
+    rc = keep ? PyObject_SetAttr(made, s_keep, keep) : -1;
+    Py_XDECREF(keep);
+  }
+  if (rc < 0) Py_CLEAR(made);
+  return made;
+}
 
 static PyObject* py_rotate(FAST) {
   (void)self;
   Frame3 f = {0};
-  vvs_rope_axes rope;
+  RopeAxes rope;
   vvs_heads q, q_out, k, k_out;
   int32_t d[4] = {0}, e[4] = {0};
-  if (PARSE("vvs_rotate_axes", rotate_params, N(rotate_params)) < 0 || struct_of(f.rope, &rope, sizeof(rope), "vvs_rope_axes") < 0 ||
-      heads_of(f.q, "q", f.ctx, &q, d) < 0 || heads_of(f.q_out, "q_out", f.ctx, &q_out, d) < 0)
+  if (PARSE("vvs_rotate_axes", rotate_params, N(rotate_params)) < 0 || heads_of(&f, f.q, "q", &q, d) < 0 ||
+      heads_of(&f, f.q_out, "q_out", &q_out, d) < 0 || rope_of(f.rope, d[0], d[1], &rope) < 0)
     return NULL;
   const int two = given(f.k), two_out = given(f.k_out);
   e[0] = d[0], e[1] = d[1], e[3] = d[3];
-  if (two && heads_of(f.k, "k", f.ctx, &k, e) < 0) return NULL;
-  if (two_out && heads_of(f.k_out, "k_out", f.ctx, &k_out, e) < 0) return NULL;
-  CALL("vvs_rotate_axes", vvs_rotate_axes(f.ctx, &rope, d[0], d[1], d[2], e[2], d[3], &q, &q_out, two ? &k : NULL,
+  if (two && heads_of(&f, f.k, "k", &k, e) < 0) return NULL;
+  if ((two_out && heads_of(&f, f.k_out, "k_out", &k_out, e) < 0) || all_on_device(&f) < 0) return NULL;
+  CALL("vvs_rotate_axes", vvs_rotate_axes(f.ctx, &rope.r, d[0], d[1], d[2], e[2], d[3], &q, &q_out, two ? &k : NULL,
                                           two_out ? &k_out : NULL, f.stream));
 }
 static PyObject* py_append(FAST) {
   (void)self;
   Frame3 f = {0};
   vvs_qcache qc;
-  vvs_rope_axes rope;
+  RopeAxes rope;
   vvs_heads q, q_out, k, v;
   if (PARSE("vvs_quant_cache_append", append_params, N(append_params)) < 0 || struct_of(f.qc, &qc, sizeof(qc), "vvs_qcache") < 0)
     return NULL;
   int32_t d[4] = {qc.n_seqs, 0, qc.n_heads, qc.head_dim}, e[4] = {0};
-  if (heads_of(f.k, "k", f.ctx, &k, d) < 0 || heads_of(f.v, "v", f.ctx, &v, d) < 0) return NULL;
+  if (heads_of(&f, f.k, "k", &k, d) < 0 || heads_of(&f, f.v, "v", &v, d) < 0) return NULL;
   const int turn = given(f.rope), also_q = given(f.q), also_out = given(f.q_out);
-  if (turn && struct_of(f.rope, &rope, sizeof(rope), "vvs_rope_axes") < 0) return NULL;
+  if (turn && rope_of(f.rope, d[0], d[1], &rope) < 0) return NULL;
   e[0] = d[0], e[1] = d[1], e[3] = d[3];
-  if (also_q && heads_of(f.q, "q", f.ctx, &q, e) < 0) return NULL;
-  if (also_out && heads_of(f.q_out, "q_out", f.ctx, &q_out, e) < 0) return NULL;
+  if (also_q && heads_of(&f, f.q, "q", &q, e) < 0) return NULL;
+  if (also_out && heads_of(&f, f.q_out, "q_out", &q_out, e) < 0) return NULL;
+  const int64_t seqs[2] = {d[0], d[1]};
+  void *cache_len = NULL, *row_count = NULL, *row_index = NULL, *next_age = NULL;
+  if (array_of(&f, f.cache_len, "cache_len", kInt, 1, seqs, &cache_len) < 0 ||
+      array_of(&f, f.row_count, "row_count", kInt, 1, seqs, &row_count) < 0 ||
+      array_of(&f, f.row_index, "row_index", kInt, also_q ? 0 : 2, seqs, &row_index) < 0 ||
+      array_of(&f, f.next_age, "next_age", kInt, 1, seqs, &next_age) < 0 || all_on_device(&f) < 0)
+    return NULL;
   CALL("vvs_quant_cache_append",
-       vvs_quant_cache_append(f.ctx, &qc, &k, &v, f.cache_len, d[1], f.row_count, f.row_index, f.next_age, turn ? &rope : NULL, e[2],
+       vvs_quant_cache_append(f.ctx, &qc, &k, &v, cache_len, d[1], row_count, row_index, next_age, turn ? &rope.r : NULL, e[2],
                               also_q ? &q : NULL, also_out ? &q_out : NULL, f.stream));
 }
 static PyObject* py_attend(FAST) {
@@ -443,10 +579,17 @@ static PyObject* py_attend(FAST) {
   if (PARSE("vvs_quant_cache_attend", attend_params, N(attend_params)) < 0 || struct_of(f.qc, &qc, sizeof(qc), "vvs_qcache") < 0)
     return NULL;
   int32_t d[4] = {qc.n_seqs, 0, 0, qc.head_dim};
-  if (heads_of(f.q, "q", f.ctx, &q, d) < 0 || heads_of(f.out, "out", f.ctx, &out, d) < 0) return NULL;
-  CALL("vvs_quant_cache_attend",
-       vvs_quant_cache_attend(f.ctx, &qc, &q, &out, f.cache_len, d[1], d[2], f.row_count, f.first_slot, f.visible, f.lse, f.scale,
-                              f.mass_rows, f.mass_decay, f.max_len, f.stream));
+  if (heads_of(&f, f.q, "q", &q, d) < 0 || heads_of(&f, f.out, "out", &out, d) < 0) return NULL;
+  const int64_t seqs[3] = {d[0], d[1], d[2]};
+  void *cache_len = NULL, *row_count = NULL, *first_slot = NULL, *visible = NULL, *lse = NULL;
+  if (array_of(&f, f.cache_len, "cache_len", kInt, 1, seqs, &cache_len) < 0 ||
+      array_of(&f, f.row_count, "row_count", kInt, 1, seqs, &row_count) < 0 ||
+      array_of(&f, f.first_slot, "first_slot", kInt, 1, seqs, &first_slot) < 0 ||
+      array_of(&f, f.visible, "visible", kInt, d[1] > 32 ? 0 : 2, seqs, &visible) < 0 ||
+      array_of(&f, f.lse, "lse", kFloat, 3, seqs, &lse) < 0 || all_on_device(&f) < 0)
+    return NULL;
+  CALL("vvs_quant_cache_attend", vvs_quant_cache_attend(f.ctx, &qc, &q, &out, cache_len, d[1], d[2], row_count, first_slot, visible, lse, f.scale,
+                                                        f.mass_rows, f.mass_decay, f.max_len, f.stream));
 }
 static PyObject* py_evict(FAST) {
   (void)self;
@@ -454,18 +597,36 @@ static PyObject* py_evict(FAST) {
   vvs_qcache qc;
   if (PARSE("vvs_quant_cache_evict", evict_params, N(evict_params)) < 0 || struct_of(f.qc, &qc, sizeof(qc), "vvs_qcache") < 0)
     return NULL;
-  CALL("vvs_quant_cache_evict", vvs_quant_cache_evict(f.ctx, &qc, f.cache_len, f.keep, f.n_sink, f.n_recent, f.next_age, f.mass_out,
-                                                      f.age_out, f.new_len, f.kept, f.stream));
+  const int64_t slots[3] = {qc.n_seqs, qc.n_heads, qc.cap}, stay[3] = {qc.n_seqs, qc.n_heads, f.keep};
+  void *cache_len = NULL, *next_age = NULL, *mass_out = NULL, *age_out = NULL, *new_len = NULL, *kept = NULL;
+  if (array_of(&f, f.cache_len, "cache_len", kInt, 1, slots, &cache_len) < 0 || array_of(&f, f.next_age, "next_age", kInt, 1, slots, &next_age) < 0 ||
+      array_of(&f, f.mass_out, "mass_out", kFloat, 3, slots, &mass_out) < 0 || array_of(&f, f.age_out, "age_out", kInt, 3, slots, &age_out) < 0 ||
+      array_of(&f, f.new_len, "new_len", kInt, 1, slots, &new_len) < 0 ||
+      array_of(&f, f.kept, "kept", kInt, f.keep < 1 || f.keep > qc.cap ? 0 : 3, stay, &kept) < 0 || all_on_device(&f) < 0)
+    return NULL;
+  CALL("vvs_quant_cache_evict", vvs_quant_cache_evict(f.ctx, &qc, cache_len, f.keep, f.n_sink, f.n_recent, next_age, mass_out, age_out, new_len, kept,
+                                                      f.stream));
 }
 
-/* setup(VvsError, current_raw_stream, current_device) */
+/* setup(VvsError, current_raw_stream, current_device, Tensor, class of make_rope_axes' results) */
 static PyObject* py_setup(PyObject* self, PyObject* args) {
   (void)self;
-  PyObject *e, *r, *d;
-  if (!PyArg_ParseTuple(args, "OOO", &e, &r, &d)) return NULL;
+  PyObject *e, *r, *d, *t, *rope;
+  if (!PyArg_ParseTuple(args, "OOOO!O", &e, &r, &d, &PyType_Type, &t, &rope)) return NULL;
+  PyObject* api = PyObject_GetAttrString(t, "__dlpack_c_exchange_api__");
+  if (!api) return NULL;
+  g_exchange = PyCapsule_GetPointer(api, "dlpack_exchange_api");        /* (torch's own, for as long as it is loaded) */
+  Py_DECREF(api);
+  if (!g_exchange) return NULL;
+  if (g_exchange->major != 1 || g_exchange->minor < 3) {
+    PyErr_Format(PyExc_ImportError, "torch offers tensors by DLPack %u.%u, expected 1.3 or a later 1.x", g_exchange->major, g_exchange->minor);
+    return NULL;
+  }
   Py_XSETREF(g_error, Py_NewRef(e));
   Py_XSETREF(g_raw_stream, Py_NewRef(r));
   Py_XSETREF(g_get_device, Py_NewRef(d));
+  Py_XSETREF(g_tensor, Py_NewRef(t));
+  Py_XSETREF(g_rope, Py_NewRef(rope));
   Py_RETURN_NONE;
 }
 
@@ -489,6 +650,9 @@ static PyMethodDef methods[] = {
     FN("vvs_select_unverified", py_select,
        "Sec. 4.2 / Eq. 3: uniform draw of one candidate path per image, cut to gamma tokens: vvs_select_unverified(ctx, paths, "
        "path_len, uniforms, out_path, out_gamma, out_tokens, stream=None)."),
+    FN("make_rope_axes", py_rope,
+       "make_rope_axes(inv_freq, axis, pos, halves=False): inv_freq float32 [n_pairs], axis int32 [n_pairs], pos int32 [n_axes, n_seqs, n_rows] "
+       "(CUDA tensors, contiguous), for calls of n_seqs sequences and n_rows rows."),
     FN("vvs_rotate_axes", py_rotate,
        "vvs_rotate_axes(ctx, rope, q, q_out, k=None, k_out=None, stream=None): q, k [n_seqs, n_rows, heads, head_dim], any strides of "
        "whole 16 bytes but the last; rope from make_rope_axes."),
@@ -512,12 +676,11 @@ PyMODINIT_FUNC PyInit__native(void) {
   s_data_ptr = PyUnicode_InternFromString("data_ptr");
   s_shape = PyUnicode_InternFromString("shape");
   s_cuda_stream = PyUnicode_InternFromString("cuda_stream");
-  s_stride = PyUnicode_InternFromString("stride");
-  s_element_size = PyUnicode_InternFromString("element_size");
+  s_keep = PyUnicode_InternFromString("_keep");
 #define I(ps) intern(ps, N(ps)) < 0
-  if (!s_data_ptr || !s_shape || !s_cuda_stream || !s_stride || !s_element_size || I(verify_params) || I(epilogue_params) || I(decide_params) || I(noalloc_params) ||
+  if (!s_data_ptr || !s_shape || !s_cuda_stream || !s_keep || I(verify_params) || I(epilogue_params) || I(decide_params) || I(noalloc_params) ||
       I(reset_params) || I(store_params) || I(fetch_params) || I(skip_params) || I(select_params) || I(rotate_params) ||
-      I(append_params) || I(attend_params) || I(evict_params))
+      I(append_params) || I(attend_params) || I(evict_params) || I(rope_params))
     return NULL;
   return PyModule_Create(&module);
 }
