@@ -428,7 +428,8 @@ typedef struct vvs_qcache {
  * cache_len[b] slots that sequence b holds: slots cache_len[b] .. of every head, mass 0, age next_age[b] + row (next_age:
  * device int32 [n_seqs]; NULL = cache_len).  With `rope` the keys are turned first, in float32, and so are the q heads
  * (n_heads of them) into q_out, where q is given.  row_index (device int32 [n_seqs][n_rows], or NULL): row j is source row
- * row_index[b][j], with its position; after a tree call the rows on the accepted path are put again, at the block's start.
+ * row_index[b][j], with its position; after a tree call the rows on the accepted path are put again, at the block's start (weights that the
+ * rows have got since go with them only if the caller moves them: mass is 0 after this call too, or, with qc->mass NULL, as it was).
  * A block's scale starts from its new rows where they begin the block, and else only grows; then the rows before them
  * are rounded again.  Sequences that do not fit (cache_len + rows > cap) are skipped: VVS_DEV_CACHE_OVERFLOW. */
 int vvs_quant_cache_append(vvs_ctx* ctx, const vvs_qcache* qc, const vvs_heads* k, const vvs_heads* v, const int32_t* cache_len,

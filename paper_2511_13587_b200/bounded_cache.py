@@ -3,11 +3,11 @@ place of the bf16 cache of `vvs_verify`.
 
 Per layer and step: `append` turns the block's queries and keys to their positions (time, row, column, ..) and puts keys and values behind
 the cache, `attend` reads it and adds the weights that every key got.  `commit` moves the fill levels behind the accepted rows
-(a tree's rows on the accepted path are put again, side by side, layer by layer).  `make_room` brings every layer back to the budget
+(a tree's rows on the accepted path are put again, side by side, layer by layer, and keep the weights that `attend` gave them).  `make_room` brings every layer back to the budget
 when a block could pass the capacity: the tokens of the least accumulated weight leave, the first and the last ones never.  Positions
 are the caller's: a token keeps the ones it was turned to, whatever slot it lies in.
 
-All work runs in the library's kernels on the current stream; nothing here waits for the device.  `python -m
+The library's kernels do the work on the current stream, a few small torch operations a step the bookkeeping; nothing here waits for the device.  `python -m
 paper_2511_13587_b200.bounded_cache` decodes a synthetic clip through it."""
 from __future__ import annotations
 
@@ -40,11 +40,16 @@ class BoundedCache:
         self.turn = 0                                          # which of the two buffers holds the weights and ages
         self.fill_most = 0                                     # no sequence's fill is above it
         self.evictions = 0
+        self._rows = torch.arange(max_rows, device=device)
+        self._picked = None                                    # of a tree that was put again: the block's rows, and their new places,
+        self._picked_by = -1                                   # .. and the layer that was the first
         self._caches = [[self._cache(layer, turn) for layer in range(n_layers)] for turn in range(2)]
+        self._unweighted = [self._cache(layer, None) for layer in range(n_layers)]
 
-    def _cache(self, layer: int, turn: int):
-        return vb.make_qcache(self.k[layer], self.v[layer], self.k_scale[layer], self.v_scale[layer], self.mass[turn][layer],
-                              self.age[turn][layer])
+    def _cache(self, layer: int, turn: int | None):
+        """Without a turn, keys and values alone: an append leaves weights and ages as they are."""
+        more = () if turn is None else (self.mass[turn][layer], self.age[turn][layer])
+        return vb.make_qcache(self.k[layer], self.v[layer], self.k_scale[layer], self.v_scale[layer], *more)
 
     def rope(self, pos: torch.Tensor):
         """pos int32 [axes, n_seqs, rows] of a block, for the layers' `append` calls."""
@@ -52,6 +57,8 @@ class BoundedCache:
 
     def append(self, layer: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, rope, row_count: torch.Tensor | None = None) -> torch.Tensor:
         """A block's rows [n_seqs, rows, heads, head_dim], as the projection left them; returns the turned queries (a buffer of this object)."""
+        if layer == self._picked_by:                           # (a block in the place of one that was put again and not committed)
+            self._picked, self._picked_by = None, -1
         turned = self.rotated[:, :q.shape[1]]
         vb.vvs_quant_cache_append(self.ctx, self._caches[self.turn][layer], k, v, self.fill, rope=rope, q=q, q_out=turned, row_count=row_count,
                                   next_age=self.next_age)
@@ -65,12 +72,25 @@ class BoundedCache:
         return out
 
     def put_again(self, layer: int, k: torch.Tensor, v: torch.Tensor, rope, path: torch.Tensor, n_commit: torch.Tensor) -> None:
-        """After a tree call and before `commit`: the rows path[b, :n_commit[b]] of the block lie side by side behind the cache."""
-        vb.vvs_quant_cache_append(self.ctx, self._caches[self.turn][layer], k, v, self.fill, rope=rope, row_count=n_commit, row_index=path,
+        """After a tree call and before `commit`: the rows path[b, :n_commit[b]] of the block lie side by side behind the cache.  Path and
+        number are the same for all layers; `commit` moves the rows' weights along."""
+        if self._picked is None:
+            rows = self._rows[:path.shape[1]].expand(path.shape)
+            self._picked_by = layer
+            self._picked = torch.stack((torch.where(rows < n_commit.view(-1, 1), path, rows), rows))
+        # (the places have their ages from the block's own append: that of the place, not of the row)
+        vb.vvs_quant_cache_append(self.ctx, self._unweighted[layer], k, v, self.fill, rope=rope, row_count=n_commit, row_index=path,
                                   next_age=self.next_age)
 
     def commit(self, n_commit: torch.Tensor, most: int) -> None:
         """n_commit int32 [n_seqs]: rows of the block that stay, at most `most` of any sequence."""
+        if self._picked is not None:
+            # (places behind the last committed row keep what they have; the bounds are for rows out of range and blocks that did not fit,
+            # which the append has left out and told of)
+            mass = self.mass[self.turn]
+            rows, places = (self._picked + self.fill.view(-1, 1)).clamp_(0, self.cap - 1)[:, None, :, None].expand((2,) + mass.shape[:3] + (-1,))
+            mass.scatter_(3, places, mass.gather(3, rows))
+            self._picked, self._picked_by = None, -1
         self.fill += n_commit
         self.next_age += n_commit
         self.fill_most += most
