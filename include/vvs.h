@@ -452,6 +452,8 @@ int vvs_quant_cache_attend(vvs_ctx* ctx, const vvs_qcache* qc, const vvs_heads* 
                            const uint32_t* visible, float* lse, float scale, int32_t mass_rows, float mass_decay, int32_t max_len,
                            void* stream);
 
+#define VVS_QCACHE_EVICT_CAP 131072 /* most slots of a cache that vvs_quant_cache_evict takes */
+
 /* Brings every sequence to at most `keep` slots: of each head stay the rows of the n_sink first and n_recent last tokens
  * (age < n_sink, age >= next_age[b] - n_recent; n_sink + n_recent <= keep) and, of the others, those of the largest mass,
  * the lower slot first among equals (a NaN counts as the least).  Rows that stay and lie in slots below keep stay there; the
@@ -460,7 +462,7 @@ int vvs_quant_cache_attend(vvs_ctx* ctx, const vvs_qcache* qc, const vvs_heads* 
  * (device [n_seqs][n_heads][cap], other memory than qc's; age_out may be NULL): slots from new_len to cache_len become 0
  * and -1, later ones are not touched.  new_len (device int32 [n_seqs]) = min(cache_len, keep).  kept (device int32
  * [n_seqs][n_heads][keep]): the slot that each slot's row comes from, -1 behind new_len.  next_age NULL = cache_len.
- * A sequence whose cache_len is outside 0 .. cap is skipped: VVS_DEV_CACHE_OVERFLOW.  cap <= 131072. */
+ * A sequence whose cache_len is outside 0 .. cap is skipped: VVS_DEV_CACHE_OVERFLOW.  cap <= VVS_QCACHE_EVICT_CAP. */
 int vvs_quant_cache_evict(vvs_ctx* ctx, const vvs_qcache* qc, const int32_t* cache_len, int32_t keep, int32_t n_sink, int32_t n_recent,
                           const int32_t* next_age, float* mass_out, int32_t* age_out, int32_t* new_len, int32_t* kept, void* stream);
 

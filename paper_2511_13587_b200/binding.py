@@ -29,6 +29,7 @@ VVS_ROPE_NONE, VVS_ROPE_1D, VVS_ROPE_2D_GRID = 0, 1, 2
 VVS_MODE_STRICT, VVS_MODE_RELAXED = 0, 1
 VVS_DEV_BAD_TOKEN, VVS_DEV_CACHE_OVERFLOW, VVS_DEV_BAD_NEIGHBOUR = 1, 2, 4
 VVS_DEV_TIMEOUT, VVS_DEV_FCACHE_MISS, VVS_DEV_BAD_ARG, VVS_DEV_NONFINITE = 8, 16, 32, 64
+VVS_QCACHE_EVICT_CAP = 131072
 
 
 class vvs_model_desc(C.Structure):

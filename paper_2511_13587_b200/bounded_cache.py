@@ -22,8 +22,16 @@ class BoundedCache:
                  halves: bool = False, mass_decay: float = 1.0, dtype: torch.dtype = torch.bfloat16, device: str = "cuda"):
         """`budget` tokens stay after `make_room`; `slack` more may come before it has to run again; a block has at most `max_rows` rows.
         inv_freq float32 and axis int32 [pairs] as for `make_rope_axes`."""
-        if n_sink + n_recent > budget:
+        if min(n_layers, n_seqs, n_kv_heads, budget, max_rows) < 1 or slack < 0 or n_heads < 1 or n_heads % n_kv_heads:
+            raise ValueError("layers, sequences, heads, budget and max_rows have to be positive, slack not negative, n_heads a multiple of n_kv_heads")
+        if block not in (16, 32, 64, 128) or head_dim not in (64, 128):
+            raise ValueError("a block has 16, 32, 64 or 128 slots, a head 64 or 128 elements")
+        if n_sink < 0 or n_recent < 0 or n_sink + n_recent > budget:
             raise ValueError("n_sink + n_recent tokens do not fit the budget")
+        if not 0.0 <= mass_decay < float("inf"):
+            raise ValueError("mass_decay has to be finite and not negative")
+        if -(-(budget + slack + max_rows) // block) * block > vb.VVS_QCACHE_EVICT_CAP:
+            raise ValueError(f"budget + slack + max_rows pass the {vb.VVS_QCACHE_EVICT_CAP} slots that an eviction takes")
         self.ctx, self.n_layers, self.n_seqs, self.n_heads = ctx, n_layers, n_seqs, n_heads
         self.budget, self.max_rows, self.n_sink, self.n_recent, self.mass_decay = budget, max_rows, n_sink, n_recent, mass_decay
         self.inv_freq, self.axis, self.halves = inv_freq, axis, halves

@@ -18,8 +18,6 @@ namespace vvs {
 
 namespace {
 
-constexpr int kMaxCap = 131072;
-
 // larger key, larger weight; a NaN below everything
 __device__ __forceinline__ uint32_t key_of(float w) {
   if (w != w) return 0u;
@@ -395,7 +393,7 @@ __global__ void __launch_bounds__(256) quant_move_kernel(QEvictArgs a, int begin
 }  // namespace
 
 int launch_quant_evict(const QEvictArgs& a, cudaStream_t s) {
-  if (a.c.cap > kMaxCap) return VVS_ERR_SHAPE;
+  if (a.c.cap > VVS_QCACHE_EVICT_CAP) return VVS_ERR_SHAPE;
   // a rank for every 4096 slots, while that does not leave more CTAs than SMs (32 heads of 32K slots: 81 us with four ranks, 140 with
   // eight, whose clusters do not fit all at once)
   const long long items = (long long)a.c.n_seqs * a.c.n_heads;
