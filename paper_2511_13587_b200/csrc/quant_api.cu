@@ -87,7 +87,7 @@ int vvs_quant_cache_append(vvs_ctx* ctx, const vvs_qcache* qc, const vvs_heads* 
   VVS_TRY(check_cache(qc, &a.c));
   if (n_rows < 1 || n_rows > (1 << 24) || (q && n_heads < 1)) return VVS_ERR_SHAPE;
   if (!q) n_heads = 0;
-  if (2 * (int64_t)qc->n_heads + n_heads > 65535) return VVS_ERR_SHAPE;
+  if (2 * (int64_t)qc->n_heads + n_heads > 65535 || (q && (int64_t)qc->n_seqs * n_rows > 0x7fffffff)) return VVS_ERR_SHAPE;
   const int es = is_f32(ctx) ? 4 : 2;
   VVS_TRY(check_heads(k, qc->n_seqs, n_rows, qc->n_heads, es, &a.k));
   VVS_TRY(check_heads(v, qc->n_seqs, n_rows, qc->n_heads, es, &a.v));
@@ -111,8 +111,9 @@ int vvs_quant_cache_attend(vvs_ctx* ctx, const vvs_qcache* qc, const vvs_heads* 
   VVS_TRY(check_cache(qc, &a.c));
   if (!std::isfinite(scale) || !std::isfinite(mass_decay) || mass_decay < 0.f || (mass_rows > 0 && !qc->mass)) return VVS_ERR_INVALID_ARG;
   if (n_rows < 1 || n_heads < 1 || n_heads % qc->n_heads || (visible && n_rows > 32) || mass_rows < 0 || max_len < 0) return VVS_ERR_SHAPE;
-  // tiles of 16 rows at least, one grid row for each tile of a cached head
-  if ((int64_t)n_rows * n_heads > (int64_t)65535 * 16) return VVS_ERR_SHAPE;
+  // one row of the grid for each cached head and tile: of 16 rows where there are no more, else of 32 at least (a tile that is not full: with more
+  // than 16 rows a head, at most 61680 heads are left by the second condition)
+  if (qc->n_heads > 65535 || (int64_t)n_rows * n_heads > (int64_t)65535 * 16) return VVS_ERR_SHAPE;
   const int es = is_f32(ctx) ? 4 : 2;
   VVS_TRY(check_heads(q, qc->n_seqs, n_rows, n_heads, es, &a.q));
   VVS_TRY(check_heads(out, qc->n_seqs, n_rows, n_heads, es, &a.out));
