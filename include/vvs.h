@@ -409,7 +409,7 @@ int vvs_rotate_axes(vvs_ctx* ctx, const vvs_rope_axes* rope, int32_t n_seqs, int
  * for each block of `block` slots of a head: element = code * scale.  vvs_quant_cache_append writes powers of two, the
  * smallest (2^-60 at least) by which a block's largest magnitude is at most 448: a scale that has to grow then changes codes
  * by their exponent, without another rounding of anything but the smallest ones.  vvs_quant_cache_attend takes any positive
- * scales.  Device memory of the caller; what lies behind a sequence's fill level may be anything. */
+ * scales of values from 2^-80 to 2^120, side by side too, and of keys as long as scale * q k_j are float32 numbers.  Device memory of the caller; what lies behind a sequence's fill level may be anything. */
 typedef struct vvs_qcache {
   void* k;          /* e4m3 [n_seqs][n_heads][cap][head_dim], keys after rotation */
   void* v;

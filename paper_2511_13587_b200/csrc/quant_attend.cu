@@ -43,15 +43,6 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t* a, uint32
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
-  const __half2 h = __floats2half2_rn(a, b);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
 // 16 bytes from an address and a constant offset; or `bytes` of them, the rest zeros
 template <int TO, int FROM>
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
@@ -325,8 +316,8 @@ quant_attend_kernel(QAttendArgs a, int tiles_each, int score_bytes) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[mt][j][e] = 0.f;
     }
-    // the weights of a slice's scores, in place of them; MASKED: some row does not see some key
-    auto weights = [&](auto masked, int slice, float ks, float lv, float inv_vs, float (&s)[MT][2][4], uint32_t (&p)[L::kP][MT][4]) {
+    // the weights of a slice's scores, in place of them; MASKED: some row does not see some key; apart: weights may vanish that count
+    auto weights = [&](auto masked, bool apart, int slice, float ks, float lv, float inv_vs, float (&s)[MT][2][4], uint32_t (&p)[L::kP][MT][4]) {
       constexpr bool MASKED = decltype(masked)::value;
       const int slot0 = slice << 4;
 #pragma unroll
@@ -363,7 +354,7 @@ quant_attend_kernel(QAttendArgs a, int tiles_each, int score_bytes) {
           }
           passes = passes || top > kShift + kSlack || (m[mt][i] == -CUDART_INF_F && top > -CUDART_INF_F);
         }
-        if (__any_sync(0xffffffffu, passes)) {               // some row's reference moves up to the slice's largest score
+        if (__any_sync(0xffffffffu, passes || apart)) {      // some row's reference moves up to the slice's largest score
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             float top = fmaxf(fmaxf(s[mt][0][2 * i], s[mt][0][2 * i + 1]), fmaxf(s[mt][1][2 * i], s[mt][1][2 * i + 1]));
@@ -374,13 +365,18 @@ quant_attend_kernel(QAttendArgs a, int tiles_each, int score_bytes) {
             if (up == -CUDART_INF_F) continue;
             const float alpha = none ? 0.f : ex2(-up);
             m[mt][i] = none ? up : m[mt][i] + up;
-            l[mt][i] *= alpha;
+            l[mt][i] = none ? 0.f : times_ex2(l[mt][i], -up);
 #pragma unroll
             for (int e = 0; e < 4; ++e) s[mt][e >> 1][2 * i + (e & 1)] -= up;
 #pragma unroll
             for (int j = 0; j < HD / 8; ++j) {
               o[mt][j][2 * i] *= alpha;
               o[mt][j][2 * i + 1] *= alpha;
+            }
+            if (apart) {
+              const float gone = (gone_weight(s[mt][0][2 * i]) + gone_weight(s[mt][0][2 * i + 1])) +
+                                 (gone_weight(s[mt][1][2 * i]) + gone_weight(s[mt][1][2 * i + 1]));
+              l[mt][i] = fmaf(gone, inv_vs * kGoneDown, l[mt][i]);
             }
           }
           __syncwarp();
@@ -402,6 +398,7 @@ quant_attend_kernel(QAttendArgs a, int tiles_each, int score_bytes) {
         }
       }
     };
+    bool apart = false;                     // a scale was met that is not an ordinary one
     uint32_t at = 0, ahead = (kDepth - 1) * L::kSlot;
     for (int slice = s0 + warp; slice < s1; slice += kWarps) {
       tc::cp_async_wait<kDepth - 2>();
@@ -410,11 +407,12 @@ quant_attend_kernel(QAttendArgs a, int tiles_each, int score_bytes) {
       float s[MT][2][4];
       scores(at, s);
       const float lv = __log2f(vs), inv_vs = __frcp_rn(vs);
+      apart = apart || odd_scale(vs);
       uint32_t p[L::kP][MT][4];
       if ((slice << 4) >= first && (slice << 4) + 16 <= len)
-        weights(std::false_type{}, slice, ks, lv, inv_vs, s, p);
+        weights(std::false_type{}, apart, slice, ks, lv, inv_vs, s, p);
       else
-        weights(std::true_type{}, slice, ks, lv, inv_vs, s, p);
+        weights(std::true_type{}, apart, slice, ks, lv, inv_vs, s, p);
       // values: this lane's keys are 2c, 2c + 1, 8 + 2c, 9 + 2c, its columns g * HD / 8 ..
       uint32_t w[4][HD / 32];
       if (HD == 128) {
@@ -487,13 +485,22 @@ quant_attend_kernel(QAttendArgs a, int tiles_each, int score_bytes) {
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) top = fmaxf(top, ml[(w * L::kRows + r) * 2]);
       float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-      float total = 0.f;
+      float total = 0.f, low = 0.f;
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) {
         const float mw = ml[(w * L::kRows + r) * 2], f = mw == -CUDART_INF_F ? 0.f : ex2(mw - top);
         const float4 x = reinterpret_cast<const float4*>(smem + L::kRingAt + w * L::kRing)[v];
         sum.x = fmaf(x.x, f, sum.x); sum.y = fmaf(x.y, f, sum.y); sum.z = fmaf(x.z, f, sum.z); sum.w = fmaf(x.w, f, sum.w);
         total = fmaf(ml[(w * L::kRows + r) * 2 + 1], f, total);
+        low = fminf(low, mw == -CUDART_INF_F ? 0.f : mw - top);
+      }
+      if (low < -100.f) {
+        total = 0.f;
+#pragma unroll 1
+        for (int w = 0; w < kWarps; ++w) {
+          const float mw = ml[(w * L::kRows + r) * 2];
+          total = add_times_ex2(total, ml[(w * L::kRows + r) * 2 + 1], mw == -CUDART_INF_F ? 0.f : mw - top);
+        }
       }
       reinterpret_cast<float4*>(smem + L::kRingAt)[v] = sum;              // (of warp 0's sums this thread reads no other)
       if (v % (HD / 4) == 0) { tot[2 * r] = top; tot[2 * r + 1] = total; }
@@ -512,7 +519,8 @@ quant_attend_kernel(QAttendArgs a, int tiles_each, int score_bytes) {
         const float mk = tc::ld_cluster_f32(tot_at + 8 * r, k), f = mk == -CUDART_INF_F ? 0.f : ex2(mk - top);
         const float4 x = tc::ld_cluster_f4(sum_at + 16 * v, k);
         sum.x = fmaf(x.x, f, sum.x); sum.y = fmaf(x.y, f, sum.y); sum.z = fmaf(x.z, f, sum.z); sum.w = fmaf(x.w, f, sum.w);
-        total = fmaf(tc::ld_cluster_f32(tot_at + 8 * r + 4, k), f, total);
+        const float lk = tc::ld_cluster_f32(tot_at + 8 * r + 4, k);
+        total = mk == -CUDART_INF_F || mk - top > -100.f ? fmaf(lk, f, total) : add_times_ex2(total, lk, mk - top);
       }
       const bool some = t < n && !(total == 0.f);            // (a NaN among the queries is an answer of NaN)
       const float inv = some ? 1.f / total : 0.f;
@@ -530,7 +538,8 @@ quant_attend_kernel(QAttendArgs a, int tiles_each, int score_bytes) {
         for (int k = 0; k < ranks; ++k) top = fmaxf(top, tc::ld_cluster_f32(tot_at + 8 * tid, k));
         for (int k = 0; k < ranks; ++k) {
           const float mk = tc::ld_cluster_f32(tot_at + 8 * tid, k);
-          total = fmaf(tc::ld_cluster_f32(tot_at + 8 * tid + 4, k), mk == -CUDART_INF_F ? 0.f : ex2(mk - top), total);
+          const float lk = tc::ld_cluster_f32(tot_at + 8 * tid + 4, k);
+          total = add_times_ex2(total, lk, mk == -CUDART_INF_F ? 0.f : mk - top);
         }
         lse2[tid] = total == 0.f ? CUDART_INF_F : top - kShift + log2f(total);
       }

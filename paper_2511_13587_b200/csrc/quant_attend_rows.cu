@@ -38,15 +38,6 @@ constexpr int kTilesEach = 2;                   // of a stream, at least, where 
 constexpr float kShift = 7.f, kMost = 32768.f;   // log2 of a weight at the reference; the most a row's weights of a tile may add up to
 constexpr float kLog2e = 1.4426950408889634f;
 
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
-  const __half2 h = __floats2half2_rn(a, b);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
 // two float32 at a time
 __device__ __forceinline__ uint64_t pair_of(float x, float y) { return (uint64_t)__float_as_uint(x) | (uint64_t)__float_as_uint(y) << 32; }
 __device__ __forceinline__ float low_of(uint64_t v) { return __uint_as_float((uint32_t)v); }
@@ -373,6 +364,7 @@ __global__ void __launch_bounds__(kThreads, 1) quant_attend_rows_kernel(QAttendA
     if (!ok) give_up(i, nt);
   } else {                                                      // ---- scores to weights, sums
     float next_scale = nt > 0 ? scale_of_tile(0) : 1.f;
+    bool odd = false;                                           // this lane has met a scale of values that is not an ordinary one
     float m = -CUDART_INF_F, l = 0.f;                           // (a row that is not there has neither)
     if (nt > 0) ok = tc::warp_wait_or_abort(q_full, 0, abort_flag);
     const float fac = fac_of[mine];
@@ -435,9 +427,11 @@ __global__ void __launch_bounds__(kThreads, 1) quant_attend_rows_kernel(QAttendA
       };
       tile_logs();
       // A sum of at most kMost has no weight beyond it.  Else, and where a row has no reference yet, rows' references move up to their largest
-      // score of the tile, which lies in tensor memory still.
+      // score of the tile, which lies in tensor memory still.  And where scales of
+      // values lie far apart.
       const bool none = live && m == -CUDART_INF_F;
-      bool moves = __any_sync(0xffffffffu, none);
+      odd = odd || ((lane & 4) && odd_scale(scale));
+      bool moves = __any_sync(0xffffffffu, none || odd);
       if (!moves) {
         const float all = powers(inv_vs, s, by_value);
         moves = __any_sync(0xffffffffu, live && !(all <= kMost));
@@ -451,13 +445,23 @@ __global__ void __launch_bounds__(kThreads, 1) quant_attend_rows_kernel(QAttendA
         if (up != -CUDART_INF_F && live) {
           alpha = none ? 0.f : ex2(-up);
           m = none ? up : m + up;
-          l *= alpha;
+          l = none ? 0.f : times_ex2(l, -up);
         } else {
           up = 0.f;
         }
 #pragma unroll
         for (int e = 0; e < kKeys; ++e) s[e] -= up;
-        if (i > 0) {
+        if (__any_sync(0xffffffffu, odd)) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const float inv = __shfl_sync(0xffffffffu, inv_vs, 4 + q) * kGoneDown;
+            float gone = 0.f;
+#pragma unroll
+            for (int e = 16 * q; e < 16 * q + 16; ++e) gone += gone_weight(s[e]);
+            l = fmaf(gone, inv, l);
+          }
+        }
+        if (i > 0 && __any_sync(0xffffffffu, alpha != 1.f)) {
           ok = tc::warp_wait_or_abort(&o_done[(i - 1) & 1], ((i - 1) >> 1) & 1, abort_flag);
           if (!ok) break;
           tc::tc_fence_after();
@@ -532,7 +536,7 @@ __global__ void __launch_bounds__(kThreads, 1) quant_attend_rows_kernel(QAttendA
 #pragma unroll
       for (int st = 0; st < kStreams; ++st) top = fmaxf(top, ml[k][st].x);
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-    float total = 0.f;
+    float total = 0.f, low = 0.f;
 #pragma unroll
     for (int k0 = 0; k0 < kMaxRanks; k0 += kTogether) {
       if (k0 >= ranks) break;
@@ -554,7 +558,15 @@ __global__ void __launch_bounds__(kThreads, 1) quant_attend_rows_kernel(QAttendA
           const float4 y = x[k][st];
           sum.x = fmaf(y.x, f, sum.x); sum.y = fmaf(y.y, f, sum.y); sum.z = fmaf(y.z, f, sum.z); sum.w = fmaf(y.w, f, sum.w);
           total = fmaf(m.y, f, total);
+          low = fminf(low, m.x == -CUDART_INF_F ? 0.f : m.x - top);
         }
+    }
+    if (low < -100.f) {
+      total = 0.f;
+#pragma unroll
+      for (int k = 0; k < kMaxRanks; ++k)
+#pragma unroll
+        for (int st = 0; st < kStreams; ++st) total = add_times_ex2(total, ml[k][st].y, ml[k][st].x == -CUDART_INF_F ? 0.f : ml[k][st].x - top);
     }
     const bool some = t < n && !(total == 0.f);                // (a NaN among the queries is an answer of NaN)
     const float inv = some ? 1.f / total : 0.f;
@@ -580,7 +592,8 @@ __global__ void __launch_bounds__(kThreads, 1) quant_attend_rows_kernel(QAttendA
 #pragma unroll
     for (int k = 0; k < kMaxRanks; ++k)
 #pragma unroll
-      for (int st = 0; st < kStreams; ++st) total = fmaf(ml[k][st].y, ml[k][st].x == -CUDART_INF_F ? 0.f : ex2(ml[k][st].x - top), total);
+      for (int st = 0; st < kStreams; ++st)
+        total = add_times_ex2(total, ml[k][st].y, ml[k][st].x == -CUDART_INF_F ? 0.f : ml[k][st].x - top);
     if (!(total == 0.f)) sub = top - kShift + log2f(total);
   }
   if (MASS) tc::fence_proxy_async();                            // codes come where the sums were

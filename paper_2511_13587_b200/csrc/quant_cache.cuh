@@ -295,4 +295,27 @@ __device__ __forceinline__ uint32_t rescale_e4m3x4(uint32_t w, float f) {
   return to_e4m3x4(lo.x * f, lo.y * f, hi.x * f, hi.y * f);
 }
 
+// ---- weights ----------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+  const __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+// Weights carry their value's scale, a row's sum does not: sum_j w_j / V_b.  Where values' scales lie up to 2^200 apart (a block of zeros has
+// 2^-60, the largest is 2^120), weights of the smaller ones vanish at the row's reference although their keys may have most of the row's softmax.
+// Nothing is lost from the outputs then, next to values so much larger, but it is from the sum.  So where a scale was met that is
+// not an ordinary one, weights that vanish go into the sum from 2^100 times themselves; and sums come to another reference in two steps.
+// Ordinary scales lie within 2^80: a key's weight at its row's reference is 2^(7 - 80) times its share of the softmax at least.
+__device__ __forceinline__ bool odd_scale(float v) { return !(v >= 0x1p-62f && v <= 0x1p18f); }
+constexpr float kGone = -126.f, kGoneUp = 100.f, kGoneDown = 0x1p-100f;
+// 2^(a + 100) if 2^a vanishes, else nothing
+__device__ __forceinline__ float gone_weight(float a) { return a < kGone ? ex2(a + kGoneUp) : 0.f; }
+// x 2^d, y + x 2^d
+__device__ __forceinline__ float times_ex2(float x, float d) { return x * ex2(fmaxf(d, -100.f)) * ex2(fminf(d + 100.f, 0.f)); }
+__device__ __forceinline__ float add_times_ex2(float y, float x, float d) { return fmaf(x * ex2(fmaxf(d, -100.f)), ex2(fminf(d + 100.f, 0.f)), y); }
+
 }  // namespace vvs
