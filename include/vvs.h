@@ -409,7 +409,8 @@ int vvs_rotate_axes(vvs_ctx* ctx, const vvs_rope_axes* rope, int32_t n_seqs, int
  * for each block of `block` slots of a head: element = code * scale.  vvs_quant_cache_append writes powers of two, the
  * smallest (2^-60 at least) by which a block's largest magnitude is at most 448: a scale that has to grow then changes codes
  * by their exponent, without another rounding of anything but the smallest ones.  vvs_quant_cache_attend takes any positive
- * scales of values from 2^-80 to 2^120, side by side too, and of keys as long as scale * q k_j are float32 numbers.  Device memory of the caller; what lies behind a sequence's fill level may be anything. */
+ * scales of values from 2^-80 to 2^120, side by side too, and of keys as long as scale * q k_j are float32 numbers.  Device
+ * memory of the caller; what lies behind a sequence's fill level may be anything. */
 typedef struct vvs_qcache {
   void* k;          /* e4m3 [n_seqs][n_heads][cap][head_dim], keys after rotation */
   void* v;
@@ -425,13 +426,15 @@ typedef struct vvs_qcache {
 } vvs_qcache;
 
 /* Puts n_rows rows (row_count[b] of them where row_count, device int32 [n_seqs], is given) of k and v behind the
- * cache_len[b] slots that sequence b holds: slots cache_len[b] .. of every head, mass 0, age next_age[b] + row (next_age:
- * device int32 [n_seqs]; NULL = cache_len).  With `rope` the keys are turned first, in float32, and so are the q heads
- * (n_heads of them) into q_out, where q is given.  row_index (device int32 [n_seqs][n_rows], or NULL): row j is source row
- * row_index[b][j], with its position; after a tree call the rows on the accepted path are put again, at the block's start (weights that the
- * rows have got since go with them only if the caller moves them: mass is 0 after this call too, or, with qc->mass NULL, as it was).
- * A block's scale starts from its new rows where they begin the block, and else only grows; then the rows before them
- * are rounded again.  Sequences that do not fit (cache_len + rows > cap) are skipped: VVS_DEV_CACHE_OVERFLOW. */
+ * cache_len[b] slots that sequence b holds: slots cache_len[b] .. of every head, mass 0, age next_age[b] + row
+ * (next_age: device int32 [n_seqs]; NULL = cache_len).  With `rope` the keys are turned first, in float32, and so are
+ * the q heads (n_heads of them) into q_out, where q is given.  row_index (device int32 [n_seqs][n_rows], or NULL): row j
+ * is source row row_index[b][j], with its position; after a tree call the rows on the accepted path are put again, at
+ * the block's start (weights that the rows have got since go with them only if the caller moves them: mass is 0 after
+ * this call too or, with qc->mass NULL, as it was).  An infinity is stored as the largest code, a NaN as 0:
+ * VVS_DEV_NONFINITE.  A block's scale starts from its new rows where they begin the block, and else only grows; then the
+ * rows before them are rounded again.  Sequences that do not fit (cache_len + rows > cap) are skipped:
+ * VVS_DEV_CACHE_OVERFLOW. */
 int vvs_quant_cache_append(vvs_ctx* ctx, const vvs_qcache* qc, const vvs_heads* k, const vvs_heads* v, const int32_t* cache_len,
                            int32_t n_rows, const int32_t* row_count, const int32_t* row_index, const int32_t* next_age,
                            const vvs_rope_axes* rope, int32_t n_heads, const vvs_heads* q, const vvs_heads* q_out, void* stream);
@@ -446,7 +449,11 @@ int vvs_quant_cache_append(vvs_ctx* ctx, const vvs_qcache* qc, const vvs_heads* 
  * mass_rows > 0: qc->mass[slot] = mass_decay * mass[slot] + the sum of p over the first mass_rows rows and the query heads
  * of each cached head, for all slots below cache_len + row_count; mass_decay 0 overwrites.  The order of every sum is fixed.
  * scale <= 0 stands for 1 / sqrt(head_dim).  max_len: an upper bound of cache_len + n_rows that the caller knows, by which
- * the work is split (results do not depend on its truth, their speed does); 0 = cap. */
+ * the work is split (results depend on it by the rounding of sums that are split otherwise, on its truth not at all, their
+ * speed does); 0 = cap.
+ * Scores, maxima and sums are float32; tensor cores take halves: a row's queries times a power of two, its weights with 11 bits
+ * (an output is within 2^-11 of sum p |v| beside T's own rounding).  Float32 contexts split queries into three halves and
+ * weights into two (22 bits). */
 int vvs_quant_cache_attend(vvs_ctx* ctx, const vvs_qcache* qc, const vvs_heads* q, const vvs_heads* out, const int32_t* cache_len,
                            int32_t n_rows, int32_t n_heads, const int32_t* row_count, const int32_t* first_slot,
                            const uint32_t* visible, float* lse, float scale, int32_t mass_rows, float mass_decay, int32_t max_len,
@@ -455,14 +462,16 @@ int vvs_quant_cache_attend(vvs_ctx* ctx, const vvs_qcache* qc, const vvs_heads* 
 #define VVS_QCACHE_EVICT_CAP 131072 /* most slots of a cache that vvs_quant_cache_evict takes */
 
 /* Brings every sequence to at most `keep` slots: of each head stay the rows of the n_sink first and n_recent last tokens
- * (age < n_sink, age >= next_age[b] - n_recent; n_sink + n_recent <= keep) and, of the others, those of the largest mass,
- * the lower slot first among equals (a NaN counts as the least).  Rows that stay and lie in slots below keep stay there; the
- * others, in the order of their slots, fill the slots that became free.  A block's scale grows to the largest that its new
- * rows come with.  Reads qc->mass and qc->age (NULL: age = slot), writes them for the new order to mass_out and age_out
- * (device [n_seqs][n_heads][cap], other memory than qc's; age_out may be NULL): slots from new_len to cache_len become 0
- * and -1, later ones are not touched.  new_len (device int32 [n_seqs]) = min(cache_len, keep).  kept (device int32
- * [n_seqs][n_heads][keep]): the slot that each slot's row comes from, -1 behind new_len.  next_age NULL = cache_len.
- * A sequence whose cache_len is outside 0 .. cap is skipped: VVS_DEV_CACHE_OVERFLOW.  cap <= VVS_QCACHE_EVICT_CAP. */
+ * (age < n_sink, age >= next_age[b] - n_recent; n_sink + n_recent <= keep) and, of the others, those of the largest
+ * mass, the lower slot first among equals (a NaN counts as the least).  Rows that stay and lie in slots below keep stay
+ * there; the others, in the order of their slots, fill the slots that became free.  A block's scale grows to the largest
+ * that its new rows come with.  Reads qc->mass and qc->age (NULL: age = slot), writes them for the new order to mass_out
+ * and age_out (device [n_seqs][n_heads][cap], other memory than qc's; age_out may be NULL): slots from new_len to
+ * cache_len become 0 and -1, later ones are not touched.  Slots below a first_slot of vvs_quant_cache_attend count like
+ * any other: a sequence that is padded on the left must not be evicted (its padding would stay as its first tokens, and
+ * others move into it).  new_len (device int32 [n_seqs]) = min(cache_len, keep).  kept (device int32
+ * [n_seqs][n_heads][keep]): the slot that each slot's row comes from, -1 behind new_len.  next_age NULL = cache_len. A
+ * sequence whose cache_len is outside 0 .. cap is skipped: VVS_DEV_CACHE_OVERFLOW.  cap <= VVS_QCACHE_EVICT_CAP. */
 int vvs_quant_cache_evict(vvs_ctx* ctx, const vvs_qcache* qc, const int32_t* cache_len, int32_t keep, int32_t n_sink, int32_t n_recent,
                           const int32_t* next_age, float* mass_out, int32_t* age_out, int32_t* new_len, int32_t* kept, void* stream);
 

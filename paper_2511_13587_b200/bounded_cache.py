@@ -1,14 +1,14 @@
 """A decoder's key / value cache in 8 bits that never grows beyond a bound: what a program decoding long images or video keeps in the
 place of the bf16 cache of `vvs_verify`.
 
-Per layer and step: `append` turns the block's queries and keys to their positions (time, row, column, ..) and puts keys and values behind
-the cache, `attend` reads it and adds the weights that every key got.  `commit` moves the fill levels behind the accepted rows
-(a tree's rows on the accepted path are put again, side by side, layer by layer, and keep the weights that `attend` gave them).  `make_room` brings every layer back to the budget
-when a block could pass the capacity: the tokens of the least accumulated weight leave, the first and the last ones never.  Positions
-are the caller's: a token keeps the ones it was turned to, whatever slot it lies in.
+Per layer and step: `append` turns the block's queries and keys to their positions (time, row, column, ..) and puts keys and values behind the
+cache, `attend` reads it and adds the weights that every key got.  `commit` moves the fill levels behind the accepted rows (a tree's rows on the
+accepted path are put again, side by side, layer by layer, and keep the weights that `attend` gave them).  `make_room` brings every layer back to
+the budget when a block could pass the capacity: the tokens of the least accumulated weight leave, the first and the last ones never.  Positions
+are the caller's: a token keeps the ones it was turned to, whatever slot it lies in.  Sequences begin in slot 0: there is no padding on the left.
 
-The library's kernels do the work on the current stream, a few small torch operations a step the bookkeeping; nothing here waits for the device.  `python -m
-paper_2511_13587_b200.bounded_cache` decodes a synthetic clip through it."""
+The library's kernels do the work on the current stream, a few small torch operations a step the bookkeeping; nothing here waits for the device.
+`python -m paper_2511_13587_b200.bounded_cache` decodes a synthetic clip through it."""
 from __future__ import annotations
 
 import torch

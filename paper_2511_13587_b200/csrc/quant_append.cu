@@ -6,9 +6,9 @@
 // Few rows: a warp has a head, so that nothing but the table of sines is waited for by a whole CTA, and queries are heads like others.
 // Prompts: a CTA has a head.
 //
-// Eight prompts of 1301 rows, 32 + 2 x 8 heads of 128: 73 us for 235 MB, 50 % of a copy's rate: the queries' launch 29 of them, the keys' and
-// values' 44, in which half of the issue slots turn, compare, scale and round (two passes over what a head's rows hold in registers).  32 blocks
-// of 9 rows, 32 + 2 x 32 heads: 9.3 us; two of them of 3 x 20 heads of 64: 6.6, as long as the call itself.
+// Eight prompts of 1301 rows, 32 + 2 x 8 heads of 128: 71.5 us for 235 MB, 51 % of a copy's rate: the queries' launch 29 of them, the keys' and
+// values' 42, in which half of the issue slots turn, compare, scale and round (two passes over what a head's rows hold in registers).  32 blocks
+// of 9 rows, 32 + 2 x 32 heads: 8.7 us; two of them of 3 x 20 heads of 64: 5.5, where a call that does next to nothing takes 4.1.
 #include "quant_cache.cuh"
 
 namespace vvs {
@@ -288,7 +288,7 @@ int launch_rows(const QAppendArgs& a, cudaStream_t s) {
   const int chunks = (a.n_rows + blk - 2) / blk + 1, items = 2 * a.c.n_heads + (FEW ? a.n_heads : 0);
   const size_t smem = a.rope.inv_freq ? (size_t)rows * (HD / 2) * sizeof(float2) : 0;
   // Heads of a CTA: few rows, one for each warp (fewer where that leaves SMs without work).  Prompts, as many as leave every SM six
-  // CTAs (73 us; two 77, sixteen 72): the cosines and sines of the rows serve all of them.
+  // CTAs (71.5 us; two 75.8, sixteen 70.4): the cosines and sines of the rows serve all of them.
   const long long each_head = (long long)chunks * a.c.n_seqs;
   int each;
   if (FEW) {
@@ -305,8 +305,8 @@ int launch_rows(const QAppendArgs& a, cudaStream_t s) {
   return e == cudaSuccess ? VVS_OK : VVS_ERR_CUDA;
 }
 
-// A call of few rows, or of small blocks, is one launch: two blocks of 9 rows 6.6 us, a CTA for a head and the queries by themselves 8.5; 32
-// blocks 9.3 against 24.3.  Of prompts the queries have a launch of their own, whose threads keep their
+// A call of few rows, or of small blocks, is one launch: two blocks of 9 rows 5.5 us, a CTA for a head and the queries by themselves 7.2; 32
+// blocks 8.6 against 25.0.  Of prompts the queries have a launch of their own, whose threads keep their
 // angles in registers and have no block to wait for.
 template <typename T, int HD>
 int launch_hd(const QAppendArgs& a, cudaStream_t s) {

@@ -18,11 +18,11 @@
 // The weights' sums need the whole row's maximum and sum: from the scores, kept in shared memory, where those of the CTA's keys fit, else by a
 // second walk over the CTA's keys (from L2).
 //
-// 32 sequences of nine rows behind 900 to 2380 keys, 32 heads of 128: 118 us, 3.8 TB/s, 59 % of a copy's rate.  Every key is turned to halves
+// 32 sequences of nine rows behind 900 to 2380 keys, 32 heads of 128: 119 us, 3.8 TB/s, 59 % of a copy's rate.  Every key is turned to halves
 // by the warp that multiplies it, for 16 rows of which nine are there: a slice takes a warp 3400 cycles beside eleven others on its SM,
 // conversions, the two products and the weights in one chain.  Left out, measured: slices of 32 keys (116 where 16 took 107), rings of two, four
-// and five slices (108 and more), eight warps a CTA (138), keys as 8-bit operands of mma.sync (131).  One token of a float32 context: 7 us, the
-// call itself 6; nine rows behind 311 keys, weights summed: 9.5.
+// and five slices (108 and more), eight warps a CTA (138), keys as 8-bit operands of mma.sync (131).  One token of a float32 context: 7.1 us, a
+// call that does next to nothing 4.1; nine rows behind 311 keys, weights summed: 9.4.
 #include <type_traits>
 
 #include "quant_cache.cuh"
@@ -701,7 +701,7 @@ template <typename T, int HD>
 int launch_hd(const QAttendArgs& a, cudaStream_t s) {
   const int rows = a.n_rows * (a.n_heads / a.c.n_heads);
   // Many rows of bf16 contexts: the kernel with 128 of them a tile.  Two trees of 27 rows x 4 heads behind 31K keys 79 us against 158 here (four
-  // tiles of 32 rows turn every key four times), with their first rows' weights summed 167 against 447; 36 rows 75 against 101.  Up to 32 rows
+  // tiles of 32 rows turn every key four times), with their first rows' weights summed 163 against 447; 36 rows 75 against 101.  Up to 32 rows
   // only where its items are on the device at once and no weights are summed: 20 rows, 300 to 500 keys, 140 items 13.0 us against 15.2,
   // 160 items 20.6 against 18.2; 100 items behind 300 keys, weights summed, 17.8 against 13.5.  Summed rows have to lie in its first
   // tile.  (Rows by 2^32 / share: exact up to 2^20 rows of 4096 heads.)

@@ -14,11 +14,11 @@
 // Weights summed for eviction (of rows of the first tile): with the rows' sums at hand the keys go through the first product once more, and
 // the lanes' weights are added over the rows by shuffles.
 //
-// Two sequences, 27 rows x 4 heads over each of 8 cached heads of 128, 30K to 33K keys: 80 us, 346 TFLOP/s (bytes alone are 20 us, the products
-// 16); 167 with the first rows' weights summed.  A stream needs 3000 cycles for 64 keys: the row's lane 1200 for its powers, sums and halves, the rest waits of one stage
-// for another; an SM issues in 47 of 100 cycles, its tensor pipe is busy in 27.  Clusters of six CTAs with an SM each are what the
-// device holds for 16 items at once: 96 of 148 SMs work (eight: 15 clusters, one waits for another to end, 124 us).  One CTA with one stream,
-// twice on an SM, is packed on half of the SMs: 135 us.
+// Two sequences, 27 rows x 4 heads over each of 8 cached heads of 128, 30K to 33K keys: 79 us, 350 TFLOP/s (bytes alone are 20 us, the products
+// 16); 163 with the first rows' weights summed.  A stream needs 3000 cycles for 64 keys: the row's lane 1200 for its powers, sums and halves, the
+// rest waits of one stage for another; an SM issues in 42 of 100 cycles, its tensor pipe is busy in 30.  Clusters of six CTAs with an SM each are
+// what the device holds for 16 items at once: 96 of 148 SMs work (eight: 15 clusters, one waits for another to end, 124 us).  One CTA with one
+// stream, twice on an SM, is packed on half of the SMs: 135 us.
 #include <type_traits>
 
 #include "quant_cache.cuh"
@@ -126,7 +126,8 @@ struct Layout {
   static constexpr int kBars = 2 * kStages + 8;                 // of a stream; and one of the queries
   static constexpr int kNeed = kBarAt + (kStreams * kBars + 1) * 8 + 16 + 1024;       // (the base is brought to a multiple of 1024)
   // One CTA on an SM: it has all of the tensor memory, S twice 64 columns and O HD of them for each stream.  And none of another kernel that
-  // multiplies there: two clusters that hold tensor memory on one SM each and wait for it on the other's would wait forever.
+  // multiplies there: two clusters that hold tensor memory on one SM each and wait for it on the other's would wait forever.  (Its 512 threads have
+  // all registers of an SM beside that, 128 each.)
   static constexpr int kBytes = kNeed < 200 * 1024 ? 200 * 1024 : kNeed;
   static constexpr int kColumns = 512, kStreamColumns = 256, kOut = 2 * kKeys;
   static_assert(kStreamBytes >= kRows * HD * 4, "a stream's sums fit");
@@ -427,8 +428,7 @@ __global__ void __launch_bounds__(kThreads, 1) quant_attend_rows_kernel(QAttendA
       };
       tile_logs();
       // A sum of at most kMost has no weight beyond it.  Else, and where a row has no reference yet, rows' references move up to their largest
-      // score of the tile, which lies in tensor memory still.  And where scales of
-      // values lie far apart.
+      // score of the tile, which lies in tensor memory still.  And where scales of values lie far apart.
       const bool none = live && m == -CUDART_INF_F;
       odd = odd || ((lane & 4) && odd_scale(scale));
       bool moves = __any_sync(0xffffffffu, none || odd);

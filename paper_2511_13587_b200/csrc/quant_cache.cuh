@@ -165,7 +165,7 @@ __device__ __forceinline__ void turn_unit(float (&x)[8], bool split, const float
 }
 // In the place of a cosine: the pair stays as it is.  It is left alone, not turned by an angle of 0: next to an infinity,
 // x * 1 + inf * 0 would be a NaN.  A unit of which only some pairs are turned (the last pair lies in it, or one of an unknown axis) has a
-// path of its own: selections in the loops over whole units cost an append of prompts 83 us in the place of 71.
+// path of its own: selections in the loops over whole units cost an append of prompts 83 us in the place of 71.5.
 constexpr float kStays = 2.f;
 // Which of a unit's four pairs are turned: bit i is pair 4u + i.
 __device__ __forceinline__ uint32_t pairs_of(const float (&c)[4]) {

@@ -3,7 +3,7 @@
 // four angles once and goes through a group of heads with them: sines and cosines of float32 angles (some 40 instructions each)
 // cost more than the elements' traffic if every head computes its own.
 //
-// 5460 rows of 32 + 8 heads of 128: 23.7 us, 4.7 TB/s (73 % of a copy's rate); 18 rows of 40 heads of 64 6 us, as long as the call itself.
+// 5460 rows of 32 + 8 heads of 128: 23.8 us, 4.7 TB/s (73 % of a copy's rate); 18 rows of 40 heads of 64 4.2 us, as long as the call itself.
 #include "quant_cache.cuh"
 
 namespace vvs {
@@ -11,7 +11,7 @@ namespace vvs {
 namespace {
 
 constexpr int kThreads = 128;
-constexpr int kFlight = 4;   // heads whose elements are on their way together (23.7 us; one 30.1; eight, with their registers, 33.5)
+constexpr int kFlight = 4;   // heads whose elements are on their way together (23.7 us; one 30.9; eight, with their registers, 33.2)
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 7) rotate_axes_kernel(RotateArgs a, int heads_each) {
@@ -70,7 +70,7 @@ template <typename T>
 int launch_rotate_axes(const RotateArgs& a, cudaStream_t s) {
   const long long threads = (long long)a.n_seqs * a.n_rows * (a.hd / 8);
   const int heads = a.n_heads + a.n_kv_heads;
-  // as many groups of heads as fill the device with threads (2048 an SM): 18 rows 5.9 us, with all heads in one thread 9.6
+  // as many groups of heads as fill the device with threads (2048 an SM): 18 rows 4.2 us, with all heads in one thread 9.6
   const long long room = (long long)a.n_sms * 2048;
   int groups = (int)((room + threads - 1) / threads);
   groups = groups < 1 ? 1 : groups > heads ? heads : groups;
