@@ -451,10 +451,10 @@ int vvs_quant_cache_append(vvs_ctx* ctx, const vvs_qcache* qc, const vvs_heads* 
  * scale <= 0 stands for 1 / sqrt(head_dim).  max_len: an upper bound of cache_len + n_rows that the caller knows, by which
  * the work is split (results depend on it by the rounding of sums that are split otherwise, on its truth not at all, their
  * speed does); 0 = cap.
- * Scores, maxima and sums are float32; tensor cores take halves: a row's queries times a power of two, its weights with 11
- * bits down to 2^-21 of the row's largest and as multiples of 2^-31 of it below.  An output is within 2^-11 of sum p |v| and,
- * where almost all of the softmax is on keys whose values are 0, 2^-31 of sum |v|, beside T's own rounding.  Float32 contexts
- * split queries into three halves and weights into two (22 bits). */
+ * Scores, maxima and sums are float32; tensor cores take halves: a row's queries times a power of two, and its weights p_j
+ * times their value's scale with 11 bits down to 2^-21 of the row's largest, below as multiples of 2^-31 of it.  An output is
+ * within 2^-11 of sum p |v| beside that and T's own rounding.  Float32 contexts split queries into three halves and weights
+ * into two (22 bits). */
 int vvs_quant_cache_attend(vvs_ctx* ctx, const vvs_qcache* qc, const vvs_heads* q, const vvs_heads* out, const int32_t* cache_len,
                            int32_t n_rows, int32_t n_heads, const int32_t* row_count, const int32_t* first_slot,
                            const uint32_t* visible, float* lse, float scale, int32_t mass_rows, float mass_decay, int32_t max_len,
