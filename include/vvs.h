@@ -67,7 +67,8 @@ enum {
   VVS_DEV_FCACHE_MISS = 16,   /* feature-cache fetch asked for a position not in the ring */
   VVS_DEV_BAD_ARG = 32,       /* n_draft / gamma / n_store (and the device arguments of the 8-bit cache and of
                                  vvs_rotate_axes) outside its documented range */
-  VVS_DEV_NONFINITE = 64      /* vvs_quant_cache_append met an infinity (stored as the largest code) or a NaN (stored as 0) */
+  VVS_DEV_NONFINITE = 64      /* vvs_quant_cache_append or one of the calls that make 8-bit rows and weights met an infinity (stored as
+                                 the largest code) or a NaN (stored as 0) */
 };
 
 typedef struct vvs_ctx vvs_ctx;
@@ -475,6 +476,55 @@ int vvs_quant_cache_attend(vvs_ctx* ctx, const vvs_qcache* qc, const vvs_heads* 
  * sequence whose cache_len is outside 0 .. cap is skipped: VVS_DEV_CACHE_OVERFLOW.  cap <= VVS_QCACHE_EVICT_CAP. */
 int vvs_quant_cache_evict(vvs_ctx* ctx, const vvs_qcache* qc, const int32_t* cache_len, int32_t keep, int32_t n_sink, int32_t n_recent,
                           const int32_t* next_age, float* mass_out, int32_t* age_out, int32_t* new_len, int32_t* kept, void* stream);
+
+/* ---- Rows and weights in 8 bits, and their product ----------------------------------------------------------------------
+ * (No counterpart in the paper: a decoder's projections beside the 8-bit cache, at half the bytes of bf16 weights.)  Elements are e4m3
+ * codes (as in the cache) times a float32 scale: of a row, one for each block of 128 columns; of a weight matrix, one for each block of
+ * 128 x 128.  The last block of a row, and of a matrix's rows, may be short.  The calls that make them take the smallest scale by which a
+ * block's largest finite magnitude is at most 448, max / 448, 2^-60 at least; an infinity is stored as the largest code, a NaN as 0:
+ * VVS_DEV_NONFINITE.  Columns are multiples of 16; rows that are written do not overlap (stride >= columns).  The calls need a context for its storage type T and its status word only; calls on
+ * different streams may share it. */
+
+/* Rows of T: row t begins at data + t * row (elements; data is 16-byte aligned, the stride of more than one row a multiple of 16 bytes). */
+typedef struct vvs_rows {
+  void* data;
+  int64_t row;
+} vvs_rows;
+
+/* Rows in 8 bits: the codes of row t begin at codes + t * row (bytes, a multiple of 16 where there is more than one row). */
+typedef struct vvs_qrows {
+  void* codes;
+  int64_t row;
+  float* scale;   /* [n_rows][(n_cols + 127) / 128], 4-byte aligned */
+} vvs_qrows;
+
+/* A weight matrix [n_rows = outputs, n_cols = inputs] in 8 bits, rows as those of vvs_qrows. */
+typedef struct vvs_qweight {
+  void* codes;
+  int64_t row;
+  float* scale;   /* [(n_rows + 127) / 128][(n_cols + 127) / 128], 4-byte aligned */
+  int32_t n_rows; /* at most 65535 * 128 */
+  int32_t n_cols;
+} vvs_qweight;
+
+/* s = x + residual (NULL: x), y = s / sqrt(mean(s^2) + eps) * weight (T [n_cols]), out = y in 8 bits.  sum_out = s and norm_out = y, both
+ * rounded to T, where they are given.  Sums and products are float32; y comes from s before it is rounded.  sum_out and norm_out may be x
+ * or residual, where address and stride are the same; other overlaps are not allowed.  A row whose squares' sum is no finite float32 sets
+ * VVS_DEV_NONFINITE.  n_cols <= 32768; n_rows times the blocks of a row at most 2^30, here and below. */
+int vvs_norm_quant(vvs_ctx* ctx, int32_t n_rows, int32_t n_cols, const vvs_rows* x, const vvs_rows* residual, const void* weight, float eps,
+                   const vvs_rows* sum_out, const vvs_rows* norm_out, const vvs_qrows* out, void* stream);
+
+/* out = x in 8 bits or, with gate, gate / (1 + exp(-gate)) * x (SwiGLU; gate and x may be halves of one projection's rows). */
+int vvs_rows_quant(vvs_ctx* ctx, int32_t n_rows, int32_t n_cols, const vvs_rows* x, const vvs_rows* gate, const vvs_qrows* out, void* stream);
+
+/* out = w (T [n_rows, n_cols]) in 8 bits; what out points to is written. */
+int vvs_weight_quant(vvs_ctx* ctx, const vvs_rows* w, const vvs_qweight* out, void* stream);
+
+/* out[m, n] = sum over blocks b of a_scale[m, b] * w_scale[n / 128, b] * sum over b's columns of a[m, k] * w[n, k]: out T [n_rows,
+ * w->n_rows], a [n_rows, w->n_cols].  Any scales whose products with the sums are float32 numbers; codes that are e4m3's NaN give NaN.
+ * A block's sum is taken by the tensor cores in float32, blocks are added in float32; the order is fixed for a size.  Rows of out need no
+ * alignment but the first's (16 bytes). */
+int vvs_block_matmul(vvs_ctx* ctx, int32_t n_rows, const vvs_qrows* a, const vvs_qweight* w, const vvs_rows* out, void* stream);
 
 /* Synchronise `stream`, copy the device status word to *out_bits (VVS_DEV_* bits) and clear
  * it.  Returns VVS_ERR_DEVICE_TIMEOUT / VVS_ERR_DEVICE_BOUNDS if such a bit was set. */

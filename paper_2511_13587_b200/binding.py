@@ -89,6 +89,23 @@ class vvs_qcache(C.Structure):
                [(n, C.c_int32) for n in ("n_seqs", "n_heads", "head_dim", "cap", "block")]
 
 
+class vvs_rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("row", C.c_int64)]
+
+
+class vvs_qrows(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("row", C.c_int64), ("scale", C.c_void_p)]
+
+
+class vvs_qweight(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("row", C.c_int64), ("scale", C.c_void_p), ("n_rows", C.c_int32), ("n_cols", C.c_int32)]
+
+
+class _WeightOnDevice(vvs_qweight):
+    """What make_qweight gives: with the device that it lies on, which the calls compare with theirs."""
+    _fields_ = [("device", C.c_int32)]
+
+
 _P = C.c_void_p
 lib.vvs_create.argtypes = [C.POINTER(vvs_model_desc), C.POINTER(_P)]
 lib.vvs_destroy.argtypes = [_P]
@@ -120,6 +137,11 @@ lib.vvs_quant_cache_append.argtypes = [_P, C.POINTER(vvs_qcache), C.POINTER(vvs_
 lib.vvs_quant_cache_attend.argtypes = [_P, C.POINTER(vvs_qcache), C.POINTER(vvs_heads), C.POINTER(vvs_heads), _P, C.c_int32, C.c_int32,
                                        _P, _P, _P, _P, C.c_float, C.c_int32, C.c_float, C.c_int32, _P]
 lib.vvs_quant_cache_evict.argtypes = [_P, C.POINTER(vvs_qcache), _P, C.c_int32, C.c_int32, C.c_int32, _P, _P, _P, _P, _P, _P]
+lib.vvs_norm_quant.argtypes = [_P, C.c_int32, C.c_int32, C.POINTER(vvs_rows), C.POINTER(vvs_rows), _P, C.c_float, C.POINTER(vvs_rows),
+                               C.POINTER(vvs_rows), C.POINTER(vvs_qrows), _P]
+lib.vvs_rows_quant.argtypes = [_P, C.c_int32, C.c_int32, C.POINTER(vvs_rows), C.POINTER(vvs_rows), C.POINTER(vvs_qrows), _P]
+lib.vvs_weight_quant.argtypes = [_P, C.POINTER(vvs_rows), C.POINTER(vvs_qweight), _P]
+lib.vvs_block_matmul.argtypes = [_P, C.c_int32, C.POINTER(vvs_qrows), C.POINTER(vvs_qweight), C.POINTER(vvs_rows), _P]
 lib.vvs_element_bytes.argtypes = [_P]
 lib.vvs_device_status.argtypes = [_P, _P, C.POINTER(C.c_int32)]
 lib.vvs_last_launch_count.argtypes = [_P]
@@ -131,7 +153,8 @@ for _n in ("vvs_create", "vvs_destroy", "vvs_workspace_bytes", "vvs_bind_weights
            "vvs_bind_neighbors", "vvs_verify", "vvs_epilogue", "vvs_feature_cache_reset",
            "vvs_feature_cache_store", "vvs_feature_cache_fetch", "vvs_device_status",
            "vvs_last_launch_count", "vvs_profile_enable", "vvs_profile_read", "vvs_rotate_axes", "vvs_quant_cache_append",
-           "vvs_quant_cache_attend", "vvs_quant_cache_evict", "vvs_element_bytes"):
+           "vvs_quant_cache_attend", "vvs_quant_cache_evict", "vvs_element_bytes", "vvs_norm_quant", "vvs_rows_quant", "vvs_weight_quant",
+           "vvs_block_matmul"):
     getattr(lib, _n).restype = C.c_int
 
 
@@ -221,7 +244,7 @@ def vvs_bind_neighbors(ctx: int, row_ptr: torch.Tensor, col: torch.Tensor) -> No
 
 # The calls a decoding loop makes per step are marshalled natively, csrc/binding_native.c (keyword arguments named as
 # the fields of the C structures, `ctx` first; a call through ctypes costs 6-10 us of host time).
-_native.setup(VvsError, torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice, torch.Tensor, _RopeOfRows)
+_native.setup(VvsError, torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice, torch.Tensor, _RopeOfRows, _WeightOnDevice)
 vvs_verify = _native.vvs_verify
 vvs_epilogue = _native.vvs_epilogue
 vvs_decide = _native.vvs_decide
@@ -236,6 +259,11 @@ vvs_rotate_axes = _native.vvs_rotate_axes
 vvs_quant_cache_append = _native.vvs_quant_cache_append
 vvs_quant_cache_attend = _native.vvs_quant_cache_attend
 vvs_quant_cache_evict = _native.vvs_quant_cache_evict
+make_qweight = _native.make_qweight
+vvs_norm_quant = _native.vvs_norm_quant
+vvs_rows_quant = _native.vvs_rows_quant
+vvs_weight_quant = _native.vvs_weight_quant
+vvs_block_matmul = _native.vvs_block_matmul
 
 
 def vvs_selftest_bounded_wait(ctx: int, stream=None):

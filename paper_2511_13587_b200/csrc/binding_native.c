@@ -338,7 +338,7 @@ static PyObject* py_select(FAST) {
 /* What a tensor is, by the C interface that torch.Tensor offers for it (__dlpack_c_exchange_api__ of DLPack 1.3; the layouts are that
  * standard's).  One call of some 40 ns; each of data_ptr(), shape, stride() and is_contiguous() costs more, and these entry points look at
  * up to nine tensors of a call that takes 6 us. */
-enum { kInt = 0, kUint = 1, kFloat = 2, kBfloat = 4, kDeviceCuda = 2 };
+enum { kInt = 0, kUint = 1, kFloat = 2, kBfloat = 4, kE4m3 = 10, kDeviceCuda = 2 };
 typedef struct {
   void* data;
   int32_t device, device_id, ndim;
@@ -354,7 +354,7 @@ typedef struct {
   void* work_stream;
 } ExchangeApi;
 static const ExchangeApi* g_exchange;
-static PyObject *g_tensor, *g_rope;              /* torch.Tensor; the class of make_rope_axes' results */
+static PyObject *g_tensor, *g_rope, *g_qweight;  /* torch.Tensor; the classes of make_rope_axes' and make_qweight's results */
 
 static int look(PyObject* o, const char* name, TensorView* v) {
   if (!PyObject_TypeCheck(o, (PyTypeObject*)g_tensor)) {
@@ -608,11 +608,217 @@ static PyObject* py_evict(FAST) {
                                                       f.stream));
 }
 
-/* setup(VvsError, current_raw_stream, current_device, Tensor, class of make_rope_axes' results) */
+/* ---- rows and weights in 8 bits --------------------------------------------------------------------------------------- */
+/* vvs_qweight, and the device that it lies on */
+typedef struct {
+  vvs_qweight w;
+  int32_t device;                                /* -1: a structure that the caller has made */
+} QWeight;
+typedef struct {
+  vvs_ctx* ctx;
+  PyObject *x, *weight, *residual, *sum_out, *norm_out, *gate, *codes, *scale, *w, *out;
+  void* stream;
+  float eps;
+  int32_t device;                                /* of the tensors looked at so far; -1: none yet */
+} Frame4;
+#define Q(f) offsetof(Frame4, f)
+static Param norm_params[] = {
+    {"ctx", 'c', 1, Q(ctx)}, {"x", 'o', 1, Q(x)}, {"weight", 'o', 1, Q(weight)}, {"eps", 'f', 1, Q(eps)}, {"codes", 'o', 1, Q(codes)},
+    {"scale", 'o', 1, Q(scale)}, {"residual", 'o', 0, Q(residual)}, {"sum_out", 'o', 0, Q(sum_out)}, {"norm_out", 'o', 0, Q(norm_out)},
+    {"stream", 's', 0, Q(stream)}};
+static Param rows_params[] = {
+    {"ctx", 'c', 1, Q(ctx)}, {"x", 'o', 1, Q(x)}, {"codes", 'o', 1, Q(codes)}, {"scale", 'o', 1, Q(scale)}, {"gate", 'o', 0, Q(gate)},
+    {"stream", 's', 0, Q(stream)}};
+static Param weight_params[] = {
+    {"ctx", 'c', 1, Q(ctx)}, {"w", 'o', 1, Q(w)}, {"codes", 'o', 1, Q(codes)}, {"scale", 'o', 1, Q(scale)}, {"stream", 's', 0, Q(stream)}};
+static Param matmul_params[] = {
+    {"ctx", 'c', 1, Q(ctx)}, {"codes", 'o', 1, Q(codes)}, {"scale", 'o', 1, Q(scale)}, {"w", 'o', 1, Q(w)}, {"out", 'o', 1, Q(out)},
+    {"stream", 's', 0, Q(stream)}};
+static Param qweight_params[] = {{"codes", 'o', 1, Q(codes)}, {"scale", 'o', 1, Q(scale)}};
+
+enum { kContext, kCodes, kFloat32 };             /* elements: of the context's type, e4m3 codes (as such or as bytes), float32 */
+/* Tensors of two dimensions (one: `cols` of them) whose rows have their elements side by side; rows and cols are taken from the tensor where
+ * they are 0 and compared with it where not.  `dense`: the rows side by side too.  All on one CUDA device, which is looked at last, in
+ * one_device. */
+static int matrix_of(Frame4* f, PyObject* t, const char* name, int elements, int dims, int dense, int32_t* rows, int32_t* cols, void** data,
+                     int64_t* row) {
+  TensorView v;
+  if (look(t, name, &v) < 0) return -1;
+  if (v.ndim != dims) {
+    PyErr_Format(PyExc_ValueError, "%s: expected a tensor of %d dimension%s", name, dims, dims > 1 ? "s" : "");
+    return -1;
+  }
+  const int wide = f->ctx && vvs_element_bytes(f->ctx) == 4;
+  if (elements == kCodes ? v.bits != 8 || (v.code != kE4m3 && v.code != kUint) : elements == kFloat32 ? v.code != kFloat || v.bits != 32
+                                          : f->ctx && (v.code != (wide ? kFloat : kBfloat) || v.bits != (wide ? 32 : 16))) {
+    PyErr_Format(PyExc_ValueError, "%s: expected %s elements", name,
+                 elements == kCodes ? "float8_e4m3fn or uint8" : elements == kFloat32 ? "float32" : wide ? "float32, the context's," : "bfloat16, the context's,");
+    return -1;
+  }
+  if (v.lanes != 1) {
+    PyErr_Format(PyExc_ValueError, "%s: expected elements of one number", name);
+    return -1;
+  }
+  int32_t* want[2] = {rows, cols};
+  for (int i = 0; i < dims; ++i) {
+    int32_t* d = want[i + 2 - dims];
+    if (v.shape[i] > INT32_MAX || (*d && *d != v.shape[i])) {
+      PyErr_Format(PyExc_ValueError, "%s: dimension %d is %lld, expected %d", name, i, (long long)v.shape[i], *d);
+      return -1;
+    }
+    *d = (int32_t)v.shape[i];
+  }
+  const int64_t n = v.shape[dims - 1], step = dims > 1 ? v.strides ? v.strides[0] : n : 0;
+  if ((v.strides && v.strides[dims - 1] != 1 && n > 1) || (dense && dims > 1 && step != n && v.shape[0] > 1)) {
+    PyErr_Format(PyExc_ValueError, dense ? "%s: expected a contiguous tensor" : "%s: the elements of a row do not lie side by side", name);
+    return -1;
+  }
+  *data = v.data;
+  if (row) *row = step;
+  const int32_t device = v.device == kDeviceCuda ? v.device_id : -2;
+  f->device = f->device == -1 || f->device == device ? device : -2;
+  return 0;
+}
+/* asked once all the tensors of a call are known to be what they should be: they lie on the current device, whose context and stream the call uses */
+static int one_device(const Frame4* f) {
+  int32_t now = -1;
+  if (f->device >= 0) {
+    PyObject* v = PyObject_CallNoArgs(g_get_device);
+    if (!v || to_int(v, &now) < 0) {
+      Py_XDECREF(v);
+      return -1;
+    }
+    Py_DECREF(v);
+  }
+  if (f->device >= 0 && f->device == now) return 0;
+  PyErr_SetString(PyExc_ValueError, f->device < 0 ? "expected CUDA tensors, all on one device" : "expected tensors on the current CUDA device");
+  return -1;
+}
+static int32_t blocks_of(int32_t n) { return n / 128 + (n % 128 != 0); }
+/* codes [rows, cols] and scale float32 [rows (of a weight: blocks of rows), blocks of columns] */
+static int coded_of(Frame4* f, int of_weight, int32_t* rows, int32_t* cols, void** codes, int64_t* row, void** scale) {
+  if (matrix_of(f, f->codes, "codes", kCodes, 2, 0, rows, cols, codes, row) < 0) return -1;
+  int32_t r = of_weight ? blocks_of(*rows) : *rows, c = blocks_of(*cols);
+  return r && c ? matrix_of(f, f->scale, "scale", kFloat32, 2, 1, &r, &c, scale, NULL) : 0;
+}
+/* nothing lies behind an empty matrix; the library's checks refuse its sizes */
+static PyObject* py_norm(FAST) {
+  (void)self;
+  Frame4 f = {0};
+  vvs_rows x, residual, sum, norm;
+  vvs_qrows out = {0};
+  void *weight, *scale = NULL;
+  int32_t rows = 0, cols = 0, one = 1;
+  f.device = -1;
+  if (PARSE("vvs_norm_quant", norm_params, N(norm_params)) < 0 || matrix_of(&f, f.x, "x", kContext, 2, 0, &rows, &cols, &x.data, &x.row) < 0 ||
+      matrix_of(&f, f.weight, "weight", kContext, 1, 1, &one, &cols, &weight, NULL) < 0 ||
+      coded_of(&f, 0, &rows, &cols, &out.codes, &out.row, &scale) < 0)
+    return NULL;
+  const int more = given(f.residual), keep = given(f.sum_out), also = given(f.norm_out);
+  if ((more && matrix_of(&f, f.residual, "residual", kContext, 2, 0, &rows, &cols, &residual.data, &residual.row) < 0) ||
+      (keep && matrix_of(&f, f.sum_out, "sum_out", kContext, 2, 0, &rows, &cols, &sum.data, &sum.row) < 0) ||
+      (also && matrix_of(&f, f.norm_out, "norm_out", kContext, 2, 0, &rows, &cols, &norm.data, &norm.row) < 0) || one_device(&f) < 0)
+    return NULL;
+  out.scale = scale;
+  CALL("vvs_norm_quant", vvs_norm_quant(f.ctx, rows, cols, &x, more ? &residual : NULL, weight, f.eps, keep ? &sum : NULL, also ? &norm : NULL,
+                                        &out, f.stream));
+}
+static PyObject* py_rows(FAST) {
+  (void)self;
+  Frame4 f = {0};
+  vvs_rows x, gate;
+  vvs_qrows out = {0};
+  void* scale = NULL;
+  int32_t rows = 0, cols = 0;
+  f.device = -1;
+  if (PARSE("vvs_rows_quant", rows_params, N(rows_params)) < 0 || matrix_of(&f, f.x, "x", kContext, 2, 0, &rows, &cols, &x.data, &x.row) < 0 ||
+      coded_of(&f, 0, &rows, &cols, &out.codes, &out.row, &scale) < 0)
+    return NULL;
+  const int two = given(f.gate);
+  if ((two && matrix_of(&f, f.gate, "gate", kContext, 2, 0, &rows, &cols, &gate.data, &gate.row) < 0) || one_device(&f) < 0) return NULL;
+  out.scale = scale;
+  CALL("vvs_rows_quant", vvs_rows_quant(f.ctx, rows, cols, &x, two ? &gate : NULL, &out, f.stream));
+}
+static PyObject* py_weight(FAST) {
+  (void)self;
+  Frame4 f = {0};
+  vvs_rows w;
+  vvs_qweight out = {0};
+  void* scale = NULL;
+  f.device = -1;
+  if (PARSE("vvs_weight_quant", weight_params, N(weight_params)) < 0 ||
+      matrix_of(&f, f.w, "w", kContext, 2, 0, &out.n_rows, &out.n_cols, &w.data, &w.row) < 0 ||
+      coded_of(&f, 1, &out.n_rows, &out.n_cols, &out.codes, &out.row, &scale) < 0 || one_device(&f) < 0)
+    return NULL;
+  out.scale = scale;
+  CALL("vvs_weight_quant", vvs_weight_quant(f.ctx, &w, &out, f.stream));
+}
+static PyObject* py_qweight(FAST) {
+  (void)self;
+  Frame4 f = {0};
+  QWeight q = {{0}, -1};
+  void* scale = NULL;
+  f.device = -1;
+  if (PARSE("make_qweight", qweight_params, N(qweight_params)) < 0 ||
+      coded_of(&f, 1, &q.w.n_rows, &q.w.n_cols, &q.w.codes, &q.w.row, &scale) < 0)
+    return NULL;
+  if (f.device < 0) {
+    PyErr_SetString(PyExc_ValueError, "expected CUDA tensors, all on one device");
+    return NULL;
+  }
+  q.w.scale = scale;
+  q.device = f.device;
+  PyObject* made = PyObject_CallNoArgs(g_qweight);
+  if (!made) return NULL;
+  Py_buffer b;
+  int rc = PyObject_GetBuffer(made, &b, PyBUF_WRITABLE);
+  if (rc == 0) {
+    if (b.len >= (Py_ssize_t)sizeof(q)) memcpy(b.buf, &q, sizeof(q));
+    else rc = -1, PyErr_SetString(PyExc_SystemError, "the class of make_qweight's results has another layout");
+    PyBuffer_Release(&b);
+  }
+  if (rc == 0) {
+    PyObject* keep = PyTuple_Pack(2, f.codes, f.scale);
+    rc = keep ? PyObject_SetAttr(made, s_keep, keep) : -1;
+    Py_XDECREF(keep);
+  }
+  if (rc < 0) Py_CLEAR(made);
+  return made;
+}
+static PyObject* py_matmul(FAST) {
+  (void)self;
+  Frame4 f = {0};
+  vvs_qrows a = {0};
+  vvs_rows out;
+  QWeight q = {{0}, -1};
+  void* scale = NULL;
+  int32_t rows = 0;
+  f.device = -1;
+  if (PARSE("vvs_block_matmul", matmul_params, N(matmul_params)) < 0) return NULL;
+  Py_buffer b;
+  if (PyObject_GetBuffer(f.w, &b, PyBUF_SIMPLE) < 0) return NULL;
+  const int ok = b.len == (Py_ssize_t)sizeof(vvs_qweight) || PyObject_TypeCheck(f.w, (PyTypeObject*)g_qweight);
+  if (ok) memcpy(&q, b.buf, b.len == (Py_ssize_t)sizeof(vvs_qweight) ? sizeof(vvs_qweight) : sizeof(q));
+  PyBuffer_Release(&b);
+  if (!ok) {
+    PyErr_SetString(PyExc_TypeError, "w: expected a vvs_qweight");
+    return NULL;
+  }
+  if (q.w.n_rows < 1 || q.w.n_cols < 1) return done(VVS_ERR_SHAPE, "vvs_block_matmul");
+  if (coded_of(&f, 0, &rows, &q.w.n_cols, &a.codes, &a.row, &scale) < 0 ||
+      matrix_of(&f, f.out, "out", kContext, 2, 0, &rows, &q.w.n_rows, &out.data, &out.row) < 0)
+    return NULL;
+  if (q.device >= 0 && q.device != f.device) f.device = -2;
+  if (one_device(&f) < 0) return NULL;
+  a.scale = scale;
+  CALL("vvs_block_matmul", vvs_block_matmul(f.ctx, rows, &a, &q.w, &out, f.stream));
+}
+
+/* setup(VvsError, current_raw_stream, current_device, Tensor, class of make_rope_axes' results, class of make_qweight's) */
 static PyObject* py_setup(PyObject* self, PyObject* args) {
   (void)self;
-  PyObject *e, *r, *d, *t, *rope;
-  if (!PyArg_ParseTuple(args, "OOOO!O", &e, &r, &d, &PyType_Type, &t, &rope)) return NULL;
+  PyObject *e, *r, *d, *t, *rope, *qweight;
+  if (!PyArg_ParseTuple(args, "OOOO!OO!", &e, &r, &d, &PyType_Type, &t, &rope, &PyType_Type, &qweight)) return NULL;
   PyObject* api = PyObject_GetAttrString(t, "__dlpack_c_exchange_api__");
   if (!api) return NULL;
   g_exchange = PyCapsule_GetPointer(api, "dlpack_exchange_api");        /* (torch's own, for as long as it is loaded) */
@@ -627,6 +833,7 @@ static PyObject* py_setup(PyObject* self, PyObject* args) {
   Py_XSETREF(g_get_device, Py_NewRef(d));
   Py_XSETREF(g_tensor, Py_NewRef(t));
   Py_XSETREF(g_rope, Py_NewRef(rope));
+  Py_XSETREF(g_qweight, Py_NewRef(qweight));
   Py_RETURN_NONE;
 }
 
@@ -664,6 +871,20 @@ static PyMethodDef methods[] = {
        "mass_decay=1.0, max_len=0, stream=None): q, out [n_seqs, n_rows, heads, head_dim]; scale 0 = 1 / sqrt(head_dim)."),
     FN("vvs_quant_cache_evict", py_evict,
        "vvs_quant_cache_evict(ctx, qc, cache_len, keep, n_sink, n_recent, next_age, mass_out, age_out, new_len, kept, stream=None)"),
+    FN("vvs_norm_quant", py_norm,
+       "vvs_norm_quant(ctx, x, weight, eps, codes, scale, residual=None, sum_out=None, norm_out=None, stream=None): x [n_rows, n_cols] (and "
+       "residual, sum_out, norm_out), codes float8_e4m3fn or uint8 [n_rows, n_cols], scale float32 [n_rows, ceil(n_cols / 128)]."),
+    FN("vvs_rows_quant", py_rows,
+       "vvs_rows_quant(ctx, x, codes, scale, gate=None, stream=None): x, or silu(gate) * x, in 8 bits; codes and scale as in vvs_norm_quant."),
+    FN("vvs_weight_quant", py_weight,
+       "vvs_weight_quant(ctx, w, codes, scale, stream=None): w [outputs, inputs], codes alike, scale float32 [ceil(outputs / 128), "
+       "ceil(inputs / 128)]."),
+    FN("make_qweight", py_qweight,
+       "make_qweight(codes, scale): a weight matrix in 8 bits, codes float8_e4m3fn or uint8 [outputs, inputs], scale float32 [ceil(outputs / 128), "
+       "ceil(inputs / 128)] (CUDA tensors)."),
+    FN("vvs_block_matmul", py_matmul,
+       "vvs_block_matmul(ctx, codes, scale, w, out, stream=None): rows in 8 bits [n_rows, inputs] times the transpose of w (from "
+       "make_qweight) into out [n_rows, outputs]."),
     {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
@@ -680,7 +901,8 @@ PyMODINIT_FUNC PyInit__native(void) {
 #define I(ps) intern(ps, N(ps)) < 0
   if (!s_data_ptr || !s_shape || !s_cuda_stream || !s_keep || I(verify_params) || I(epilogue_params) || I(decide_params) || I(noalloc_params) ||
       I(reset_params) || I(store_params) || I(fetch_params) || I(skip_params) || I(select_params) || I(rotate_params) ||
-      I(append_params) || I(attend_params) || I(evict_params) || I(rope_params))
+      I(append_params) || I(attend_params) || I(evict_params) || I(rope_params) || I(norm_params) || I(rows_params) || I(weight_params) ||
+      I(matmul_params) || I(qweight_params))
     return NULL;
   return PyModule_Create(&module);
 }

@@ -1,0 +1,290 @@
+// Product of rows and weights in e4m3 with scales of blocks of 128, for few to some hundred rows.
+//
+//   out[m, n] = sum_b a_scale[m, b] * w_scale[n / 128, b] * sum_{k in b} a[m, k] * w[n, k]
+//
+// Weights lie on the tensor cores' M side (128 of them a tile, one scale a block), the rows on its N side, so that few rows cost few
+// columns.  A block of K is one sum in tensor memory; while the next blocks' are under way, eight warps take it from there and add it, times
+// the two scales, to float32 sums in registers: a thread has a weight's row and half of the pass's rows.  The blocks of K of a tile are
+// dealt to the CTAs of a cluster where tiles are few; their sums are added in rank order through distributed shared memory.
+//
+// Bound by the weights' way from HBM, small ones by their chain of round trips.
+#include "block_matmul.cuh"
+
+namespace vvs {
+
+using namespace bmm;
+
+namespace {
+
+constexpr int kThreads = 384, kSumWarps = 8;
+constexpr int kMaxStages = 8, kChunk = 8;          // kChunk: blocks whose factors lie in shared memory together
+
+struct SplitPlan {
+  int stages, splits, passes, tn;
+};
+
+// CPT: columns (rows of the call) of a summing thread; a pass has 2 CPT of them
+template <int CPT, typename T>
+__global__ void __launch_bounds__(kThreads, CPT <= 32 ? 2 : 1)
+block_matmul_kernel(const __grid_constant__ MatmulParams p, const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_a, int stages) {
+  constexpr int TN = 2 * CPT, kBufs = CPT <= 32 ? 4 : 2, kCols = CPT <= 16 ? 32 : CPT <= 32 ? 64 : 128;     // kCols: tensor memory of a sum
+  constexpr uint32_t kStageBytes = kTileBytes + TN * kQBlock;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) uint64_t full_bar[kMaxStages], empty_bar[kMaxStages], sum_bar[kBufs], free_bar[kBufs];
+  __shared__ uint32_t tmem_slot;
+  __shared__ volatile int s_abort;
+  __shared__ __align__(16) float s_factor[2][2][kChunk][CPT];     // of a half, of even or odd chunks
+
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+  const int splits = (int)gridDim.x, rank = (int)blockIdx.x, tile = (int)blockIdx.y, tok0 = (int)blockIdx.z * TN;
+  const int kb0 = (int)((long long)p.nkb * rank / splits), kb1 = (int)((long long)p.nkb * (rank + 1) / splits), n_kb = kb1 - kb0;
+
+  if (tid == 0) {
+    for (int i = 0; i < stages; ++i) {
+      mbar_init(&full_bar[i], 1);
+      mbar_init(&empty_bar[i], 1);
+    }
+    for (int i = 0; i < kBufs; ++i) {
+      mbar_init(&sum_bar[i], 1);
+      mbar_init(&free_bar[i], kSumWarps);
+    }
+    s_abort = 0;
+    fence_barrier_init();
+  }
+  if (warp == 2) {
+    tmem_alloc(&tmem_slot, kBufs * kCols);
+    tmem_relinquish();
+  }
+  if (warp == 0 && elect_one()) {
+    tma_prefetch_desc(&tm_w);
+    tma_prefetch_desc(&tm_a);
+    // Weights go as far as L2 before the wait, not into shared memory: what precedes this kernel may be what writes them.
+    for (int i = 0; i < min(n_kb, stages); ++i) tma_prefetch_2d(&tm_w, (kb0 + i) * kQBlock, tile * 128);
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+  pdl_launch_dependents();
+  pdl_wait();
+
+  if (warp == 0) {
+    // ---- producer -------------------------------------------------------------------------------------------------------
+    uint32_t stage = 0, par = 1;                   // parity of the stage's previous release
+    int issued = 0;
+    bool ok = true;
+    for (int i = 0; i < n_kb; ++i, ++issued) {
+      if (i >= stages && !(ok = warp_wait_or_abort(&empty_bar[stage], par, &s_abort))) break;
+      __syncwarp();
+      if (elect_one()) {
+        uint8_t* st = smem + stage * kStageBytes;
+        mbar_expect_tx(&full_bar[stage], kStageBytes);
+        tma_load_2d(st, &tm_w, &full_bar[stage], (kb0 + i) * kQBlock, tile * 128);
+        tma_load_2d(st + kTileBytes, &tm_a, &full_bar[stage], (kb0 + i) * kQBlock, tok0);
+      }
+      if (++stage == (uint32_t)stages) { stage = 0; par ^= 1; }
+    }
+    if (!ok) {
+      if (lane == 0) atomicOr(p.status, VVS_DEV_TIMEOUT);
+      s_abort = 1;
+      for (int i = issued > stages ? issued - stages : 0; i < issued; ++i)     // nothing may be in flight when the CTA leaves (bounded)
+        mbar_wait(&full_bar[i % stages], (i / stages) & 1);
+      __syncwarp();
+    }
+  } else if (warp == 1) {
+    // ---- MMA issuer (a wait that ran out is reported, and nothing more is issued) -------------------------------------------
+    const uint32_t idesc = idesc_e4m3_f32(128, TN), lo0 = desc_lo_sw128(smem_u32(smem));
+    uint32_t stage = 0, par = 0, buf = 0, bpar = 1;
+    for (int i = 0; i < n_kb; ++i) {
+      const bool ok = (i < kBufs || warp_wait_or_abort(&free_bar[buf], bpar, &s_abort)) && warp_wait_or_abort(&full_bar[stage], par, &s_abort);
+      __syncwarp();
+      if (!ok) {
+        if (lane == 0) atomicOr(p.status, VVS_DEV_TIMEOUT);
+        s_abort = 1;
+        break;
+      }
+      tc_fence_after();
+      const uint32_t a_lo = lo0 + stage * (kStageBytes >> 4);
+      mma_e4m3_block<1>(tmem + buf * kCols, a_lo, a_lo + (kTileBytes >> 4), idesc);
+      mma_commit_elect(&empty_bar[stage]);
+      mma_commit_elect(&sum_bar[buf]);
+      if (++stage == (uint32_t)stages) { stage = 0; par ^= 1; }
+      if (++buf == kBufs) { buf = 0; bpar ^= 1; }
+    }
+  } else if (warp >= 4) {
+    // ---- sums -----------------------------------------------------------------------------------------------------------
+    const int half = (warp - 4) >> 2, t = tid & 127;                  // t: of the 128 threads of a half
+    const uint32_t t_row = tmem + ((uint32_t)((warp & 3) * 32) << 16) + half * CPT;
+    const int n_chunks = (n_kb + kChunk - 1) / kChunk;
+    // factors a_scale * w_scale of a chunk: eight neighbouring blocks of a row by eight neighbouring threads
+    constexpr int kLoads = (CPT * kChunk + 127) / 128;
+    float next[kLoads];
+    auto request = [&](int chunk) {
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) {
+        const int at = j * 128 + t, b = chunk * kChunk + (at & (kChunk - 1)), tok = tok0 + half * CPT + at / kChunk;
+        const bool in = at < CPT * kChunk && b < n_kb && tok < p.m;
+        next[j] = in ? p.a_scale[(size_t)tok * p.nkb + kb0 + b] * p.w_scale[(size_t)tile * p.nkb + kb0 + b] : 0.f;
+      }
+    };
+    auto put = [&](int chunk) {
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) {
+        const int at = j * 128 + t;
+        if (at < CPT * kChunk) s_factor[half][chunk & 1][at & (kChunk - 1)][at / kChunk] = next[j];
+      }
+    };
+    float acc[CPT];
+#pragma unroll
+    for (int j = 0; j < CPT; ++j) acc[j] = 0.f;
+    uint32_t buf = 0, bpar = 0;
+    bool ok = true;
+    request(0);
+    for (int c = 0; c < n_chunks; ++c) {
+      put(c);
+      if (c + 1 < n_chunks) request(c + 1);
+      named_bar_sync(1 + half, 128);               // (a chunk's place was last read two chunks ago, before the barrier between)
+      const int blocks = min(kChunk, n_kb - c * kChunk);
+#pragma unroll 1
+      for (int b = 0; b < blocks; ++b) {
+        ok = ok && warp_wait_or_abort(&sum_bar[buf], bpar, &s_abort);
+        __syncwarp();
+        if (ok) {
+          tc_fence_after();
+          const float4* f = reinterpret_cast<const float4*>(&s_factor[half][c & 1][b][0]);
+          constexpr int kLd = CPT < 16 ? 8 : 16;
+#pragma unroll
+          for (int j0 = 0; j0 < CPT; j0 += kLd) {
+            float part[kLd];
+            tmem_request(t_row + buf * kCols + j0, part);
+            tmem_wait(part);
+#pragma unroll
+            for (int j = 0; j < kLd; j += 4) {
+              const float4 g = f[(j0 + j) / 4];
+              fma2(acc[j0 + j], acc[j0 + j + 1], part[j], part[j + 1], g.x, g.y);
+              fma2(acc[j0 + j + 2], acc[j0 + j + 3], part[j + 2], part[j + 3], g.z, g.w);
+            }
+          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&free_bar[buf]);
+        }
+        if (++buf == kBufs) { buf = 0; bpar ^= 1; }
+      }
+    }
+    if (!ok) {
+      if (lane == 0) atomicOr(p.status, VVS_DEV_TIMEOUT);
+      s_abort = 1;
+    }
+    // the stages have drained: the last sum is behind every MMA.  [row of the call][weight]
+    float* red = reinterpret_cast<float*>(smem);
+    const int w_row = (warp & 3) * 32 + lane;
+    if (ok)
+#pragma unroll
+      for (int j = 0; j < CPT; ++j) red[(half * CPT + j) * 128 + w_row] = acc[j];
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (splits > 1) cluster_sync();
+  // ---- out: four weights of a row a thread, the CTAs of a cluster share the rows ------------------------------------------------
+  const int toks = min(TN, p.m - tok0), n0 = tile * 128 + (tid & 31) * 4;
+  const uint32_t red_at = smem_u32(smem);
+  if (!s_abort && n0 < p.n) {
+    for (int r = rank + (tid >> 5) * splits; r < toks; r += (kThreads / 32) * splits) {
+      float v[4] = {0.f, 0.f, 0.f, 0.f};
+      const uint32_t at = red_at + (uint32_t)(r * 128 + (tid & 31) * 4) * 4;
+      for (int s = 0; s < splits; ++s) {
+        const float4 x = ld_cluster_f4(at, s);
+        v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
+      }
+      T* o = static_cast<T*>(p.out) + (size_t)(tok0 + r) * p.out_row + n0;
+      if (p.wide && n0 + 4 <= p.n) {
+        store4(o, v);
+      } else {
+        for (int j = 0; j < 4 && n0 + j < p.n; ++j) {
+          if constexpr (sizeof(T) == 2) o[j] = __float2bfloat16_rn(v[j]);
+          else o[j] = v[j];
+        }
+      }
+    }
+  }
+  __syncwarp();
+  if (splits > 1) cluster_sync();                  // no CTA leaves while another reads its sums
+  if (warp == 2) tmem_dealloc(tmem, kBufs * kCols);
+}
+
+template <int CPT, typename T>
+int launch_cpt(const BlockMatmulArgs& g, const SplitPlan& pl, const MatmulParams& p, cudaStream_t s) {
+  CUtensorMap tm_w, tm_a;
+  int rc = make_tmap_e4m3(&tm_w, g.w, g.n, g.k, g.w_row, 128);
+  if (rc == VVS_OK) rc = make_tmap_e4m3(&tm_a, g.a, g.m, g.k, g.a_row, 2 * CPT);
+  if (rc != VVS_OK) return rc;
+  auto* fn = block_matmul_kernel<CPT, T>;
+  const int smem = pl.stages * (kTileBytes + 2 * CPT * kQBlock) + 1024;
+  if (ensure_dynamic_smem(reinterpret_cast<const void*>(fn), smem) != cudaSuccess) return VVS_ERR_CUDA;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(pl.splits, (g.n + 127) / 128, pl.passes);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = pl.splits;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = pl.splits > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, fn, p, tm_w, tm_a, pl.stages) == cudaSuccess ? VVS_OK : VVS_ERR_CUDA;
+}
+
+template <typename T>
+int launch_split(const BlockMatmulArgs& g, const SplitPlan& pl, const MatmulParams& p, cudaStream_t s) {
+  switch (pl.tn) {
+    case 16: return launch_cpt<8, T>(g, pl, p, s);
+    case 32: return launch_cpt<16, T>(g, pl, p, s);
+    case 64: return launch_cpt<32, T>(g, pl, p, s);
+    case 96: return launch_cpt<48, T>(g, pl, p, s);
+    default: return launch_cpt<64, T>(g, pl, p, s);
+  }
+}
+
+SplitPlan plan_split(const BlockMatmulArgs& g) {
+  SplitPlan pl{};
+  pl.passes = (g.m + 127) / 128;
+  const int each = (g.m + pl.passes - 1) / pl.passes;
+  pl.tn = each <= 16 ? 16 : each <= 32 ? 32 : each <= 64 ? 64 : each <= 96 ? 96 : 128;
+  pl.passes = (g.m + pl.tn - 1) / pl.tn;
+  const int nkb = qblocks(g.k);
+  const long long tiles = (long long)((g.n + 127) / 128) * pl.passes;
+  pl.splits = 1;
+  while (pl.splits < 8 && tiles * pl.splits * 2 <= 2 * g.n_sms && nkb >= 2 * pl.splits * 2) pl.splits *= 2;
+  const int room = pl.tn <= 64 ? 108 * 1024 : 200 * 1024;
+  pl.stages = room / (kTileBytes + pl.tn * kQBlock);
+  if (pl.stages > kMaxStages) pl.stages = kMaxStages;
+  return pl;
+}
+
+}  // namespace
+
+namespace bmm {
+int make_tmap_e4m3(CUtensorMap* out, const void* base, int64_t rows, int64_t cols, int64_t row_bytes, uint32_t box_rows) {
+  return make_tmap_bytes_2d(out, base, (uint64_t)rows, (uint64_t)cols, (uint64_t)row_bytes, kQBlock, box_rows);
+}
+}  // namespace bmm
+
+int launch_block_matmul(const BlockMatmulArgs& g, cudaStream_t s) try {
+  MatmulParams p{};
+  p.a_scale = g.a_scale; p.w_scale = g.w_scale; p.out = g.out; p.out_row = g.out_row; p.m = g.m; p.n = g.n; p.nkb = qblocks(g.k);
+  p.wide = g.out_row % 4 == 0;
+  p.status = g.status;
+  const SplitPlan pl = plan_split(g);
+  if (pl.passes > 65535) return VVS_ERR_SHAPE;
+  return g.f32 ? launch_split<float>(g, pl, p, s) : launch_split<__nv_bfloat16>(g, pl, p, s);
+} catch (...) {
+  return VVS_ERR_NOMEM;
+}
+
+}  // namespace vvs

@@ -572,6 +572,19 @@ int make_tmap_bf16_2d(CUtensorMap* out, const void* base, uint64_t rows, uint64_
   return r == CUDA_SUCCESS ? VVS_OK : VVS_ERR_CUDA;
 }
 
+// [rows, cols] bytes, rows `row_bytes` (a multiple of 16) apart; a box is `box_rows` rows of `box_cols` bytes (128 at most), 128-byte swizzled.
+int make_tmap_bytes_2d(CUtensorMap* out, const void* base, uint64_t rows, uint64_t cols, uint64_t row_bytes, uint32_t box_cols, uint32_t box_rows) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return VVS_ERR_CUDA;
+  cuuint64_t dims[2] = {cols, rows};
+  cuuint64_t strides[1] = {row_bytes};
+  cuuint32_t box[2] = {box_cols, box_rows};
+  cuuint32_t estr[2] = {1, 1};
+  CUresult r = fn(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? VVS_OK : VVS_ERR_CUDA;
+}
+
 // [rows, cols] seen as cols / 64 blocks of 64 columns, cols a multiple of 64: a box is `box_rows` rows of `box_blocks` blocks, each
 // block a 128-byte swizzled tile of its own.
 int make_tmap_bf16_blocks(CUtensorMap* out, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows, uint32_t box_blocks) {

@@ -1,0 +1,122 @@
+// A residual is added, the sum normalised by its root mean square, and the row rounded to e4m3 with a scale for each 128 columns.
+//
+//   s = x + residual,  y_k = s_k / sqrt(sum_j s_j^2 / n + eps) * weight_k,  scale_b = max |y_k| / 448,  code_k = e4m3(y_k / scale_b)
+//
+// Every element is read once and stays in registers between the sum of squares, the block's maximum and its code: bound by HBM for
+// prompts, by the launch and two dependent steps (sum over the row, maximum over a block) for a step's rows.  A thread has units of eight
+// elements; the sixteen lanes of half a warp have a block of 128 columns, so that a block's maximum is four shuffles.
+#include "block_quant.cuh"
+
+namespace vvs {
+
+namespace {
+
+// U: units of a thread.  blockDim (threads of a row, rows of a CTA).
+template <typename T, int U>
+__global__ void __launch_bounds__(512) norm_quant_kernel(NormQuantArgs a) {
+  __shared__ float s_sum[16];
+  grid_dep_launch();
+  const int t = threadIdx.x, threads = blockDim.x;
+  const int units = a.n_cols >> 3, nb = qblocks(a.n_cols);
+  const int row = min(blockIdx.x * blockDim.y + threadIdx.y, a.n_rows - 1);        // (a row of its own that is not there: the last one again)
+  const bool there = blockIdx.x * blockDim.y + threadIdx.y < (unsigned)a.n_rows;
+  grid_dep_wait();
+  Unit<T> x[U], r[U], w[U];
+#pragma unroll
+  for (int j = 0; j < U; ++j) {
+    const int u = j * threads + t;
+    x[j] = u < units ? load8<T>(a.x.data, row * a.x.row + 8 * u) : no_unit<T>();
+  }
+  if (a.residual.data)
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      const int u = j * threads + t;
+      r[j] = u < units ? load8<T>(a.residual.data, row * a.residual.row + 8 * u) : no_unit<T>();
+    }
+  constexpr bool kEarly = U * sizeof(T) <= 8;      // the norm's weights travel beside the row, where there are registers for both
+  auto weights = [&](int j) {
+    const int u = j * threads + t;
+    w[j] = u < units ? load8<T>(a.weight, 8 * u) : no_unit<T>();
+  };
+  if (kEarly)
+#pragma unroll
+    for (int j = 0; j < U; ++j) weights(j);
+  float y[U][8], ss = 0.f;
+#pragma unroll
+  for (int j = 0; j < U; ++j) {
+    widen_unit(x[j], y[j]);
+    if (a.residual.data) {
+      float z[8];
+      widen_unit(r[j], z);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[j][e] += z[e];
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ss = fmaf(y[j][e], y[j][e], ss);
+  }
+  if (a.sum_out.data && there)
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      const int u = j * threads + t;
+      if (u < units) store_unit(static_cast<T*>(a.sum_out.data) + row * a.sum_out.row + 8 * u, false, 0, narrow_unit(y[j], x[j]));
+    }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+  if (threads > 32) {                              // (one row a CTA then)
+    if ((t & 31) == 0) s_sum[t >> 5] = ss;
+    __syncthreads();
+    ss = (t & 31) < (threads >> 5) ? s_sum[t & 31] : 0.f;
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+    ss = __shfl_sync(0xffffffffu, ss, 0);
+  }
+  const float rs = rsqrtf(ss / (float)a.n_cols + a.eps);
+  bool odd = false;
+#pragma unroll
+  for (int j = 0; j < U; ++j) {
+    const int u = j * threads + t;
+    float g[8];
+    if (!kEarly) weights(j);
+    widen_unit(w[j], g);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[j][e] = y[j][e] * rs * g[e];
+    if (a.norm_out.data && there && u < units)
+      store_unit(static_cast<T*>(a.norm_out.data) + row * a.norm_out.row + 8 * u, false, 0, narrow_unit(y[j], x[j]));
+    float m = amax8(y[j]);
+    if (odd8(y[j])) {
+      odd = true;
+      m = amax8_finite(y[j]);
+      no_nan8(y[j]);
+    }
+    const float scale = block_scale(half_warp_max(m));
+    const uint2 c = codes8(y[j], __frcp_rn(scale));
+    if (there && u < units) {
+      *reinterpret_cast<uint2*>(a.codes + row * a.codes_row + 8 * u) = c;
+      if ((u & 15) == 0) a.scale[(size_t)row * nb + (u >> 4)] = scale;
+    }
+  }
+  if (!(fabsf(ss) <= 3.402823466e38f)) odd = true;                 // squares that are no float32 numbers: the row became zeros
+  if (odd && there) atomicOr(a.status, VVS_DEV_NONFINITE);
+}
+
+}  // namespace
+
+template <typename T>
+int launch_norm_quant(const NormQuantArgs& a, cudaStream_t s) {
+  const int units = a.n_cols / 8;
+  // Threads of a row: a unit each as long as that leaves at most 2048 threads an SM, else up to four
+  const long long room = (long long)a.n_sms * 2048;
+  int per = 1;
+  while (per < 4 && (long long)a.n_rows * units > room * per) per *= 2;
+  while (per < 8 && (units + per - 1) / per > 512) per *= 2;
+  const int threads = ((units + per - 1) / per + 31) / 32 * 32;
+  if (threads > 512) return VVS_ERR_SHAPE;
+  const int rows = threads == 32 ? 4 : 1;
+  auto* fn = per == 1 ? norm_quant_kernel<T, 1> : per == 2 ? norm_quant_kernel<T, 2> : per == 4 ? norm_quant_kernel<T, 4> : norm_quant_kernel<T, 8>;
+  const cudaError_t e = launch_kernel(fn, dim3((a.n_rows + rows - 1) / rows), dim3(threads, rows), 0, true, s, a);
+  return e == cudaSuccess ? VVS_OK : VVS_ERR_CUDA;
+}
+template int launch_norm_quant<float>(const NormQuantArgs&, cudaStream_t);
+template int launch_norm_quant<__nv_bfloat16>(const NormQuantArgs&, cudaStream_t);
+
+}  // namespace vvs

@@ -270,6 +270,7 @@ int make_tmap_bf16_blocks(CUtensorMap* out, const void* base, uint64_t rows, uin
 int make_tmap_bf16_pair_blocks(CUtensorMap* out, const void* base, uint64_t dist, uint64_t rows, uint64_t cols, uint32_t box_rows,
                                uint32_t box_blocks, bool in_turns);
 int make_tmap_bf16_2d(CUtensorMap* out, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows);
+int make_tmap_bytes_2d(CUtensorMap* out, const void* base, uint64_t rows, uint64_t cols, uint64_t row_bytes, uint32_t box_cols, uint32_t box_rows);
 int make_weight_tmap(CUtensorMap* out, const void* w, int rows, int cols);
 GemmTcPlan plan_gemm_tc(int m, int n, int k, bool dual, bool allow_split, int n_sms, int split_cap = 32);
 int launch_gemm_tc(int epi, const GemmTcPlan& plan, const GemmTcArgs& g, cudaStream_t s);
