@@ -103,10 +103,10 @@ int vvs_block_matmul(vvs_ctx* ctx, int32_t n_rows, const vvs_qrows* a, const vvs
   if (!aligned16(out->data)) return VVS_ERR_ALIGN;
   BlockMatmulArgs g{};
   g.a = static_cast<const uint8_t*>(a->codes); g.w = static_cast<const uint8_t*>(w->codes);
-  g.a_row = n_rows > 1 ? a->row : w->n_cols;         // (a tensor map's stride is looked at even where there is one row)
+  g.a_row = n_rows > 1 ? a->row : w->n_cols;         // (strides of tensor maps, which are looked at even where there is one row)
   g.w_row = w->n_rows > 1 ? w->row : w->n_cols;
   g.a_scale = a->scale; g.w_scale = w->scale;
-  g.out = out->data; g.out_row = n_rows > 1 ? out->row : 0;
+  g.out = out->data; g.out_row = n_rows > 1 ? out->row : (w->n_rows + 15) / 16 * 16;
   g.m = n_rows; g.n = w->n_rows; g.k = w->n_cols; g.f32 = is_f32(ctx); g.status = ctx->ws.status; g.n_sms = ctx->n_sms;
   return launch_block_matmul(g, static_cast<cudaStream_t>(stream));
 }

@@ -9,6 +9,7 @@
 //
 // Bound by the weights' way from HBM, small ones by their chain of round trips.
 #include "block_matmul.cuh"
+#include "block_plans.h"
 
 namespace vvs {
 
@@ -17,11 +18,9 @@ using namespace bmm;
 namespace {
 
 constexpr int kThreads = 384, kSumWarps = 8;
-constexpr int kMaxStages = 8, kChunk = 8;          // kChunk: blocks whose factors lie in shared memory together
+constexpr int kMaxStages = kMatmulMaxStages, kMaxSplits = kMatmulMaxSplits, kChunk = 8;     // kChunk: blocks whose factors lie in shared memory together
 
-struct SplitPlan {
-  int stages, splits, passes, tn;
-};
+static_assert(kTileBytes == kMatmulTileBytes, "what the plans count with");
 
 // CPT: columns (rows of the call) of a summing thread; a pass has 2 CPT of them
 template <int CPT, typename T>
@@ -30,7 +29,7 @@ block_matmul_kernel(const __grid_constant__ MatmulParams p, const __grid_constan
   constexpr int TN = 2 * CPT, kBufs = CPT <= 32 ? 4 : 2, kCols = CPT <= 16 ? 32 : CPT <= 32 ? 64 : 128;     // kCols: tensor memory of a sum
   constexpr uint32_t kStageBytes = kTileBytes + TN * kQBlock;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t full_bar[kMaxStages], empty_bar[kMaxStages], sum_bar[kBufs], free_bar[kBufs];
+  __shared__ __align__(8) uint64_t full_bar[kMaxStages], done_bar[kMaxStages], free_bar[kBufs];
   __shared__ uint32_t tmem_slot;
   __shared__ volatile int s_abort;
   __shared__ __align__(16) float s_factor[2][2][kChunk][CPT];     // of a half, of even or odd chunks
@@ -43,12 +42,9 @@ block_matmul_kernel(const __grid_constant__ MatmulParams p, const __grid_constan
   if (tid == 0) {
     for (int i = 0; i < stages; ++i) {
       mbar_init(&full_bar[i], 1);
-      mbar_init(&empty_bar[i], 1);
+      mbar_init(&done_bar[i], 1);
     }
-    for (int i = 0; i < kBufs; ++i) {
-      mbar_init(&sum_bar[i], 1);
-      mbar_init(&free_bar[i], kSumWarps);
-    }
+    for (int i = 0; i < kBufs; ++i) mbar_init(&free_bar[i], kSumWarps);
     s_abort = 0;
     fence_barrier_init();
   }
@@ -75,7 +71,7 @@ block_matmul_kernel(const __grid_constant__ MatmulParams p, const __grid_constan
     int issued = 0;
     bool ok = true;
     for (int i = 0; i < n_kb; ++i, ++issued) {
-      if (i >= stages && !(ok = warp_wait_or_abort(&empty_bar[stage], par, &s_abort))) break;
+      if (i >= stages && !(ok = warp_wait_or_abort(&done_bar[stage], par, &s_abort))) break;
       __syncwarp();
       if (elect_one()) {
         uint8_t* st = smem + stage * kStageBytes;
@@ -107,8 +103,7 @@ block_matmul_kernel(const __grid_constant__ MatmulParams p, const __grid_constan
       tc_fence_after();
       const uint32_t a_lo = lo0 + stage * (kStageBytes >> 4);
       mma_e4m3_block<1>(tmem + buf * kCols, a_lo, a_lo + (kTileBytes >> 4), idesc);
-      mma_commit_elect(&empty_bar[stage]);
-      mma_commit_elect(&sum_bar[buf]);
+      mma_commit_elect(&done_bar[stage]);          // the sum is there, and its stage may be filled again
       if (++stage == (uint32_t)stages) { stage = 0; par ^= 1; }
       if (++buf == kBufs) { buf = 0; bpar ^= 1; }
     }
@@ -119,26 +114,27 @@ block_matmul_kernel(const __grid_constant__ MatmulParams p, const __grid_constan
     const int n_chunks = (n_kb + kChunk - 1) / kChunk;
     // factors a_scale * w_scale of a chunk: eight neighbouring blocks of a row by eight neighbouring threads
     constexpr int kLoads = (CPT * kChunk + 127) / 128;
-    float next[kLoads];
+    float next_a[kLoads], next_w[kLoads];         // (multiplied where they are put down: a product here would wait for the loads)
     auto request = [&](int chunk) {
 #pragma unroll
       for (int j = 0; j < kLoads; ++j) {
         const int at = j * 128 + t, b = chunk * kChunk + (at & (kChunk - 1)), tok = tok0 + half * CPT + at / kChunk;
         const bool in = at < CPT * kChunk && b < n_kb && tok < p.m;
-        next[j] = in ? p.a_scale[(size_t)tok * p.nkb + kb0 + b] * p.w_scale[(size_t)tile * p.nkb + kb0 + b] : 0.f;
+        next_a[j] = in ? p.a_scale[(size_t)tok * p.nkb + kb0 + b] : 0.f;
+        next_w[j] = in ? p.w_scale[(size_t)tile * p.nkb + kb0 + b] : 0.f;
       }
     };
     auto put = [&](int chunk) {
 #pragma unroll
       for (int j = 0; j < kLoads; ++j) {
         const int at = j * 128 + t;
-        if (at < CPT * kChunk) s_factor[half][chunk & 1][at & (kChunk - 1)][at / kChunk] = next[j];
+        if (at < CPT * kChunk) s_factor[half][chunk & 1][at & (kChunk - 1)][at / kChunk] = next_a[j] * next_w[j];
       }
     };
     float acc[CPT];
 #pragma unroll
     for (int j = 0; j < CPT; ++j) acc[j] = 0.f;
-    uint32_t buf = 0, bpar = 0;
+    uint32_t buf = 0, stage = 0, par = 0;
     bool ok = true;
     request(0);
     for (int c = 0; c < n_chunks; ++c) {
@@ -148,29 +144,33 @@ block_matmul_kernel(const __grid_constant__ MatmulParams p, const __grid_constan
       const int blocks = min(kChunk, n_kb - c * kChunk);
 #pragma unroll 1
       for (int b = 0; b < blocks; ++b) {
-        ok = ok && warp_wait_or_abort(&sum_bar[buf], bpar, &s_abort);
-        __syncwarp();
+        ok = ok && warp_wait_lean(smem_u32(&done_bar[stage]), par, &s_abort);
         if (ok) {
           tc_fence_after();
           const float4* f = reinterpret_cast<const float4*>(&s_factor[half][c & 1][b][0]);
-          constexpr int kLd = CPT < 16 ? 8 : 16;
+          constexpr int kLd = CPT < 16 ? 8 : 16, kPieces = CPT / kLd;
+          float part[kPieces > 1 ? 2 : 1][kLd];
+          tmem_request(t_row + buf * kCols, part[0]);
 #pragma unroll
-          for (int j0 = 0; j0 < CPT; j0 += kLd) {
-            float part[kLd];
-            tmem_request(t_row + buf * kCols + j0, part);
-            tmem_wait(part);
+          for (int c = 0; c < kPieces; ++c) {
+            float (&now)[kLd] = part[kPieces > 1 ? c & 1 : 0];
+            tmem_wait(now);
+            if (c + 1 < kPieces) tmem_request(t_row + buf * kCols + (c + 1) * kLd, part[(c + 1) & 1]);
 #pragma unroll
             for (int j = 0; j < kLd; j += 4) {
-              const float4 g = f[(j0 + j) / 4];
-              fma2(acc[j0 + j], acc[j0 + j + 1], part[j], part[j + 1], g.x, g.y);
-              fma2(acc[j0 + j + 2], acc[j0 + j + 3], part[j + 2], part[j + 3], g.z, g.w);
+              const float4 g = f[(c * kLd + j) / 4];
+              acc[c * kLd + j] = fmaf(now[j], g.x, acc[c * kLd + j]);
+              acc[c * kLd + j + 1] = fmaf(now[j + 1], g.y, acc[c * kLd + j + 1]);
+              acc[c * kLd + j + 2] = fmaf(now[j + 2], g.z, acc[c * kLd + j + 2]);
+              acc[c * kLd + j + 3] = fmaf(now[j + 3], g.w, acc[c * kLd + j + 3]);
             }
           }
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(&free_bar[buf]);
         }
-        if (++buf == kBufs) { buf = 0; bpar ^= 1; }
+        if (++buf == kBufs) buf = 0;
+        if (++stage == (uint32_t)stages) { stage = 0; par ^= 1; }
       }
     }
     if (!ok) {
@@ -193,12 +193,15 @@ block_matmul_kernel(const __grid_constant__ MatmulParams p, const __grid_constan
   const uint32_t red_at = smem_u32(smem);
   if (!s_abort && n0 < p.n) {
     for (int r = rank + (tid >> 5) * splits; r < toks; r += (kThreads / 32) * splits) {
-      float v[4] = {0.f, 0.f, 0.f, 0.f};
       const uint32_t at = red_at + (uint32_t)(r * 128 + (tid & 31) * 4) * 4;
-      for (int s = 0; s < splits; ++s) {
-        const float4 x = ld_cluster_f4(at, s);
-        v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
-      }
+      float4 x[kMaxSplits];
+#pragma unroll
+      for (int s = 0; s < kMaxSplits; ++s)
+        if (s < splits) x[s] = ld_cluster_f4(at, s);
+      float v[4] = {x[0].x, x[0].y, x[0].z, x[0].w};
+#pragma unroll
+      for (int s = 1; s < kMaxSplits; ++s)
+        if (s < splits) v[0] += x[s].x, v[1] += x[s].y, v[2] += x[s].z, v[3] += x[s].w;
       T* o = static_cast<T*>(p.out) + (size_t)(tok0 + r) * p.out_row + n0;
       if (p.wide && n0 + 4 <= p.n) {
         store4(o, v);
@@ -211,12 +214,15 @@ block_matmul_kernel(const __grid_constant__ MatmulParams p, const __grid_constan
     }
   }
   __syncwarp();
-  if (splits > 1) cluster_sync();                  // no CTA leaves while another reads its sums
+  if (splits > 1) {                                // no CTA leaves while another reads its sums (a release would wait for the stores to out)
+    cluster_arrive_relaxed();
+    cluster_wait();
+  }
   if (warp == 2) tmem_dealloc(tmem, kBufs * kCols);
 }
 
 template <int CPT, typename T>
-int launch_cpt(const BlockMatmulArgs& g, const SplitPlan& pl, const MatmulParams& p, cudaStream_t s) {
+int launch_cpt(const BlockMatmulArgs& g, const BlockMatmulPlan& pl, const MatmulParams& p, cudaStream_t s) {
   CUtensorMap tm_w, tm_a;
   int rc = make_tmap_e4m3(&tm_w, g.w, g.n, g.k, g.w_row, 128);
   if (rc == VVS_OK) rc = make_tmap_e4m3(&tm_a, g.a, g.m, g.k, g.a_row, 2 * CPT);
@@ -241,7 +247,7 @@ int launch_cpt(const BlockMatmulArgs& g, const SplitPlan& pl, const MatmulParams
 }
 
 template <typename T>
-int launch_split(const BlockMatmulArgs& g, const SplitPlan& pl, const MatmulParams& p, cudaStream_t s) {
+int launch_split(const BlockMatmulArgs& g, const BlockMatmulPlan& pl, const MatmulParams& p, cudaStream_t s) {
   switch (pl.tn) {
     case 16: return launch_cpt<8, T>(g, pl, p, s);
     case 32: return launch_cpt<16, T>(g, pl, p, s);
@@ -249,22 +255,6 @@ int launch_split(const BlockMatmulArgs& g, const SplitPlan& pl, const MatmulPara
     case 96: return launch_cpt<48, T>(g, pl, p, s);
     default: return launch_cpt<64, T>(g, pl, p, s);
   }
-}
-
-SplitPlan plan_split(const BlockMatmulArgs& g) {
-  SplitPlan pl{};
-  pl.passes = (g.m + 127) / 128;
-  const int each = (g.m + pl.passes - 1) / pl.passes;
-  pl.tn = each <= 16 ? 16 : each <= 32 ? 32 : each <= 64 ? 64 : each <= 96 ? 96 : 128;
-  pl.passes = (g.m + pl.tn - 1) / pl.tn;
-  const int nkb = qblocks(g.k);
-  const long long tiles = (long long)((g.n + 127) / 128) * pl.passes;
-  pl.splits = 1;
-  while (pl.splits < 8 && tiles * pl.splits * 2 <= 2 * g.n_sms && nkb >= 2 * pl.splits * 2) pl.splits *= 2;
-  const int room = pl.tn <= 64 ? 108 * 1024 : 200 * 1024;
-  pl.stages = room / (kTileBytes + pl.tn * kQBlock);
-  if (pl.stages > kMaxStages) pl.stages = kMaxStages;
-  return pl;
 }
 
 }  // namespace
@@ -276,12 +266,12 @@ int make_tmap_e4m3(CUtensorMap* out, const void* base, int64_t rows, int64_t col
 }  // namespace bmm
 
 int launch_block_matmul(const BlockMatmulArgs& g, cudaStream_t s) try {
+  const BlockMatmulPlan pl = plan_block_matmul(g.m, g.n, g.k, g.n_sms);
+  if (pl.pairs) return launch_block_matmul_pair(g, s);
   MatmulParams p{};
   p.a_scale = g.a_scale; p.w_scale = g.w_scale; p.out = g.out; p.out_row = g.out_row; p.m = g.m; p.n = g.n; p.nkb = qblocks(g.k);
   p.wide = g.out_row % 4 == 0;
   p.status = g.status;
-  const SplitPlan pl = plan_split(g);
-  if (pl.passes > 65535) return VVS_ERR_SHAPE;
   return g.f32 ? launch_split<float>(g, pl, p, s) : launch_split<__nv_bfloat16>(g, pl, p, s);
 } catch (...) {
   return VVS_ERR_NOMEM;

@@ -55,11 +55,25 @@ __device__ __forceinline__ void tma_prefetch_2d(const CUtensorMap* m, int x, int
   asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global [%0, {%1, %2}];" ::"l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(y) : "memory");
 }
 
-// two sums at once: acc += part * f
-__device__ __forceinline__ void fma2(float& a0, float& a1, float p0, float p1, float f0, float f1) {
-  asm("{\n\t.reg .b64 a, p, f;\n\tmov.b64 a, {%0, %1};\n\tmov.b64 p, {%2, %3};\n\tmov.b64 f, {%4, %5};\n\t"
-      "fma.rn.f32x2 a, p, f, a;\n\tmov.b64 {%0, %1}, a;\n\t}"
-      : "+f"(a0), "+f"(a1) : "f"(p0), "f"(p1), "f"(f0), "f"(f1));
+// Bounded wait of a warp, which goes on as one, in as few instructions as it takes where the phase is complete.
+__device__ __forceinline__ bool warp_wait_lean(uint32_t bar, uint32_t parity, const volatile int* abort_flag) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .u32 n, a;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "@p bra VVS_DONE_%=;\n\t"
+      "mov.u32 n, %4;\n"
+      "VVS_AGAIN_%=:\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "@p bra VVS_DONE_%=;\n\t"
+      "ld.volatile.shared.u32 a, [%3];\n\tsetp.ne.u32 p, a, 0;\n\t@p bra VVS_GONE_%=;\n\t"
+      "sub.u32 n, n, 1;\n\tsetp.ne.u32 p, n, 0;\n\t@p bra VVS_AGAIN_%=;\n"
+      "VVS_GONE_%=:\n\t"
+      "setp.ne.u32 p, n, n;\n"
+      "VVS_DONE_%=:\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok) : "r"(bar), "r"(parity), "r"(smem_u32(const_cast<const int*>(abort_flag))), "n"(kSpinLimit) : "memory");
+  return __all_sync(0xffffffffu, ok);
 }
 
 // N (8, 16 or 32) consecutive columns of the warp's 32 lanes are requested; tmem_wait before they are read

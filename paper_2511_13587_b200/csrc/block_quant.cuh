@@ -2,6 +2,8 @@
 // parameters of the kernels, and what several of them do with a value.
 #pragma once
 
+#include <algorithm>
+
 #include "quant_cache.cuh"
 
 namespace vvs {
@@ -56,6 +58,7 @@ struct BlockMatmulArgs {
   int n_sms;
 };
 int launch_block_matmul(const BlockMatmulArgs& a, cudaStream_t s);
+int launch_block_matmul_pair(const BlockMatmulArgs& a, cudaStream_t s);          // many rows
 
 // ---- eight elements of a row, as they are stored ----------------------------------------------------------------------
 template <typename T>
