@@ -72,37 +72,42 @@ __device__ __forceinline__ Unit<T> no_unit() {
 
 // ---- a block's scale and codes ----------------------------------------------------------------------------------------
 // A scale is the largest finite magnitude / 448, 2^-60 at least: not a power of two as in the cache, whose scales grow while their
-// codes stay.  The largest element takes the largest code, so a block uses e4m3's whole range whatever its magnitude.
-__device__ __forceinline__ float block_scale(float amax) { return fmaxf(__fdiv_rn(amax, 448.f), 0x1p-60f); }
-__device__ __forceinline__ float finite_abs(float x) {
-  const float a = fabsf(x);
-  return a <= 3.402823466e38f ? a : 0.f;           // neither an infinity nor a NaN counts for the scale
+// codes stay.  The largest element takes the largest code, so a block uses e4m3's whole range whatever its magnitude.  The quotient by a
+// constant is its product with the reciprocal and one correction, rounded as a division is; the factor that codes are made with is within a
+// unit of the last place of 1 / scale.  (All sixteen lanes of a block do this: a division each cost a third of what SwiGLU's rows took.)
+__device__ __forceinline__ float block_scale(float amax) {
+  constexpr float k = 1.f / 448.f;
+  const float q = amax * k;
+  return fmaxf(fmaf(fmaf(-448.f, q, amax), k, q), 0x1p-60f);
 }
+__device__ __forceinline__ float scale_inverse(float scale) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(scale));
+  return fmaf(fmaf(-scale, r, 1.f), r, r);
+}
+// the largest magnitude of eight, NaN if one of them is
 __device__ __forceinline__ float amax8(const float (&y)[8]) {
+  auto three = [](float a, float b, float c) {
+    float m;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(a), "f"(b), "f"(c));
+    return m;
+  };
+  return three(three(y[0], y[1], y[2]), three(y[3], y[4], y[5]), three(y[6], y[7], y[7]));
+}
+__device__ __forceinline__ bool odd(float m) { return !(m <= 3.402823466e38f); }       // of an amax8: there is an infinity or a NaN
+// Neither counts for the scale; an infinity becomes the largest code (the conversion saturates), a NaN 0.
+__device__ __forceinline__ float amax8_finite(float (&y)[8]) {
   float m = 0.f;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(y[e]));           // (fmaxf drops a NaN)
-  return m;
-}
-// an infinity becomes the largest code (the conversion saturates), a NaN 0
-__device__ __forceinline__ bool odd8(const float (&y)[8]) {
-  float z = 0.f;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) z = fmaf(y[e], 0.f, z);              // NaN once one of them is no finite number
-  return z != z;
-}
-__device__ __forceinline__ float amax8_finite(const float (&y)[8]) {
-  float m = 0.f;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) m = fmaxf(m, finite_abs(y[e]));
+  for (int e = 0; e < 8; ++e) {
+    const float a = fabsf(y[e]);
+    m = fmaxf(m, a <= 3.402823466e38f ? a : 0.f);
+    y[e] = y[e] != y[e] ? 0.f : y[e];
+  }
   return m;
 }
 __device__ __forceinline__ uint2 codes8(const float (&y)[8], float inv) {
   return make_uint2(to_e4m3x4(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv), to_e4m3x4(y[4] * inv, y[5] * inv, y[6] * inv, y[7] * inv));
-}
-__device__ __forceinline__ void no_nan8(float (&y)[8]) {
-#pragma unroll
-  for (int e = 0; e < 8; ++e) y[e] = y[e] != y[e] ? 0.f : y[e];
 }
 // the largest of the sixteen lanes that have a block's 128 columns
 __device__ __forceinline__ float half_warp_max(float m) {
@@ -110,6 +115,5 @@ __device__ __forceinline__ float half_warp_max(float m) {
   for (int o = 8; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
   return m;
 }
-__device__ __forceinline__ float warp_max(float m) { return fmaxf(half_warp_max(m), __shfl_xor_sync(0xffffffffu, half_warp_max(m), 16)); }
 
 }  // namespace vvs

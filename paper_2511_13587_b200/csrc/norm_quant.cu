@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(512) norm_quant_kernel(NormQuantArgs a) {
     ss = __shfl_sync(0xffffffffu, ss, 0);
   }
   const float rs = rsqrtf(ss / (float)a.n_cols + a.eps);
-  bool odd = false;
+  bool strange = false;
 #pragma unroll
   for (int j = 0; j < U; ++j) {
     const int u = j * threads + t;
@@ -83,20 +83,19 @@ __global__ void __launch_bounds__(512) norm_quant_kernel(NormQuantArgs a) {
     if (a.norm_out.data && there && u < units)
       store_unit(static_cast<T*>(a.norm_out.data) + row * a.norm_out.row + 8 * u, false, 0, narrow_unit(y[j], x[j]));
     float m = amax8(y[j]);
-    if (odd8(y[j])) {
-      odd = true;
+    if (odd(m)) {
+      strange = true;
       m = amax8_finite(y[j]);
-      no_nan8(y[j]);
     }
     const float scale = block_scale(half_warp_max(m));
-    const uint2 c = codes8(y[j], __frcp_rn(scale));
+    const uint2 c = codes8(y[j], scale_inverse(scale));
     if (there && u < units) {
       *reinterpret_cast<uint2*>(a.codes + row * a.codes_row + 8 * u) = c;
       if ((u & 15) == 0) a.scale[(size_t)row * nb + (u >> 4)] = scale;
     }
   }
-  if (!(fabsf(ss) <= 3.402823466e38f)) odd = true;                 // squares that are no float32 numbers: the row became zeros
-  if (odd && there) atomicOr(a.status, VVS_DEV_NONFINITE);
+  // (squares that are no float32 numbers have made the row zeros)
+  if ((strange || odd(ss)) && there) atomicOr(a.status, VVS_DEV_NONFINITE);
 }
 
 }  // namespace

@@ -11,58 +11,68 @@ namespace vvs {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kFlight = 4;                         // blocks of a half warp whose elements are on their way together
+constexpr int kFlight = 4;                         // rows whose elements are on their way together
 
+// gate / (1 + e^-gate) * x
+__device__ __forceinline__ float gated(float gate, float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + ex2(gate * -1.442695041f)));
+  return gate * r * x;
+}
+
+// A CTA has up to sixteen blocks of columns, a half warp each, and goes through `each` rows.
 template <typename T, bool GATE>
-__global__ void __launch_bounds__(kThreads) rows_quant_kernel(RowsQuantArgs a, int each) {
+__global__ void __launch_bounds__(kThreads, 4) rows_quant_kernel(RowsQuantArgs a, int each) {
   grid_dep_launch();
   grid_dep_wait();
-  const int nb = qblocks(a.n_cols), lane16 = threadIdx.x & 15;
-  const int total = a.n_rows * nb, first = (int)((blockIdx.x * kThreads + threadIdx.x) >> 4), step = (int)(gridDim.x * (kThreads / 16));
-  bool odd = false;
-  // (both halves of a warp take as many turns: `first` of the second is one more)
-  for (int i = 0; i < each; i += kFlight) {
-    Unit<T> x[kFlight], g[kFlight];
-    int row[kFlight], col[kFlight];
+  const int nb = qblocks(a.n_cols), block = blockIdx.x * (blockDim.x >> 4) + (threadIdx.x >> 4), col = block * kQBlock + 8 * (threadIdx.x & 15);
+  const bool in = col < a.n_cols;
+  const int r0 = blockIdx.y * each, r1 = min(a.n_rows, r0 + each);
+  const T* x = static_cast<const T*>(a.x.data) + (int64_t)r0 * a.x.row + col;
+  const T* g = static_cast<const T*>(a.gate.data) + (int64_t)r0 * a.gate.row + col;
+  uint8_t* codes = a.codes + (int64_t)r0 * a.codes_row + col;
+  float* scale_at = a.scale + (size_t)r0 * nb + block;
+  bool strange = false;
+  for (int r = r0; r < r1; r += kFlight) {
+    Unit<T> ux[kFlight], ug[kFlight];
 #pragma unroll
     for (int j = 0; j < kFlight; ++j) {
-      const int b = first + (i + j) * step;                        // (below 2^31: kMaxBlocks)
-      row[j] = b / nb;
-      col[j] = (b - row[j] * nb) * kQBlock + 8 * lane16;
-      const bool in = i + j < each && b < total && col[j] < a.n_cols;
-      if (!in) row[j] = -1;
-      x[j] = in ? load8<T>(a.x.data, row[j] * a.x.row + col[j]) : no_unit<T>();
-      if (GATE) g[j] = in ? load8<T>(a.gate.data, row[j] * a.gate.row + col[j]) : no_unit<T>();
+      const bool there = in && r + j < r1;
+      ux[j] = there ? load_unit(x, false, 0) : no_unit<T>();
+      if (GATE) ug[j] = there ? load_unit(g, false, 0) : no_unit<T>();
+      x += a.x.row;
+      if (GATE) g += a.gate.row;
     }
 #pragma unroll
     for (int j = 0; j < kFlight; ++j) {
+      if (r + j >= r1) break;                      // (of all lanes)
       float y[8];
-      widen_unit(x[j], y);
+      widen_unit(ux[j], y);
       if (GATE) {
         float z[8];
-        widen_unit(g[j], z);
+        widen_unit(ug[j], z);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] *= __fdividef(z[e], 1.f + __expf(-z[e]));
+        for (int e = 0; e < 8; ++e) y[e] = gated(z[e], y[e]);
       }
       float m = amax8(y);
-      if (odd8(y)) {
-        odd = true;
+      if (odd(m)) {
+        strange = true;
         m = amax8_finite(y);
-        no_nan8(y);
       }
       const float scale = block_scale(half_warp_max(m));
-      const uint2 c = codes8(y, __frcp_rn(scale));
-      if (row[j] >= 0) {
-        *reinterpret_cast<uint2*>(a.codes + row[j] * a.codes_row + col[j]) = c;
-        if (lane16 == 0) a.scale[(size_t)row[j] * nb + (col[j] >> 7)] = scale;
+      if (in) {
+        *reinterpret_cast<uint2*>(codes) = codes8(y, scale_inverse(scale));
+        if ((threadIdx.x & 15) == 0) *scale_at = scale;
       }
+      codes += a.codes_row;
+      scale_at += nb;
     }
   }
-  if (odd) atomicOr(a.status, VVS_DEV_NONFINITE);
+  if (strange) atomicOr(a.status, VVS_DEV_NONFINITE);
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads) weight_quant_kernel(RowsQuantArgs a) {
+__global__ void __launch_bounds__(kThreads, 3) weight_quant_kernel(RowsQuantArgs a) {
   __shared__ float s_max[kThreads / 32];
   constexpr int kRows = kThreads / 16, kUnits = kQBlock / kRows;   // rows that the CTA has at once, units of a thread
   grid_dep_wait();                                                 // (no early launch of what follows: it may read the codes ahead of its own wait)
@@ -75,47 +85,50 @@ __global__ void __launch_bounds__(kThreads) weight_quant_kernel(RowsQuantArgs a)
     x[j] = in && row < a.n_rows ? load8<T>(a.x.data, row * a.x.row + col) : no_unit<T>();
   }
   float m = 0.f;
-  bool odd = false;
+  bool strange = false;
 #pragma unroll
   for (int j = 0; j < kUnits; ++j) {
     float y[8];
     widen_unit(x[j], y);
-    const bool strange = odd8(y);
-    odd = odd || strange;
-    m = fmaxf(m, strange ? amax8_finite(y) : amax8(y));
+    float n = amax8(y);
+    if (odd(n)) {
+      strange = true;
+      n = amax8_finite(y);
+    }
+    m = fmaxf(m, n);
   }
-  m = warp_max(m);
+  m = half_warp_max(m);
+  m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
   if ((threadIdx.x & 31) == 0) s_max[threadIdx.x >> 5] = m;
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < kThreads / 32; ++i) m = fmaxf(m, s_max[i]);
-  const float scale = block_scale(m), inv = __frcp_rn(scale);
+  const float scale = block_scale(m), inv = scale_inverse(scale);
   if (threadIdx.x == 0) a.scale[(size_t)blockIdx.y * gridDim.x + blockIdx.x] = scale;
 #pragma unroll
   for (int j = 0; j < kUnits; ++j) {
     const long long row = r0 + j * kRows;
     float y[8];
     widen_unit(x[j], y);
-    if (odd) no_nan8(y);
+    if (strange) amax8_finite(y);
     if (in && row < a.n_rows) *reinterpret_cast<uint2*>(a.codes + row * a.codes_row + col) = codes8(y, inv);
   }
-  if (odd) atomicOr(a.status, VVS_DEV_NONFINITE);
+  if (strange) atomicOr(a.status, VVS_DEV_NONFINITE);
 }
 
 }  // namespace
 
 template <typename T>
 int launch_rows_quant(const RowsQuantArgs& a, cudaStream_t s) {
-  const long long total = (long long)a.n_rows * qblocks(a.n_cols), at_once = kThreads / 16;
-  const long long most = (long long)a.n_sms * 8;                   // CTAs that are on the device together
-  long long blocks = (total + at_once - 1) / at_once;
-  if (blocks > most) {                                             // whole turns of kFlight blocks for each half warp
-    const long long turns = (total + most * at_once * kFlight - 1) / (most * at_once * kFlight);
-    blocks = (total + turns * kFlight * at_once - 1) / (turns * kFlight * at_once);
-  }
-  const long long each = (total + blocks * at_once - 1) / (blocks * at_once);
+  // Blocks of columns by CTAs of sixteen at most, an even number each (27 blocks: two of fourteen); rows by as many as are on the device together
+  const int nb = qblocks(a.n_cols), groups = (nb + 15) / 16, mine = ((nb + groups - 1) / groups + 1) & ~1;
+  const long long most = std::max(1LL, (long long)a.n_sms * 4 * (kThreads / (16 * mine)) / groups);
+  long long each = (a.n_rows + most - 1) / most;
+  if (each > 1) each = (each + kFlight - 1) / kFlight * kFlight;
+  each = std::max(each, (a.n_rows + 65534LL) / 65535);
   auto* fn = a.gate.data ? rows_quant_kernel<T, true> : rows_quant_kernel<T, false>;
-  const cudaError_t e = launch_kernel(fn, dim3((unsigned)blocks), dim3(kThreads), 0, true, s, a, (int)each);
+  const cudaError_t e =
+      launch_kernel(fn, dim3(groups, (unsigned)((a.n_rows + each - 1) / each)), dim3(16 * mine), 0, true, s, a, (int)each);
   return e == cudaSuccess ? VVS_OK : VVS_ERR_CUDA;
 }
 template int launch_rows_quant<float>(const RowsQuantArgs&, cudaStream_t);
