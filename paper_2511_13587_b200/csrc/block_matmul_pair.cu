@@ -44,14 +44,16 @@ __device__ __forceinline__ Two two(float a, float b) {
   return t;
 }
 __device__ __forceinline__ void one_and_one(Two t, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(t)); }
-__device__ __forceinline__ void add_times(Two& acc, Two x, Two f) { asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc) : "l"(x), "l"(f)); }
-__device__ __forceinline__ void tmem_fma16(uint32_t taddr, Two* acc, Two ff) {
+// Eight columns of the warp's lanes are added to their sums.  (Of sixteen at once the compiler moves a half of every pair to where the packed
+// multiply-add finds it, on the pipe that it takes itself; of eight it does not.)
+__device__ __forceinline__ void add_columns8(uint32_t taddr, Two* acc, Two ff) {
   asm volatile(
-      "{\n\t.reg .b32 t<16>;\n\t.reg .b64 x;\n\t"
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {t0,t1,t2,t3,t4,t5,t6,t7,t8,t9,t10,t11,t12,t13,t14,t15}, [%8];\n\t"
+      "{\n\t.reg .b32 t<8>;\n\t.reg .b64 x;\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {t0,t1,t2,t3,t4,t5,t6,t7}, [%4];\n\t"
       "tcgen05.wait::ld.sync.aligned;\n\t"
-      "mov.b64 x, {t0,t1};\n\tfma.rn.f32x2 %0, x, %9, %0;\n\tmov.b64 x, {t2,t3};\n\tfma.rn.f32x2 %1, x, %9, %1;\n\tmov.b64 x, {t4,t5};\n\tfma.rn.f32x2 %2, x, %9, %2;\n\tmov.b64 x, {t6,t7};\n\tfma.rn.f32x2 %3, x, %9, %3;\n\tmov.b64 x, {t8,t9};\n\tfma.rn.f32x2 %4, x, %9, %4;\n\tmov.b64 x, {t10,t11};\n\tfma.rn.f32x2 %5, x, %9, %5;\n\tmov.b64 x, {t12,t13};\n\tfma.rn.f32x2 %6, x, %9, %6;\n\tmov.b64 x, {t14,t15};\n\tfma.rn.f32x2 %7, x, %9, %7;\n\t}"
-      : "+l"(acc[0]), "+l"(acc[1]), "+l"(acc[2]), "+l"(acc[3]), "+l"(acc[4]), "+l"(acc[5]), "+l"(acc[6]), "+l"(acc[7]) : "r"(taddr), "l"(ff) : "memory");
+      "mov.b64 x, {t0,t1};\n\tfma.rn.f32x2 %0, x, %5, %0;\n\tmov.b64 x, {t2,t3};\n\tfma.rn.f32x2 %1, x, %5, %1;\n\t"
+      "mov.b64 x, {t4,t5};\n\tfma.rn.f32x2 %2, x, %5, %2;\n\tmov.b64 x, {t6,t7};\n\tfma.rn.f32x2 %3, x, %5, %3;\n\t}"
+      : "+l"(acc[0]), "+l"(acc[1]), "+l"(acc[2]), "+l"(acc[3]) : "r"(taddr), "l"(ff) : "memory");
 }
 // sixteen bytes of a row
 __device__ __forceinline__ void put_piece(uint8_t* to, const float (&y)[8]) {
@@ -232,34 +234,28 @@ block_matmul_pair_kernel(const __grid_constant__ MatmulParams p, const __grid_co
     const int group = (warp - 4) >> 2, half = group >> 1, quad = warp & 3;
     const uint32_t t_row = tmem + ((uint32_t)(quad * 32) << 16) + group * kCols;
     const uint32_t my_factor = smem_u32(factors) + (uint32_t)(half * 128 + quad * 32 + lane) * 4;
+    const uint32_t sum0 = smem_u32(&sum_bar[half][0]), free0 = mapa(smem_u32(&free_bar[half][0]), 0);
     uint32_t turn = 0;                             // pairs of blocks so far
-    bool early = false;                            // the next block's sums were there when they were asked for ahead of time
     for (int id = first; id < n_tiles && ok; id += step) {
       Two acc[kCols / 2];
 #pragma unroll
       for (int j = 0; j < kCols / 2; ++j) acc[j] = 0;
 #pragma unroll 1
-      for (int kb = 0; kb < nkb; kb += 2) {
+      for (int kb = 0; kb < nkb; kb += 2, ++turn) {
         const uint32_t factor_at = my_factor + (turn & (kRing / 2 - 1)) * (2 * kFactors * 4);
 #pragma unroll
         for (int buf = 0; buf < 2; ++buf) {
-          if (!__all_sync(0xffffffffu, early)) ok = warp_wait_lean(smem_u32(&sum_bar[half][buf]), turn & 1, &s_abort);
-          if (!ok) break;
+          if (!(ok = warp_wait_lean(sum0 + buf * 8, turn & 1, &s_abort))) break;
           const float f = ld_shared(factor_at + buf * (kFactors * 4));
           tc_fence_after();
           const Two ff = two(f, f);
 #pragma unroll
-          for (int c = 0; c < kCols / 16; ++c) {
-            if (c == kCols / 16 - 1) early = mbar_test_wait(&sum_bar[half][buf ^ 1], (turn + buf) & 1);
-            tmem_fma16(t_row + buf * kTile + c * 16, acc + c * 8, ff);
-            if (c == kCols / 16 - 1) {
-              tc_fence_before();
-              __syncwarp();
-              if (lane == 0) mbar_arrive_at(mapa(smem_u32(&free_bar[half][buf]), 0));
-            }
-          }
+          for (int c = 0; c < kCols; c += 8) add_columns8(t_row + buf * kTile + c, acc + c / 2, ff);
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_at(free0 + buf * 8);
         }
-        ++turn;
+        if (!ok) break;
       }
       if (!ok) break;
       // ---- out: 128 bytes of each of the warp's rows at a time, swizzled as the bulk copy takes them -----------------------------------
