@@ -36,7 +36,7 @@ block_matmul_kernel(const __grid_constant__ MatmulParams p, const __grid_constan
 
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
-  const int splits = (int)gridDim.x, rank = (int)blockIdx.x, tile = (int)blockIdx.y, tok0 = (int)blockIdx.z * TN;
+  const int splits = (int)gridDim.x, rank = (int)blockIdx.x, tile = p.first + (int)blockIdx.y, tok0 = (int)blockIdx.z * TN;
   const int kb0 = (int)((long long)p.nkb * rank / splits), kb1 = (int)((long long)p.nkb * (rank + 1) / splits), n_kb = kb1 - kb0;
 
   if (tid == 0) {
@@ -62,8 +62,11 @@ block_matmul_kernel(const __grid_constant__ MatmulParams p, const __grid_constan
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = tmem_slot;
-  pdl_launch_dependents();
-  pdl_wait();
+  // Of two launches the first lets the second begin once what precedes both is done, so that the second need not wait for the first; it
+  // does so in the end, for what follows waits for the second alone.
+  if (p.chain != 1) pdl_launch_dependents();
+  if (p.chain != 2) pdl_wait();
+  if (p.chain == 1) pdl_launch_dependents();
 
   if (warp == 0) {
     // ---- producer -------------------------------------------------------------------------------------------------------
@@ -219,19 +222,24 @@ block_matmul_kernel(const __grid_constant__ MatmulParams p, const __grid_constan
     cluster_wait();
   }
   if (warp == 2) tmem_dealloc(tmem, kBufs * kCols);
+  if (p.chain == 2) pdl_wait();
 }
 
 template <int CPT, typename T>
-int launch_cpt(const BlockMatmulArgs& g, const BlockMatmulPlan& pl, const MatmulParams& p, cudaStream_t s) {
+int launch_cpt(const BlockMatmulArgs& g, MatmulParams p, cudaStream_t s) {
+  constexpr int TN = 2 * CPT;
+  auto* fn = block_matmul_kernel<CPT, T>;
+  const int smem = matmul_stages(TN) * (kTileBytes + TN * kQBlock) + 1024;
+  if (ensure_dynamic_smem(reinterpret_cast<const void*>(fn), smem) != cudaSuccess) return VVS_ERR_CUDA;
+  const int* clusters = resident_clusters(reinterpret_cast<const void*>(fn), kThreads, smem);
+  if (!clusters) return VVS_ERR_CUDA;
+  const BlockMatmulPlan pl = plan_block_matmul(g.m, g.n, g.k, g.n_sms, clusters);
+  if (pl.pairs) return launch_block_matmul_pair(g, s);
   CUtensorMap tm_w, tm_a;
   int rc = make_tmap_e4m3(&tm_w, g.w, g.n, g.k, g.w_row, 128);
-  if (rc == VVS_OK) rc = make_tmap_e4m3(&tm_a, g.a, g.m, g.k, g.a_row, 2 * CPT);
+  if (rc == VVS_OK) rc = make_tmap_e4m3(&tm_a, g.a, g.m, g.k, g.a_row, TN);
   if (rc != VVS_OK) return rc;
-  auto* fn = block_matmul_kernel<CPT, T>;
-  const int smem = pl.stages * (kTileBytes + 2 * CPT * kQBlock) + 1024;
-  if (ensure_dynamic_smem(reinterpret_cast<const void*>(fn), smem) != cudaSuccess) return VVS_ERR_CUDA;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(pl.splits, (g.n + 127) / 128, pl.passes);
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
@@ -239,21 +247,29 @@ int launch_cpt(const BlockMatmulArgs& g, const BlockMatmulPlan& pl, const Matmul
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = pl.splits;
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = pl.splits > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, fn, p, tm_w, tm_a, pl.stages) == cudaSuccess ? VVS_OK : VVS_ERR_CUDA;
+  const bool both = pl.part[1].count > 0;
+  for (int i = 0; i < (both ? 2 : 1); ++i) {
+    const BlockMatmulPart& part = pl.part[i];
+    cfg.gridDim = dim3(part.splits, (unsigned)part.count, pl.passes);
+    attr[1].val.clusterDim.x = part.splits;
+    cfg.numAttrs = part.splits > 1 ? 2 : 1;
+    p.first = (int)part.first;
+    p.chain = both ? i + 1 : 0;
+    if (cudaLaunchKernelEx(&cfg, fn, p, tm_w, tm_a, pl.stages) != cudaSuccess) return VVS_ERR_CUDA;
+  }
+  return VVS_OK;
 }
 
 template <typename T>
-int launch_split(const BlockMatmulArgs& g, const BlockMatmulPlan& pl, const MatmulParams& p, cudaStream_t s) {
-  switch (pl.tn) {
-    case 16: return launch_cpt<8, T>(g, pl, p, s);
-    case 32: return launch_cpt<16, T>(g, pl, p, s);
-    case 64: return launch_cpt<32, T>(g, pl, p, s);
-    case 96: return launch_cpt<48, T>(g, pl, p, s);
-    default: return launch_cpt<64, T>(g, pl, p, s);
+int launch_rows(const BlockMatmulArgs& g, const MatmulParams& p, cudaStream_t s) {
+  switch (matmul_rows(g.m)) {
+    case 16: return launch_cpt<8, T>(g, p, s);
+    case 32: return launch_cpt<16, T>(g, p, s);
+    case 64: return launch_cpt<32, T>(g, p, s);
+    case 96: return launch_cpt<48, T>(g, p, s);
+    default: return launch_cpt<64, T>(g, p, s);
   }
 }
 
@@ -266,13 +282,11 @@ int make_tmap_e4m3(CUtensorMap* out, const void* base, int64_t rows, int64_t col
 }  // namespace bmm
 
 int launch_block_matmul(const BlockMatmulArgs& g, cudaStream_t s) try {
-  const BlockMatmulPlan pl = plan_block_matmul(g.m, g.n, g.k, g.n_sms);
-  if (pl.pairs) return launch_block_matmul_pair(g, s);
   MatmulParams p{};
   p.a_scale = g.a_scale; p.w_scale = g.w_scale; p.out = g.out; p.out_row = g.out_row; p.m = g.m; p.n = g.n; p.nkb = qblocks(g.k);
   p.wide = g.out_row % 4 == 0;
   p.status = g.status;
-  return g.f32 ? launch_split<float>(g, pl, p, s) : launch_split<__nv_bfloat16>(g, pl, p, s);
+  return g.f32 ? launch_rows<float>(g, p, s) : launch_rows<__nv_bfloat16>(g, p, s);
 } catch (...) {
   return VVS_ERR_NOMEM;
 }

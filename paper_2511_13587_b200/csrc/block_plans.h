@@ -6,42 +6,75 @@
 
 namespace vvs {
 
+// Tiles of 128 weights of one launch; of each tile and pass the blocks of K are dealt to `splits` CTAs, a cluster.
+struct BlockMatmulPart {
+  int64_t first, count;
+  int splits;
+};
 struct BlockMatmulPlan {
   bool pairs;        // block_matmul_pair.cu; the rest is of block_matmul.cu
   int tn;            // rows of a pass
   int passes;
-  int splits;        // CTAs that share a tile's blocks of K (a cluster)
   int stages;        // blocks of K under way
+  BlockMatmulPart part[2];                                        // the second may have no tiles
 };
 
 constexpr int kMatmulMaxSplits = 8, kMatmulMaxStages = 8;
 constexpr int kMatmulTileBytes = 128 * 128;                       // 128 rows of a block of K
 
-inline int matmul_ctas_per_sm(int tn) { return tn <= 64 ? 2 : 1; }
+inline int matmul_rows(int64_t m) {                               // of a pass
+  const int64_t passes = (m + 127) / 128, each = (m + passes - 1) / passes;
+  return each <= 16 ? 16 : each <= 32 ? 32 : each <= 64 ? 64 : each <= 96 ? 96 : 128;
+}
+inline int matmul_stages(int tn) { return std::min(kMatmulMaxStages, (tn <= 64 ? 108 : 200) * 1024 / (kMatmulTileBytes + tn * 128)); }
 
-inline BlockMatmulPlan plan_block_matmul(int64_t m, int64_t n, int64_t k, int n_sms) {
+// clusters: how many clusters of 1 .. 8 CTAs the device holds at once where each CTA has an SM (148, 74, 45, 33, 26, 22, 15, 15).
+inline BlockMatmulPlan plan_block_matmul(int64_t m, int64_t n, int64_t k, int n_sms, const int* clusters) {
   BlockMatmulPlan pl{};
   const int64_t nkb = (k + 127) / 128;
-  int64_t passes = (m + 127) / 128;
-  const int64_t each = (m + passes - 1) / passes;
-  pl.tn = each <= 16 ? 16 : each <= 32 ? 32 : each <= 64 ? 64 : each <= 96 ? 96 : 128;
-  passes = (m + pl.tn - 1) / pl.tn;
-  // As many CTAs as the device holds at once, of two blocks of K at least (288 rows of 3456 through 1280 weights, 30 tiles: 1 / 2 / 4 / 8 splits
-  // 13.3 / 9.7 / 8.2 / 15.2 us, the last two rounds of CTAs; 18 rows of 4096 through 4096, 32 tiles: 11.2 / 8.7 / 7.2 / 7.1).
-  const int64_t tiles = (n + 127) / 128 * passes, slots = (int64_t)n_sms * matmul_ctas_per_sm(pl.tn);
-  int64_t splits = 1;
-  while (splits < kMatmulMaxSplits && tiles * splits * 2 <= slots && nkb >= 4 * splits) splits *= 2;
-  pl.splits = (int)splits;
-  pl.stages = std::min(kMatmulMaxStages, (pl.tn <= 64 ? 108 : 200) * 1024 / (kMatmulTileBytes + pl.tn * 128));
-  // Microseconds x 100 that either kernel takes: rounds of CTAs (pairs) x blocks of K, and what a round costs beside them.  Measured at 9 x 9
-  // sizes from 96 to 2048 rows, it picks the faster one or one within 4 %: 128 rows of 4096 through 22016 weights 35.2 us here, 35.6 on pairs; 256
-  // 53.9 / 36.8; 1024 194 / 104; 1024 rows of 1280 through 1280 9.3 / 9.4, 2048 18.3 / 9.8.
-  const int64_t a_block = pl.tn <= 32 ? 30 : pl.tn <= 64 ? 40 : pl.tn <= 96 ? 42 : 50;
-  const int64_t here = (tiles * splits + slots - 1) / slots * ((nkb + splits - 1) / splits * a_block + 350);
+  pl.tn = matmul_rows(m);
+  pl.stages = matmul_stages(pl.tn);
+  const int64_t passes = (m + pl.tn - 1) / pl.tn, tiles = (n + 127) / 128;
+  pl.passes = (int)std::min<int64_t>(passes, 65535);
+  // Microseconds x 100: blocks of K of the busiest SM (where two CTAs share it, one's loads fill the other's waits), and what a cluster's
+  // exchange costs.
+  const int64_t a_block = pl.tn <= 32 ? 24 : pl.tn <= 64 ? 32 : pl.tn <= 96 ? 42 : 50;
+  const int per_sm = pl.tn <= 64 ? 2 : 1;
+  auto cost = [&](int64_t count, int s) {
+    const int64_t each = (count * s + n_sms - 1) / n_sms, rounds = (each + per_sm - 1) / per_sm, blocks = (nkb + s - 1) / s;
+    return (each < per_sm ? blocks * a_block * 3 / 2 : each * blocks * a_block) + rounds * 350 + (s > 1 ? 80 + 20 * s : 0);
+  };
+  // Clusters that do not all fit at once wait for others' end and gain nothing; a CTA has two blocks at least.  288 rows of 3456 through 1280
+  // weights, 30 tiles: 1 / 2 / 4 CTAs a tile 13.3 / 9.7 / 8.2 us; 18 rows of 4096 through 4096, 32 tiles, 1 / 2 / 4 / 8: 11.2 / 8.7 / 7.2 / 7.1.
+  // Numbers between are slower where all SMs have work already (96 tiles of 32 blocks, 2 / 3: 12.9 / 14.0; ten of ten, 4 / 5: 4.1 / 4.5).
+  auto splits_of = [&](int64_t count, bool any) {
+    int best = 1;
+    for (int s = 2; s <= kMatmulMaxSplits && 2 * s <= nkb && count <= (int64_t)clusters[s] * per_sm; s += any ? 1 : s)
+      if (cost(count, s) < cost(count, best)) best = s;
+    return best;
+  };
+  const int whole_splits = splits_of(tiles * passes, false);
+  pl.part[0] = {0, tiles, whole_splits};
+  int64_t whole = cost(tiles * passes, whole_splits);
+  // Tiles that are left over where all SMs have as many as the others: in a launch of their own, dealt to all SMs, beside the first one (two CTAs
+  // fit an SM).  18 rows of 4096 through 22016 weights, 172 tiles: 20.1 us as one launch (most SMs that have a CTA have two), 18.3 as 148 and 24 by
+  // six; 64 rows, whose sums take longer, 20.9 / 21.2.
+  const int64_t full = tiles / n_sms * n_sms, left = tiles - full;
+  if (pl.tn <= 32 && full > 0 && left > 0) {
+    const int s = splits_of(left, true);
+    const int64_t blocks = full / n_sms * nkb + (left * s + n_sms - 1) / n_sms * ((nkb + s - 1) / s), both = blocks * a_block + 530 + 20 * s;
+    if (both < whole) {
+      whole = both;
+      pl.part[0] = {0, full, 1};
+      pl.part[1] = {full, left, s};
+    }
+  }
+  // The pairs' kernel: rounds of pairs x blocks of K.  Measured at 9 x 9 sizes from 96 to 2048 rows, the smaller of the two numbers is the faster
+  // kernel or one within 5 %: 128 rows of 4096 through 22016 weights 35.2 us here, 34.5 on pairs; 256 53.9 / 34.5; 1024 194 / 86; 1024 rows of 1280
+  // through 1280 9.3 / 9.4, 2048 18.3 / 9.8.
   const int64_t pair_tiles = (m + 255) / 256 * ((n + 255) / 256), pairs = n_sms / 2;
   const int64_t there = (pair_tiles + pairs - 1) / pairs * (nkb + (nkb & 1)) * 46 + 500;
-  pl.pairs = there < here || passes > 65535;
-  pl.passes = (int)std::min<int64_t>(passes, 65535);
+  pl.pairs = there < whole || passes > 65535;
   return pl;
 }
 

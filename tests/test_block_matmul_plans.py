@@ -8,12 +8,15 @@ import pytest
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2511_13587_b200", "csrc")
 SHIM = """
 #include "block_plans.h"
-extern "C" void plan(long long m, long long n, long long k, int sms, int* out) {
-  const vvs::BlockMatmulPlan p = vvs::plan_block_matmul(m, n, k, sms);
-  out[0] = p.pairs; out[1] = p.tn; out[2] = p.passes; out[3] = p.splits; out[4] = p.stages;
+extern "C" void plan(long long m, long long n, long long k, int sms, const int* clusters, long long* out) {
+  const vvs::BlockMatmulPlan p = vvs::plan_block_matmul(m, n, k, sms, clusters);
+  out[0] = p.pairs; out[1] = p.tn; out[2] = p.passes; out[3] = p.stages;
+  for (int i = 0; i < 2; ++i) out[4 + 3 * i] = p.part[i].first, out[5 + 3 * i] = p.part[i].count, out[6 + 3 * i] = p.part[i].splits;
 }
 """
 SIZES = [1, 2, 15, 16, 17, 32, 33, 64, 65, 96, 97, 128, 129, 191, 192, 193, 255, 256, 257, 300, 511, 512, 1000, 5460, 70001, 1 << 24]
+# clusters of 0 .. 8 CTAs that a device holds at once, an SM each, and of a device that holds none of more than one
+CLUSTERS = {None: [0, 148, 74, 45, 33, 26, 22, 15, 15], 0: [0, 148] + [0] * 7}
 
 
 @pytest.fixture(scope="module")
@@ -24,25 +27,33 @@ def plan(tmp_path_factory):
         f.write(SHIM)
     subprocess.run([os.environ.get("CXX", "g++"), "-std=c++17", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-I", CSRC, src, "-o", lib], check=True)
     so = ctypes.CDLL(lib)
-    so.plan.argtypes = [ctypes.c_longlong] * 3 + [ctypes.c_int, ctypes.c_void_p]
+    so.plan.argtypes = [ctypes.c_longlong] * 3 + [ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p]
 
-    def call(m, n, k, sms=148):
-        out = (ctypes.c_int * 5)()
-        so.plan(m, n, k, sms, out)
-        return dict(zip(("pairs", "tn", "passes", "splits", "stages"), out))
+    def call(m, n, k, held=None):
+        clusters = (ctypes.c_int * 9)(*CLUSTERS[held])
+        out = (ctypes.c_longlong * 10)()
+        so.plan(m, n, k, 148, clusters, out)
+        p = dict(zip(("pairs", "tn", "passes", "stages"), out))
+        return dict(p, parts=[tuple(out[4 + 3 * i:7 + 3 * i]) for i in range(2)], clusters=list(clusters))
     return call
 
 
-def test_plans_cover_their_rows_and_fit(plan):
+@pytest.mark.parametrize("held", [None, 0])
+def test_plans_cover_their_rows_and_weights_and_fit(plan, held):
     for m in SIZES:
-        for n in (1, 127, 128, 129, 1280, 4096, 22016, 65535 * 128):
+        for n in (1, 127, 128, 129, 1280, 4096, 18944, 22016, 37889, 65535 * 128):
             for k in (16, 128, 144, 1280, 4096, 11008, 1 << 20):
-                p = plan(m, n, k)
+                p = plan(m, n, k, held)
                 if p["pairs"]:
                     continue
                 assert p["tn"] in (16, 32, 64, 96, 128) and 1 <= p["passes"] <= 65535 and p["tn"] * p["passes"] >= m, (m, n, k)
                 assert p["tn"] * (p["passes"] - 1) < m                              # no pass without rows
-                assert 1 <= p["splits"] <= 8 and p["splits"] <= -(-k // 128)        # no CTA without a block of K
+                (first, count, splits), (first_2, count_2, splits_2) = p["parts"]
+                assert first == 0 and count >= 1 and count + count_2 == -(-n // 128) <= 65535
+                assert count_2 == 0 or (first_2 == count and p["passes"] == 1 and p["tn"] <= 64)
+                for c, s in ((count * p["passes"], splits), (count_2, splits_2)):
+                    assert c == 0 or 1 <= s <= 8 and s <= -(-k // 128)              # no CTA without a block of K
+                    assert c == 0 or s == 1 or c <= p["clusters"][s] * (2 if p["tn"] <= 64 else 1)      # clusters that are all there at once
                 stage = 16384 + p["tn"] * 128
                 smem = p["stages"] * stage + 1024
                 # two CTAs of a pass of 64 rows at most on an SM, one otherwise (1 KB each is the system's; factors and barriers are static)
@@ -57,6 +68,12 @@ def test_sizes_of_the_gpu_tests_on_pairs(plan, m, k, n):
 
 
 def test_few_rows_stay_with_the_weights_and_many_go_on_pairs(plan):
-    assert not plan(1, 1280, 1280)["pairs"] and plan(1, 1280, 1280)["splits"] == 4
-    assert not plan(18, 22016, 4096)["pairs"] and plan(18, 22016, 4096)["splits"] == 1
-    assert not plan(288, 1280, 3456)["pairs"] and plan(5460, 12288, 4096)["pairs"] and plan(1 << 24, 16, 128)["pairs"]
+    assert not plan(1, 1280, 1280)["pairs"] and plan(1, 1280, 1280)["parts"][0] == (0, 10, 4)
+    assert not plan(18, 22016, 4096)["pairs"] and plan(18, 22016, 4096)["parts"] == [(0, 148, 1), (148, 24, 6)]
+    assert not plan(288, 1280, 3456)["pairs"] and plan(288, 1280, 3456)["parts"][0] == (0, 10, 4)
+    assert plan(5460, 12288, 4096)["pairs"] and plan(1 << 24, 16, 128)["pairs"]
+
+
+@pytest.mark.parametrize("m,k,n", [(18, 4096, 19000), (3, 4000, 20001)])
+def test_sizes_of_the_gpu_tests_in_two_launches(plan, m, k, n):
+    assert plan(m, n, k)["parts"][1][1] > 0

@@ -243,6 +243,36 @@ def test_product(ctxs, dtype, rows, cols, outs):
     assert vb.vvs_device_status(ctxs[dtype]) == 0
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,cols,outs", [(18, 4096, 19000), (3, 4000, 20001)])
+def test_few_rows_of_many_weights(ctxs, dtype, rows, cols, outs):
+    """Two launches: tiles for all SMs, and those left over dealt to all of them.  Right behind other calls on the stream, and in a graph."""
+    rng = gen.rng_for(25, f"many{rows}{cols}{outs}")
+    codes = [rng.integers(0, 0x7F, n, np.uint8) | rng.integers(0, 2, n, np.uint8) << 7 for n in ((rows, cols), (outs, cols))]
+    scale = [np.exp(rng.standard_normal((n, -(-cols // 128)))).astype(np.float32) for n in (rows, -(-outs // 128))]
+    ops = [dev(x) for x in (codes[0], scale[0], codes[1], scale[1])]
+    w = vb.make_qweight(ops[2], ops[3])
+    out, other = (torch.zeros((rows, outs), dtype=dtype, device="cuda") for _ in range(2))
+    vb.vvs_block_matmul(ctxs[dtype], ops[0], ops[1], w, out)
+    check_product(out, ops)
+    g = torch.cuda.CUDAGraph()
+    a = torch.zeros_like(ops[0])
+    x = torch.zeros((rows, cols), dtype=dtype, device="cuda")
+    s = torch.zeros_like(ops[1])
+    with torch.cuda.graph(g):
+        for _ in range(3):                                    # rows that change right before, results that are overwritten right behind
+            a.zero_()
+            vb.vvs_block_matmul(ctxs[dtype], a, ops[1], w, other)
+            vb.vvs_rows_quant(ctxs[dtype], x, a, s)
+            a.copy_(ops[0])
+            vb.vvs_block_matmul(ctxs[dtype], a, ops[1], w, other)
+            vb.vvs_block_matmul(ctxs[dtype], a, ops[1], w, other)
+    for _ in range(3):
+        g.replay()
+        assert torch.equal(other, out)
+    assert vb.vvs_device_status(ctxs[dtype]) == 0
+
+
 def test_product_of_scales_far_apart_and_of_nan(ctxs):
     rng = gen.rng_for(26, "far")
     ops = operands(rng, 40, 512, 300)
