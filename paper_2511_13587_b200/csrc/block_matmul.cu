@@ -5,7 +5,7 @@
 // Weights lie on the tensor cores' M side (128 of them a tile, one scale a block), the rows on its N side, so that few rows cost few
 // columns.  A block of K is one sum in tensor memory; while the next blocks' are under way, eight warps take it from there and add it, times
 // the two scales, to float32 sums in registers: a thread has a weight's row and half of the pass's rows.  The blocks of K of a tile are
-// dealt to the CTAs of a cluster where tiles are few; their sums are added in rank order through distributed shared memory.
+// dealt to the CTAs of a cluster where tiles are few; each CTA is sent the others' sums of its share of the rows and adds them in rank order.
 //
 // Bound by the weights' way from HBM, small ones by their chain of round trips.
 #include "block_matmul.cuh"
@@ -20,16 +20,21 @@ namespace {
 constexpr int kThreads = 384, kSumWarps = 8;
 constexpr int kMaxStages = kMatmulMaxStages, kMaxSplits = kMatmulMaxSplits, kChunk = 8;     // kChunk: blocks whose factors lie in shared memory together
 
+constexpr int kFourBytes = 128 * 16;               // sums of four rows of the call with a tile of weights
 static_assert(kTileBytes == kMatmulTileBytes, "what the plans count with");
+
+__device__ __forceinline__ void put_one(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
+__device__ __forceinline__ void put_one(float* p, float v) { *p = v; }
 
 // CPT: columns (rows of the call) of a summing thread; a pass has 2 CPT of them
 template <int CPT, typename T>
 __global__ void __launch_bounds__(kThreads, CPT <= 32 ? 2 : 1)
 block_matmul_kernel(const __grid_constant__ MatmulParams p, const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_a, int stages) {
-  constexpr int TN = 2 * CPT, kBufs = CPT <= 32 ? 4 : 2, kCols = CPT <= 16 ? 32 : CPT <= 32 ? 64 : 128;     // kCols: tensor memory of a sum
+  constexpr int TN = 2 * CPT, kBufs = kMatmulPlaces<TN>, kCols = CPT <= 16 ? 32 : CPT <= 32 ? 64 : 128, kTmem = CPT <= 32 ? 128 : 256;
+  static_assert(kBufs * kCols <= kTmem, "columns of tensor memory, a power of two; two CTAs fit an SM");
   constexpr uint32_t kStageBytes = kTileBytes + TN * kQBlock;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t full_bar[kMaxStages], done_bar[kMaxStages], free_bar[kBufs];
+  __shared__ __align__(8) uint64_t full_bar[kMaxStages], done_bar[kMaxStages], free_bar[kBufs], recv_bar;
   __shared__ uint32_t tmem_slot;
   __shared__ volatile int s_abort;
   __shared__ __align__(16) float s_factor[2][2][kChunk][CPT];     // of a half, of even or odd chunks
@@ -39,6 +44,10 @@ block_matmul_kernel(const __grid_constant__ MatmulParams p, const __grid_constan
   const int splits = (int)gridDim.x, rank = (int)blockIdx.x, tile = p.first + (int)blockIdx.y, tok0 = (int)blockIdx.z * TN;
   const int kb0 = (int)((long long)p.nkb * rank / splits), kb1 = (int)((long long)p.nkb * (rank + 1) / splits), n_kb = kb1 - kb0;
 
+  // Rows of the call go in fours to the CTAs of a cluster, in turns: that is whose sums a CTA gets.  [CTA][four rows][weight][row] behind the stages
+  const int toks = min(TN, p.m - tok0), fours = (toks + 3) / 4, each = (TN / 4 + splits - 1) / splits;
+  uint8_t* recv = smem + stages * kStageBytes;
+
   if (tid == 0) {
     for (int i = 0; i < stages; ++i) {
       mbar_init(&full_bar[i], 1);
@@ -46,10 +55,12 @@ block_matmul_kernel(const __grid_constant__ MatmulParams p, const __grid_constan
     }
     for (int i = 0; i < kBufs; ++i) mbar_init(&free_bar[i], kSumWarps);
     s_abort = 0;
+    mbar_init(&recv_bar, 1);
     fence_barrier_init();
+    mbar_expect_tx(&recv_bar, (uint32_t)((splits - 1) * ((fours - rank + splits - 1) / splits) * kFourBytes));
   }
   if (warp == 2) {
-    tmem_alloc(&tmem_slot, kBufs * kCols);
+    tmem_alloc(&tmem_slot, kTmem);
     tmem_relinquish();
   }
   if (warp == 0 && elect_one()) {
@@ -61,6 +72,7 @@ block_matmul_kernel(const __grid_constant__ MatmulParams p, const __grid_constan
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  if (splits > 1) cluster_arrive_relaxed();        // this CTA's barrier is ready for the others' sums (fence_barrier_init above)
   const uint32_t tmem = tmem_slot;
   // Of two launches the first lets the second begin once what precedes both is done, so that the second need not wait for the first; it
   // does so in the end, for what follows waits for the second alone.
@@ -180,48 +192,81 @@ block_matmul_kernel(const __grid_constant__ MatmulParams p, const __grid_constan
       if (lane == 0) atomicOr(p.status, VVS_DEV_TIMEOUT);
       s_abort = 1;
     }
-    // the stages have drained: the last sum is behind every MMA.  [row of the call][weight]
-    float* red = reinterpret_cast<float*>(smem);
     const int w_row = (warp & 3) * 32 + lane;
-    if (ok)
+    if (splits > 1) {
+      __syncwarp();
+      cluster_wait();
+      if (ok) {
+        int owner = half * (CPT / 4) % splits, at = half * (CPT / 4) / splits;
 #pragma unroll
-      for (int j = 0; j < CPT; ++j) red[(half * CPT + j) * 128 + w_row] = acc[j];
-  }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  if (splits > 1) cluster_sync();
-  // ---- out: four weights of a row a thread, the CTAs of a cluster share the rows ------------------------------------------------
-  const int toks = min(TN, p.m - tok0), n0 = tile * 128 + (tid & 31) * 4;
-  const uint32_t red_at = smem_u32(smem);
-  if (!s_abort && n0 < p.n) {
-    for (int r = rank + (tid >> 5) * splits; r < toks; r += (kThreads / 32) * splits) {
-      const uint32_t at = red_at + (uint32_t)(r * 128 + (tid & 31) * 4) * 4;
-      float4 x[kMaxSplits];
-#pragma unroll
-      for (int s = 0; s < kMaxSplits; ++s)
-        if (s < splits) x[s] = ld_cluster_f4(at, s);
-      float v[4] = {x[0].x, x[0].y, x[0].z, x[0].w};
-#pragma unroll
-      for (int s = 1; s < kMaxSplits; ++s)
-        if (s < splits) v[0] += x[s].x, v[1] += x[s].y, v[2] += x[s].z, v[3] += x[s].w;
-      T* o = static_cast<T*>(p.out) + (size_t)(tok0 + r) * p.out_row + n0;
-      if (p.wide && n0 + 4 <= p.n) {
-        store4(o, v);
-      } else {
-        for (int j = 0; j < 4 && n0 + j < p.n; ++j) {
-          if constexpr (sizeof(T) == 2) o[j] = __float2bfloat16_rn(v[j]);
-          else o[j] = v[j];
+        for (int q = 0; q < CPT / 4; ++q) {
+          if (half * (CPT / 4) + q < fours) {
+            uint8_t* to = recv + ((rank * each + at) * 128 + w_row) * 16;
+            if (owner == rank) st_shared4(smem_u32(to), &acc[4 * q]);
+            else st_async4(mapa(smem_u32(to), owner), mapa(smem_u32(&recv_bar), owner), &acc[4 * q]);
+          }
+          if (++owner == splits) owner = 0, ++at;
         }
       }
+    } else if (ok) {
+      // the stages have drained: the last sum is behind every MMA.  [row of the call][weight]
+      float* red = reinterpret_cast<float*>(smem);
+#pragma unroll
+      for (int j = 0; j < CPT; ++j) red[(half * CPT + j) * 128 + w_row] = acc[j];
     }
   }
   __syncwarp();
-  if (splits > 1) {                                // no CTA leaves while another reads its sums (a release would wait for the stores to out)
-    cluster_arrive_relaxed();
+  if (splits > 1 && warp < 4) cluster_wait();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (splits > 1) {
+    // ---- out, of a cluster: four rows of one weight a thread, sums in rank order -----------------------------------------------------
+    bool got = false;
+    for (uint32_t k = 0; k < kSpinLimit && !got; ++k) got = mbar_try_wait_cluster(&recv_bar, 0) || ((k & 1023u) == 1023u && s_abort);
+    if (!got) {
+      atomicOr(p.status, VVS_DEV_TIMEOUT);
+      s_abort = 1;
+    }
+    __syncwarp();
+    cluster_arrive_relaxed();                      // what was sent has come, here; waited for at the end: no CTA leaves while it may be sent to
+    const int n = tile * 128 + (tid & 127);
+    if (!s_abort && n < p.n) {
+      for (int i = tid >> 7; rank + i * splits < fours; i += kThreads / 128) {
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < kMaxSplits; ++s)
+          if (s < splits) {
+            const float4 x = *reinterpret_cast<const float4*>(recv + ((s * each + i) * 128 + (tid & 127)) * 16);
+            v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
+          }
+        const int r = (rank + i * splits) * 4;
+        T* o = static_cast<T*>(p.out) + (size_t)(tok0 + r) * p.out_row + n;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (r + j < toks) put_one(o + (size_t)j * p.out_row, v[j]);
+      }
+    }
+    __syncwarp();
     cluster_wait();
+  } else if (!s_abort) {
+    // ---- out: four weights of a row a thread ---------------------------------------------------------------------------------------
+    const int n0 = tile * 128 + (tid & 31) * 4;
+    const float* red = reinterpret_cast<const float*>(smem) + (tid & 31) * 4;
+    if (n0 < p.n)
+      for (int r = tid >> 5; r < toks; r += kThreads / 32) {
+        const float4 x = *reinterpret_cast<const float4*>(red + r * 128);
+        const float v[4] = {x.x, x.y, x.z, x.w};
+        T* o = static_cast<T*>(p.out) + (size_t)(tok0 + r) * p.out_row + n0;
+        if (p.wide && n0 + 4 <= p.n) {
+          store4(o, v);
+        } else {
+          for (int j = 0; j < 4 && n0 + j < p.n; ++j) put_one(o + j, v[j]);
+        }
+      }
   }
-  if (warp == 2) tmem_dealloc(tmem, kBufs * kCols);
+  __syncwarp();
+  if (warp == 2) tmem_dealloc(tmem, kTmem);
   if (p.chain == 2) pdl_wait();
 }
 
@@ -229,9 +274,8 @@ template <int CPT, typename T>
 int launch_cpt(const BlockMatmulArgs& g, MatmulParams p, cudaStream_t s) {
   constexpr int TN = 2 * CPT;
   auto* fn = block_matmul_kernel<CPT, T>;
-  const int smem = matmul_stages(TN) * (kTileBytes + TN * kQBlock) + 1024;
-  if (ensure_dynamic_smem(reinterpret_cast<const void*>(fn), smem) != cudaSuccess) return VVS_ERR_CUDA;
-  const int* clusters = resident_clusters(reinterpret_cast<const void*>(fn), kThreads, smem);
+  if (ensure_dynamic_smem(reinterpret_cast<const void*>(fn), matmul_room(TN) + 1024) != cudaSuccess) return VVS_ERR_CUDA;
+  const int* clusters = resident_clusters(reinterpret_cast<const void*>(fn), kThreads, matmul_smem(TN, 1));
   if (!clusters) return VVS_ERR_CUDA;
   const BlockMatmulPlan pl = plan_block_matmul(g.m, g.n, g.k, g.n_sms, clusters);
   if (pl.pairs) return launch_block_matmul_pair(g, s);
@@ -241,7 +285,6 @@ int launch_cpt(const BlockMatmulArgs& g, MatmulParams p, cudaStream_t s) {
   if (rc != VVS_OK) return rc;
   cudaLaunchConfig_t cfg = {};
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -253,11 +296,12 @@ int launch_cpt(const BlockMatmulArgs& g, MatmulParams p, cudaStream_t s) {
   for (int i = 0; i < (both ? 2 : 1); ++i) {
     const BlockMatmulPart& part = pl.part[i];
     cfg.gridDim = dim3(part.splits, (unsigned)part.count, pl.passes);
+    cfg.dynamicSmemBytes = matmul_smem(TN, part.splits);
     attr[1].val.clusterDim.x = part.splits;
     cfg.numAttrs = part.splits > 1 ? 2 : 1;
     p.first = (int)part.first;
     p.chain = both ? i + 1 : 0;
-    if (cudaLaunchKernelEx(&cfg, fn, p, tm_w, tm_a, pl.stages) != cudaSuccess) return VVS_ERR_CUDA;
+    if (cudaLaunchKernelEx(&cfg, fn, p, tm_w, tm_a, matmul_stages(TN, part.splits)) != cudaSuccess) return VVS_ERR_CUDA;
   }
   return VVS_OK;
 }

@@ -15,25 +15,38 @@ struct BlockMatmulPlan {
   bool pairs;        // block_matmul_pair.cu; the rest is of block_matmul.cu
   int tn;            // rows of a pass
   int passes;
-  int stages;        // blocks of K under way
   BlockMatmulPart part[2];                                        // the second may have no tiles
 };
 
 constexpr int kMatmulMaxSplits = 8, kMatmulMaxStages = 8;
 constexpr int kMatmulTileBytes = 128 * 128;                       // 128 rows of a block of K
 
+// Places of a block's sums in tensor memory.  The summing warps wait for them on their stage's barrier, by its parity: no more places than stages,
+// or a stage could be filled and done again before its first sums are taken.
+template <int TN>
+constexpr int kMatmulPlaces = TN <= 32 ? 4 : 2;
+inline int matmul_places(int tn) { return tn <= 32 ? kMatmulPlaces<32> : kMatmulPlaces<64>; }
+
 inline int matmul_rows(int64_t m) {                               // of a pass
   const int64_t passes = (m + 127) / 128, each = (m + passes - 1) / passes;
   return each <= 16 ? 16 : each <= 32 ? 32 : each <= 64 ? 64 : each <= 96 ? 96 : 128;
 }
-inline int matmul_stages(int tn) { return std::min(kMatmulMaxStages, (tn <= 64 ? 108 : 200) * 1024 / (kMatmulTileBytes + tn * 128)); }
+// Shared memory: blocks of K under way and, of a cluster, the sums that a CTA is sent, 128 weights of its share of the rows in fours.  Two CTAs
+// fit an SM up to 64 rows, beside their factors (64 bytes a row) and barriers.
+inline int matmul_stage_bytes(int tn) { return kMatmulTileBytes + tn * 128; }
+inline int matmul_recv_bytes(int tn, int splits) { return splits > 1 ? splits * ((tn / 4 + splits - 1) / splits) * 128 * 16 : 0; }
+inline int matmul_room(int tn) { return (tn <= 32 ? 108 : tn <= 64 ? 107 : 200) * 1024; }
+inline int matmul_stages(int tn, int splits) {
+  return std::min(kMatmulMaxStages, (matmul_room(tn) - matmul_recv_bytes(tn, splits)) / matmul_stage_bytes(tn));
+}
+// (with what brings the first stage to a multiple of 1024)
+inline int matmul_smem(int tn, int splits) { return matmul_stages(tn, splits) * matmul_stage_bytes(tn) + matmul_recv_bytes(tn, splits) + 1024; }
 
 // clusters: how many clusters of 1 .. 8 CTAs the device holds at once where each CTA has an SM (148, 74, 45, 33, 26, 22, 15, 15).
 inline BlockMatmulPlan plan_block_matmul(int64_t m, int64_t n, int64_t k, int n_sms, const int* clusters) {
   BlockMatmulPlan pl{};
   const int64_t nkb = (k + 127) / 128;
   pl.tn = matmul_rows(m);
-  pl.stages = matmul_stages(pl.tn);
   const int64_t passes = (m + pl.tn - 1) / pl.tn, tiles = (n + 127) / 128;
   pl.passes = (int)std::min<int64_t>(passes, 65535);
   // Microseconds x 100: blocks of K of the busiest SM (where two CTAs share it, one's loads fill the other's waits), and what a cluster's

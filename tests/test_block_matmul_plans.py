@@ -10,9 +10,14 @@ SHIM = """
 #include "block_plans.h"
 extern "C" void plan(long long m, long long n, long long k, int sms, const int* clusters, long long* out) {
   const vvs::BlockMatmulPlan p = vvs::plan_block_matmul(m, n, k, sms, clusters);
-  out[0] = p.pairs; out[1] = p.tn; out[2] = p.passes; out[3] = p.stages;
-  for (int i = 0; i < 2; ++i) out[4 + 3 * i] = p.part[i].first, out[5 + 3 * i] = p.part[i].count, out[6 + 3 * i] = p.part[i].splits;
+  out[0] = p.pairs; out[1] = p.tn; out[2] = p.passes;
+  for (int i = 0; i < 2; ++i) out[3 + 3 * i] = p.part[i].first, out[4 + 3 * i] = p.part[i].count, out[5 + 3 * i] = p.part[i].splits;
 }
+extern "C" int stages(int tn, int splits) { return vvs::matmul_stages(tn, splits); }
+extern "C" int recv(int tn, int splits) { return vvs::matmul_recv_bytes(tn, splits); }
+extern "C" int places(int tn) { return vvs::matmul_places(tn); }
+extern "C" int room(int tn) { return vvs::matmul_room(tn) + 1024; }
+extern "C" int smem(int tn, int splits) { return vvs::matmul_smem(tn, splits); }
 """
 SIZES = [1, 2, 15, 16, 17, 32, 33, 64, 65, 96, 97, 128, 129, 191, 192, 193, 255, 256, 257, 300, 511, 512, 1000, 5460, 70001, 1 << 24]
 # clusters of 0 .. 8 CTAs that a device holds at once, an SM each, and of a device that holds none of more than one
@@ -31,10 +36,11 @@ def plan(tmp_path_factory):
 
     def call(m, n, k, held=None):
         clusters = (ctypes.c_int * 9)(*CLUSTERS[held])
-        out = (ctypes.c_longlong * 10)()
+        out = (ctypes.c_longlong * 9)()
         so.plan(m, n, k, 148, clusters, out)
-        p = dict(zip(("pairs", "tn", "passes", "stages"), out))
-        return dict(p, parts=[tuple(out[4 + 3 * i:7 + 3 * i]) for i in range(2)], clusters=list(clusters))
+        p = dict(zip(("pairs", "tn", "passes"), out))
+        call.lib = so
+        return dict(p, parts=[tuple(out[3 + 3 * i:6 + 3 * i]) for i in range(2)], clusters=list(clusters))
     return call
 
 
@@ -54,12 +60,24 @@ def test_plans_cover_their_rows_and_weights_and_fit(plan, held):
                 for c, s in ((count * p["passes"], splits), (count_2, splits_2)):
                     assert c == 0 or 1 <= s <= 8 and s <= -(-k // 128)              # no CTA without a block of K
                     assert c == 0 or s == 1 or c <= p["clusters"][s] * (2 if p["tn"] <= 64 else 1)      # clusters that are all there at once
-                stage = 16384 + p["tn"] * 128
-                smem = p["stages"] * stage + 1024
-                # two CTAs of a pass of 64 rows at most on an SM, one otherwise (1 KB each is the system's; factors and barriers are static)
-                per_sm = 2 if p["tn"] <= 64 else 1
-                assert 2 <= p["stages"] <= 8 and smem + 64 * p["tn"] + 256 <= min(227, (228 - per_sm) / per_sm) * 1024
-                assert p["tn"] * 512 <= p["stages"] * stage                         # the sums go where the stages were
+
+
+def test_shared_memory_of_a_cta(plan):
+    plan(1, 128, 128)
+    for tn in (16, 32, 64, 96, 128):
+        for splits in range(1, 9):
+            stages, recv, smem = (f(tn, splits) for f in (plan.lib.stages, plan.lib.recv, plan.lib.smem))
+            stage = 16384 + tn * 128
+            assert 2 <= stages <= 8 and smem == stages * stage + recv + 1024 <= plan.lib.room(tn)
+            assert plan.lib.places(tn) <= stages                                    # a stage's barrier never completes twice unseen
+            # two CTAs of a pass of 64 rows at most on an SM, one otherwise (1 KB each is the system's; factors and barriers are static)
+            per_sm = 2 if tn <= 64 else 1
+            assert smem + 64 * tn + 256 <= min(227, (228 - per_sm) / per_sm) * 1024
+            if splits == 1:
+                assert tn * 512 <= stages * stage                                   # the sums go where the stages were
+            else:                                                                   # the last place that is written to
+                most = max(rank * -(-(tn // 4) // splits) + q // splits for rank in range(splits) for q in range(tn // 4))
+                assert (most * 128 + 127) * 16 + 16 <= recv
 
 
 @pytest.mark.parametrize("m,k,n", [(2100, 400, 1290), (1025, 272, 3001), (5000, 16, 1000), (1300, 1296, 2056), (300, 640, 22000), (3000, 128, 17000)])
