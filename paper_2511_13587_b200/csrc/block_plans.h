@@ -69,13 +69,14 @@ inline BlockMatmulPlan plan_block_matmul(int64_t m, int64_t n, int64_t k, int n_
   const int whole_splits = splits_of(tiles * passes, false);
   pl.part[0] = {0, tiles, whole_splits};
   int64_t whole = cost(tiles * passes, whole_splits);
-  // Tiles that are left over where all SMs have as many as the others: in a launch of their own, dealt to all SMs, beside the first one (two CTAs
-  // fit an SM).  18 rows of 4096 through 22016 weights, 172 tiles: 20.1 us as one launch (most SMs that have a CTA have two), 18.3 as 148 and 24 by
-  // six; 64 rows, whose sums take longer, 20.9 / 21.2.
+  // Tiles that are left over where all SMs have as many as the others: in a launch of their own, dealt to all SMs, up to 32 rows beside the first
+  // one (two CTAs fit an SM), with more than 64 behind it.  4096 columns through 22016 weights, 172 tiles: 18 rows 20.1 us as one launch (most SMs
+  // that have a CTA have two), 18.1 as 148 and 24 by six; 64 rows, whose sums take longer, 20.9 / 21.2; 128 rows 33.8 / 27.9.
   const int64_t full = tiles / n_sms * n_sms, left = tiles - full;
-  if (pl.tn <= 32 && full > 0 && left > 0) {
+  if ((pl.tn <= 32 || pl.tn > 64) && passes == 1 && full > 0 && left > 0) {
     const int s = splits_of(left, true);
-    const int64_t blocks = full / n_sms * nkb + (left * s + n_sms - 1) / n_sms * ((nkb + s - 1) / s), both = blocks * a_block + 530 + 20 * s;
+    const int64_t blocks = full / n_sms * nkb + (left * s + n_sms - 1) / n_sms * ((nkb + s - 1) / s);
+    const int64_t both = blocks * a_block + 530 + 20 * s + (per_sm == 1 ? full / n_sms * 350 : 0);
     if (both < whole) {
       whole = both;
       pl.part[0] = {0, full, 1};

@@ -244,7 +244,7 @@ def test_product(ctxs, dtype, rows, cols, outs):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
-@pytest.mark.parametrize("rows,cols,outs", [(18, 4096, 19000), (3, 4000, 20001)])
+@pytest.mark.parametrize("rows,cols,outs", [(18, 4096, 19000), (3, 4000, 20001), (100, 4096, 20001)])
 def test_few_rows_of_many_weights(ctxs, dtype, rows, cols, outs):
     """Two launches: tiles for all SMs, and those left over dealt to all of them.  Right behind other calls on the stream, and in a graph."""
     rng = gen.rng_for(25, f"many{rows}{cols}{outs}")
