@@ -510,7 +510,8 @@ typedef struct vvs_qweight {
 /* s = x + residual (NULL: x), y = s / sqrt(mean(s^2) + eps) * weight (T [n_cols]), out = y in 8 bits.  sum_out = s and norm_out = y, both
  * rounded to T, where they are given.  Sums and products are float32; y comes from s before it is rounded.  sum_out and norm_out may be x
  * or residual, where address and stride are the same; other overlaps are not allowed.  A row whose squares' sum is no finite float32 sets
- * VVS_DEV_NONFINITE.  n_cols <= 32768; n_rows times the blocks of a row at most 2^30, here and below. */
+ * VVS_DEV_NONFINITE.  n_cols <= 32768; below 2^30 at most, and n_rows times the blocks of a row
+ * at most 2^30 everywhere. */
 int vvs_norm_quant(vvs_ctx* ctx, int32_t n_rows, int32_t n_cols, const vvs_rows* x, const vvs_rows* residual, const void* weight, float eps,
                    const vvs_rows* sum_out, const vvs_rows* norm_out, const vvs_qrows* out, void* stream);
 

@@ -26,14 +26,14 @@ int check_qrows(const vvs_qrows* q, int n_rows, int n_cols) {
 
 int check_qweight(const vvs_qweight* w) {
   if (!w || !w->codes || !w->scale) return VVS_ERR_INVALID_ARG;
-  if (w->n_rows < 1 || w->n_cols < 16 || w->n_cols % 16 || w->n_rows > 65535 * kQBlock) return VVS_ERR_SHAPE;
+  if (w->n_rows < 1 || w->n_cols < 16 || w->n_cols % 16 || w->n_cols > kMaxCols || w->n_rows > 65535 * kQBlock) return VVS_ERR_SHAPE;
   if (w->n_rows > 1 && (w->row < w->n_cols || w->row >= (int64_t)1 << 40)) return VVS_ERR_SHAPE;
   if (!aligned16(w->codes) || (reinterpret_cast<uintptr_t>(w->scale) & 3) || (w->n_rows > 1 && w->row % 16)) return VVS_ERR_ALIGN;
   return VVS_OK;
 }
 
 bool bad_size(int n_rows, int n_cols) {
-  return n_rows < 1 || n_cols < 16 || n_cols % 16 || (int64_t)n_rows * qblocks(n_cols) > kMaxBlocks;
+  return n_rows < 1 || n_cols < 16 || n_cols % 16 || n_cols > kMaxCols || (int64_t)n_rows * qblocks(n_cols) > kMaxBlocks;
 }
 bool is_f32(const vvs_ctx* ctx) { return ctx->desc.dtype == VVS_DTYPE_FP32; }
 

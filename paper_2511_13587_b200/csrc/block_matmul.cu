@@ -34,7 +34,7 @@ __device__ __forceinline__ void put_one(float* p, float v) { *p = v; }
 template <int CPT, typename T>
 __global__ void __launch_bounds__(kThreads, CPT <= 32 ? 2 : 1)
 block_matmul_kernel(const __grid_constant__ MatmulParams p, const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_a, int stages) {
-  constexpr int TN = 2 * CPT, kBufs = kMatmulPlaces<TN>, kCols = CPT <= 16 ? 32 : CPT <= 32 ? 64 : 128, kTmem = CPT <= 32 ? 128 : 256;
+  constexpr int TN = 2 * CPT, kBufs = kMatmulPlaces<TN>, kCols = CPT <= 16 ? 32 : CPT <= 32 ? 64 : 128, kTmem = kMatmulColumns<TN>;
   static_assert(kBufs * kCols <= kTmem, "columns of tensor memory, a power of two; two CTAs fit an SM");
   constexpr uint32_t kStageBytes = kTileBytes + TN * kQBlock;
   extern __shared__ uint8_t smem_raw[];

@@ -11,6 +11,7 @@
 // scheduler, whose slots are 60 % taken; a warp's own chain (wait, factor, eight loads of eight columns with four multiply-adds each, signal) is
 // what lasts.  5460 rows of 4096 through 12288 weights: 288 us, 1.91 PFLOP/s, at the power cap (987 W, 1.3 GHz), 256 us before it is reached.
 #include "block_matmul.cuh"
+#include "block_plans.h"
 
 namespace vvs {
 
@@ -22,7 +23,9 @@ constexpr int kSumWarps = 16, kThreads = 128 + kSumWarps * 32, kStages = 4, kTil
 constexpr int kRing = 8;                           // blocks whose factors lie in shared memory
 constexpr uint32_t kStageBytes = 2 * kTileBytes, kHalfBytes = kTileBytes / 2, kOutBytes = 32 * 128;      // kOutBytes: of a summing warp
 constexpr int kFactors = 2 * 128;                  // of a block: both halves, all rows
-constexpr int kSmemBytes = kStages * kStageBytes + kSumWarps * kOutBytes + kRing * kFactors * 4 + 1024;
+// (more than it needs: two clusters that hold tensor memory on one SM each and wait for it on the other's would wait forever)
+constexpr int kSmemBytes = kMatmulPairSmem;
+static_assert(kStages * kStageBytes + kSumWarps * kOutBytes + kRing * kFactors * 4 + 1024 <= kSmemBytes, "shared memory");
 constexpr int kBand = 8;                           // tiles of rows that go through the weights together
 
 // Arrivals in another CTA.  Relaxed: what it tells of has been read from tensor memory, which tcgen05's fences order.  Release: of what this

@@ -27,6 +27,13 @@ template <int TN>
 constexpr int kMatmulPlaces = TN <= 32 ? 4 : 2;
 inline int matmul_places(int tn) { return tn <= 32 ? kMatmulPlaces<32> : kMatmulPlaces<64>; }
 
+// Columns of tensor memory of a CTA.  No kernel of the library takes a larger share of an SM's tensor memory than of its shared memory, so that
+// whatever lies on an SM together fits; a CTA of the pairs' kernel has all columns and leaves room for nothing that wants some.
+template <int TN>
+constexpr int kMatmulColumns = TN <= 64 ? 128 : 256;
+inline int matmul_columns(int tn) { return tn <= 64 ? kMatmulColumns<64> : kMatmulColumns<128>; }
+constexpr int kMatmulPairSmem = 226 * 1024;
+
 inline int matmul_rows(int64_t m) {                               // of a pass
   const int64_t passes = (m + 127) / 128, each = (m + passes - 1) / passes;
   return each <= 16 ? 16 : each <= 32 ? 32 : each <= 64 ? 64 : each <= 96 ? 96 : 128;

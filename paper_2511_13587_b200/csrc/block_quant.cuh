@@ -10,6 +10,7 @@ namespace vvs {
 
 constexpr int kQBlock = 128;                       // columns (and rows of a weight) that share a scale
 constexpr int kNormMaxCols = 32768;                // widest row of vvs_norm_quant: 512 threads of 64 elements each
+constexpr int kMaxCols = 1 << 30;                  // (a column behind the last block is still an int)
 constexpr int kMaxBlocks = 1 << 30;                // blocks of a call's rows
 __host__ __device__ __forceinline__ int qblocks(int n) { return (n + kQBlock - 1) / kQBlock; }
 

@@ -16,6 +16,8 @@ extern "C" void plan(long long m, long long n, long long k, int sms, const int* 
 extern "C" int stages(int tn, int splits) { return vvs::matmul_stages(tn, splits); }
 extern "C" int recv(int tn, int splits) { return vvs::matmul_recv_bytes(tn, splits); }
 extern "C" int places(int tn) { return vvs::matmul_places(tn); }
+extern "C" int columns(int tn) { return vvs::matmul_columns(tn); }
+extern "C" int pair_smem() { return vvs::kMatmulPairSmem; }
 extern "C" int room(int tn) { return vvs::matmul_room(tn) + 1024; }
 extern "C" int smem(int tn, int splits) { return vvs::matmul_smem(tn, splits); }
 """
@@ -78,6 +80,15 @@ def test_shared_memory_of_a_cta(plan):
             else:                                                                   # the last place that is written to
                 most = max(rank * -(-(tn // 4) // splits) + q // splits for rank in range(splits) for q in range(tn // 4))
                 assert (most * 128 + 127) * 16 + 16 <= recv
+
+
+def test_shares_of_tensor_memory(plan):
+    """At least as large a share of shared memory as of tensor memory; beside a CTA that has all 512 columns nothing fits that wants 32."""
+    plan(1, 128, 128)
+    for tn in (16, 32, 64, 96, 128):
+        for splits in range(1, 9):
+            assert plan.lib.smem(tn, splits) + 1024 >= plan.lib.columns(tn) / 512 * 228 * 1024
+    assert 228 * 1024 - (plan.lib.pair_smem() + 1024) < 32 / 512 * 228 * 1024 - 2048 and plan.lib.pair_smem() + 512 <= 227 * 1024
 
 
 @pytest.mark.parametrize("m,k,n", [(2100, 400, 1290), (1025, 272, 3001), (5000, 16, 1000), (1300, 1296, 2056), (300, 640, 22000), (3000, 128, 17000)])

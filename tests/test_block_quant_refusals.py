@@ -90,9 +90,11 @@ def test_rows_and_weights(api):
     call = lambda n=ROWS, c=COLS, x=rows(), g=None, out=qrows(), ctx=ctx: api.vvs_rows_quant(ctx, n, c, x, g, out, None)  # noqa: E731
     assert call() == REACHED and call(g=rows()) == REACHED and call(c=1 << 16) == REACHED
     assert call(ctx=None) == INVALID and call(g=rows(0)) == INVALID and call(x=None) == INVALID and call(out=None) == INVALID
+    assert call(n=1, c=1 << 30) == REACHED and call(n=1, c=(1 << 30) + 16) == SHAPE
     assert call(n=0) == SHAPE and call(c=100) == SHAPE and call(g=rows(8)) == ALIGN and call(out=qrows(row=143)) == SHAPE
     call = lambda w=rows(), ctx=ctx, **kw: api.vvs_weight_quant(ctx, w, qweight(**kw), None)  # noqa: E731
     assert call() == REACHED and call(n_rows=1, row=0) == REACHED and call(n_rows=65535 * 128) == REACHED
+    assert call(n_rows=1, n_cols=1 << 30) == REACHED and call(n_rows=1, n_cols=(1 << 30) + 16) == SHAPE
     assert call(n_rows=65535 * 128 + 1) == SHAPE and call(n_rows=0) == SHAPE and call(n_cols=24) == SHAPE and call(row=128) == SHAPE
     assert call(w=None) == INVALID and call(codes=0) == INVALID and call(scale=0) == INVALID and call(ctx=None) == INVALID
     assert call(w=rows(8)) == ALIGN and call(codes=8) == ALIGN and call(scale=6) == ALIGN and call(row=150) == ALIGN
