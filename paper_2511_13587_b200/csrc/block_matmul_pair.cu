@@ -20,19 +20,16 @@ using namespace bmm;
 namespace {
 
 constexpr int kSumWarps = 16, kThreads = 128 + kSumWarps * 32, kStages = 4, kTile = 256, kCols = 64;   // kCols: weights of a summing thread
-constexpr int kRing = 8;                           // blocks whose factors lie in shared memory
+constexpr int kBatch = 4, kBatches = 4;            // blocks whose factors are told of together; batches that lie in shared memory
 constexpr uint32_t kStageBytes = 2 * kTileBytes, kHalfBytes = kTileBytes / 2, kOutBytes = 32 * 128;      // kOutBytes: of a summing warp
 constexpr int kFactors = 2 * 128;                  // of a block: both halves, all rows
 // (more than it needs: two clusters that hold tensor memory on one SM each and wait for it on the other's would wait forever)
 constexpr int kSmemBytes = kMatmulPairSmem;
-static_assert(kStages * kStageBytes + kSumWarps * kOutBytes + kRing * kFactors * 4 + 1024 <= kSmemBytes, "shared memory");
+static_assert(kStages * kStageBytes + kSumWarps * kOutBytes + kBatches * kBatch * kFactors * 4 + 1024 <= kSmemBytes, "shared memory");
 constexpr int kBand = 8;                           // tiles of rows that go through the weights together
 
-// Arrivals in another CTA.  Relaxed: what it tells of has been read from tensor memory, which tcgen05's fences order.  Release: of what this
-// CTA's own warps will read.  One to the whole cluster waits for everything that the warp has under way, 1000 to 1600 cycles.
-__device__ __forceinline__ void mbar_release_at(uint32_t cluster_addr) {
-  asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
-}
+// An arrival in another CTA, relaxed: what it tells of has been read from tensor memory, which tcgen05's fences order, or is told of by another
+// barrier.  A release to the cluster waits for everything that the warp has under way, 1000 to 1600 cycles.
 __device__ __forceinline__ void mbar_arrive_at(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
@@ -94,9 +91,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 block_matmul_pair_kernel(const __grid_constant__ MatmulParams p, const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_a,
                          const __grid_constant__ CUtensorMap tm_out, Tiles tiles) {
   extern __shared__ uint8_t smem_raw[];
-  // full: a stage of both CTAs and its factors (in the first CTA).  done: its MMAs.  sum: a half's sums are there, free: they have been taken
-  // (by both CTAs, in the first one).
-  __shared__ __align__(8) uint64_t full_bar[kStages], done_bar[kStages], sum_bar[2][2], free_bar[2][2];
+  // full: a stage of both CTAs, and their factors (in the first CTA).  done: its MMAs.  sum: a half's sums are there, free: they have been taken
+  // (by both CTAs, in the first one).  ready: this CTA's factors of a batch
+  __shared__ __align__(8) uint64_t full_bar[kStages], done_bar[kStages], sum_bar[2][2], free_bar[2][2], ready_bar[kBatches];
   __shared__ uint32_t tmem_slot;
   __shared__ volatile int s_abort;
 
@@ -116,6 +113,7 @@ block_matmul_pair_kernel(const __grid_constant__ MatmulParams p, const __grid_co
       mbar_init(&sum_bar[0][i], 1);
       mbar_init(&free_bar[0][i], kSumWarps);       // half of either CTA's
     }
+    for (int i = 0; i < kBatches; ++i) mbar_init(&ready_bar[i], 2);
     s_abort = 0;
     fence_barrier_init();
     tma_prefetch_desc(&tm_w);
@@ -189,12 +187,11 @@ block_matmul_pair_kernel(const __grid_constant__ MatmulParams p, const __grid_co
     }
   } else if (warp < 4) {
     // ---- factors: a thread has two rows, and both halves' weights ------------------------------------------------------------------
-    // A second producer: a block's factors are counted with its stage, so that its sums' barrier stands for them too.  Their place is that of
-    // eight blocks before: the MMAs of four blocks before are done, which waited for the sums of six before to be taken.
-    constexpr int kAhead = 4;                      // blocks whose scales are requested together, while those before are put down
+    // A second producer: no block's MMAs begin without its factors.  Their place is that of eight blocks before at least (a tile's last batch may
+    // have two): the MMAs of four blocks before are done, which waited for the sums of six before to be taken.
     const int r0 = (warp - 2) * 32 + lane;
     Ring<kStages> st(1);
-    int count = 0;
+    int count = 0, batch = 0;
     for (int id = first; id < n_tiles && ok; id += step) {
       int mt, nt;
       tiles.place(id, mt, nt);
@@ -202,10 +199,10 @@ block_matmul_pair_kernel(const __grid_constant__ MatmulParams p, const __grid_co
       const bool there[2] = {row < p.m, row + 64 < p.m}, second = nt * kTile + 128 < p.n;
       const float* as[2] = {p.a_scale + (size_t)(there[0] ? row : 0) * p.nkb, p.a_scale + (size_t)(there[1] ? row + 64 : 0) * p.nkb};
       const float* ws[2] = {p.w_scale + (size_t)(2 * nt) * p.nkb, p.w_scale + (size_t)(2 * nt + second) * p.nkb};
-      float a[2][kAhead], w[2][kAhead];
+      float a[2][kBatch], w[2][kBatch];
       auto request = [&](int kb) {
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j)
+        for (int j = 0; j < kBatch; ++j)
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             a[h][j] = there[h] && kb + j < p.nkb ? __ldg(as[h] + kb + j) : 0.f;     // rows that are not there: factors of nothing
@@ -213,25 +210,28 @@ block_matmul_pair_kernel(const __grid_constant__ MatmulParams p, const __grid_co
           }
       };
       request(0);
-      for (int kb = 0; kb < nkb && ok; kb += kAhead) {
-        float f[kAhead][4];
+      for (int kb = 0; kb < nkb && ok; kb += kBatch) {
+        float f[kBatch][4];
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j)
+        for (int j = 0; j < kBatch; ++j)
 #pragma unroll
           for (int h = 0; h < 4; ++h) f[j][h] = a[h & 1][j] * w[h >> 1][j];
-        request(kb + kAhead);
+        request(kb + kBatch);
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
+        for (int j = 0; j < kBatch; ++j) {
           if (kb + j >= nkb || !ok) break;
           if (count >= kStages && !(ok = warp_wait_or_abort(&done_bar[st.at], st.par, &s_abort))) break;
-          float* to = factors + (count & (kRing - 1)) * kFactors + r0;
+          float* to = factors + ((batch % kBatches) * kBatch + j) * kFactors + r0;
 #pragma unroll
           for (int h = 0; h < 4; ++h) to[(h >> 1) * 128 + (h & 1) * 64] = f[j][h];
           __syncwarp();
-          if (lane == 0) mbar_release_at(mapa(smem_u32(&full_bar[st.at]), 0));
+          if (lane == 0) mbar_arrive_at(mapa(smem_u32(&full_bar[st.at]), 0));
           st.next();
           ++count;
         }
+        if (!ok) break;
+        if (lane == 0) mbar_arrive(&ready_bar[batch % kBatches]);
+        ++batch;
       }
     }
   } else {
@@ -239,15 +239,19 @@ block_matmul_pair_kernel(const __grid_constant__ MatmulParams p, const __grid_co
     const int group = (warp - 4) >> 2, half = group >> 1, quad = warp & 3;
     const uint32_t t_row = tmem + ((uint32_t)(quad * 32) << 16) + group * kCols;
     const uint32_t my_factor = smem_u32(factors) + (uint32_t)(half * 128 + quad * 32 + lane) * 4;
-    const uint32_t sum0 = smem_u32(&sum_bar[half][0]), free0 = mapa(smem_u32(&free_bar[half][0]), 0);
-    uint32_t turn = 0;                             // pairs of blocks so far
+    const uint32_t ready0 = smem_u32(&ready_bar[0]), sum0 = smem_u32(&sum_bar[half][0]), free0 = mapa(smem_u32(&free_bar[half][0]), 0);
+    uint32_t turn = 0, batch = 0;                  // pairs of blocks so far, and batches of factors
     for (int id = first; id < n_tiles && ok; id += step) {
       Two acc[kCols / 2];
 #pragma unroll
       for (int j = 0; j < kCols / 2; ++j) acc[j] = 0;
 #pragma unroll 1
       for (int kb = 0; kb < nkb; kb += 2, ++turn) {
-        const uint32_t factor_at = my_factor + (turn & (kRing / 2 - 1)) * (2 * kFactors * 4);
+        if (kb % kBatch == 0) {
+          if (!(ok = warp_wait_lean(ready0 + batch % kBatches * 8, batch / kBatches & 1, &s_abort))) break;
+          ++batch;
+        }
+        const uint32_t factor_at = my_factor + ((batch - 1) % kBatches * kBatch + kb % kBatch) * (kFactors * 4);
 #pragma unroll
         for (int buf = 0; buf < 2; ++buf) {
           if (!(ok = warp_wait_lean(sum0 + buf * 8, turn & 1, &s_abort))) break;

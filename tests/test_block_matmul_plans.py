@@ -91,7 +91,7 @@ def test_shares_of_tensor_memory(plan):
     assert 228 * 1024 - (plan.lib.pair_smem() + 1024) < 32 / 512 * 228 * 1024 - 2048 and plan.lib.pair_smem() + 512 <= 227 * 1024
 
 
-@pytest.mark.parametrize("m,k,n", [(2100, 400, 1290), (1025, 272, 3001), (5000, 16, 1000), (1300, 1296, 2056), (300, 640, 22000), (3000, 128, 17000)])
+@pytest.mark.parametrize("m,k,n", [(2100, 400, 1290), (1025, 272, 3001), (5000, 16, 1000), (1300, 1296, 2056), (300, 640, 22000), (3000, 128, 17000), (20000, 16, 1000), (9000, 272, 1288)])
 def test_sizes_of_the_gpu_tests_on_pairs(plan, m, k, n):
     assert plan(m, n, k)["pairs"]
 
