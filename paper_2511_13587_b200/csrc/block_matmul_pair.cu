@@ -9,7 +9,7 @@
 //
 // Bound by the summing warps: 690 cycles a block of K, where its MMAs take 512 and shared memory's fill from L2 575 (32 KB).  Four of them share a
 // scheduler, whose slots are 60 % taken; a warp's own chain (wait, factor, eight loads of eight columns with four multiply-adds each, signal) is
-// what lasts.  5460 rows of 4096 through 12288 weights: 288 us, 1.91 PFLOP/s, at the power cap (987 W, 1.3 GHz), 256 us before it is reached.
+// what lasts.  5460 rows of 4096 through 12288 weights: 284 us, 1.94 PFLOP/s, at the power cap (987 W, 1.3 GHz), 252 us before it is reached.
 #include "block_matmul.cuh"
 #include "block_plans.h"
 

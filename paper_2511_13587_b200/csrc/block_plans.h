@@ -67,9 +67,9 @@ inline BlockMatmulPlan plan_block_matmul(int64_t m, int64_t n, int64_t k, int n_
   // Clusters that do not all fit at once wait for others' end and gain nothing; a CTA has two blocks at least.  288 rows of 3456 through 1280
   // weights, 30 tiles: 1 / 2 / 4 CTAs a tile 13.3 / 9.7 / 8.2 us; 18 rows of 4096 through 4096, 32 tiles, 1 / 2 / 4 / 8: 11.2 / 8.7 / 7.2 / 7.1.
   // Numbers between are slower where all SMs have work already (96 tiles of 32 blocks, 2 / 3: 12.9 / 14.0; ten of ten, 4 / 5: 4.1 / 4.5).
-  auto splits_of = [&](int64_t count, bool any) {
+  auto splits_of = [&](int64_t count, bool beside) {              // beside others: a CTA an SM, any number
     int best = 1;
-    for (int s = 2; s <= kMatmulMaxSplits && 2 * s <= nkb && count <= (int64_t)clusters[s] * per_sm; s += any ? 1 : s)
+    for (int s = 2; s <= kMatmulMaxSplits && 2 * s <= nkb && count <= (int64_t)clusters[s] * (beside ? 1 : per_sm); s += beside ? 1 : s)
       if (cost(count, s) < cost(count, best)) best = s;
     return best;
   };
@@ -78,7 +78,7 @@ inline BlockMatmulPlan plan_block_matmul(int64_t m, int64_t n, int64_t k, int n_
   int64_t whole = cost(tiles * passes, whole_splits);
   // Tiles that are left over where all SMs have as many as the others: in a launch of their own, dealt to all SMs, up to 32 rows beside the first
   // one (two CTAs fit an SM), with more than 64 behind it.  4096 columns through 22016 weights, 172 tiles: 18 rows 20.1 us as one launch (most SMs
-  // that have a CTA have two), 18.1 as 148 and 24 by six; 64 rows, whose sums take longer, 20.9 / 21.2; 128 rows 33.8 / 27.9.
+  // that have a CTA have two), 18.0 as 148 and 24 by five (by six, of which 22 fit beside the 148, 18.1); 64 rows, whose sums take longer, 20.9 / 21.2; 128 rows 33.8 / 26.7.
   const int64_t full = tiles / n_sms * n_sms, left = tiles - full;
   if ((pl.tn <= 32 || pl.tn > 64) && passes == 1 && full > 0 && left > 0) {
     const int s = splits_of(left, true);

@@ -6,7 +6,7 @@
 // warp has a block of 128 columns, eight elements a lane; SwiGLU's also by the exponential's and the reciprocal's pipe (64 % of its rate).
 // Weights: a CTA has a block of 128 x 128, eight units of eight elements a thread.
 //
-// 5460 rows of 11008, gate and up: 57 us, 5.3 TB/s (82 % of a copy's rate); 18 of 3456 3.7 us, as long as the call.  22016 x 4096 weights 46 us, 5.8 TB/s
+// 5460 rows of 11008, gate and up: 57 us, 5.3 TB/s (82 % of a copy's rate); 18 of 3456 3.4 us, as long as the call (1.2 in a graph).  22016 x 4096 weights 46 us, 5.8 TB/s
 // (three CTAs of 256 threads an SM; two of 512 50 us, one of 1024 88).
 #include "block_quant.cuh"
 

@@ -59,9 +59,10 @@ def test_plans_cover_their_rows_and_weights_and_fit(plan, held):
                 (first, count, splits), (first_2, count_2, splits_2) = p["parts"]
                 assert first == 0 and count >= 1 and count + count_2 == -(-n // 128) <= 65535
                 assert count_2 == 0 or (first_2 == count and p["passes"] == 1)
-                for c, s in ((count * p["passes"], splits), (count_2, splits_2)):
-                    assert c == 0 or 1 <= s <= 8 and s <= -(-k // 128)              # no CTA without a block of K
-                    assert c == 0 or s == 1 or c <= p["clusters"][s] * (2 if p["tn"] <= 64 else 1)      # clusters that are all there at once
+                # no CTA without a block of K, clusters that are all there at once; the second launch's beside the first one's CTAs
+                for c, s, slots in ((count * p["passes"], splits, 2 if p["tn"] <= 64 else 1), (count_2, splits_2, 1)):
+                    assert c == 0 or 1 <= s <= 8 and s <= -(-k // 128)
+                    assert c == 0 or s == 1 or c <= p["clusters"][s] * slots
 
 
 def test_shared_memory_of_a_cta(plan):
@@ -98,7 +99,7 @@ def test_sizes_of_the_gpu_tests_on_pairs(plan, m, k, n):
 
 def test_few_rows_stay_with_the_weights_and_many_go_on_pairs(plan):
     assert not plan(1, 1280, 1280)["pairs"] and plan(1, 1280, 1280)["parts"][0] == (0, 10, 4)
-    assert not plan(18, 22016, 4096)["pairs"] and plan(18, 22016, 4096)["parts"] == [(0, 148, 1), (148, 24, 6)]
+    assert not plan(18, 22016, 4096)["pairs"] and plan(18, 22016, 4096)["parts"] == [(0, 148, 1), (148, 24, 5)]
     assert not plan(288, 1280, 3456)["pairs"] and plan(288, 1280, 3456)["parts"][0] == (0, 10, 4)
     assert plan(5460, 12288, 4096)["pairs"] and plan(1 << 24, 16, 128)["pairs"]
 
