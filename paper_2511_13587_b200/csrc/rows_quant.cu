@@ -15,7 +15,7 @@ namespace vvs {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kFlight = 4;                         // rows whose elements are on their way together
+constexpr int kFlight = 4;                         // rows whose elements are on their way together (four CTAs an SM 51.9 us; three, five CTAs 51.9; two, eight 54.9)
 
 // gate / (1 + e^-gate) * x
 __device__ __forceinline__ float gated(float gate, float x) {
