@@ -74,7 +74,7 @@ SIZES = [(1, 16), (1, 128), (2, 144), (3, 256), (4, 272), (5, 1280), (18, 1376),
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
-@pytest.mark.parametrize("rows,cols", SIZES)
+@pytest.mark.parametrize("rows,cols", SIZES + [(2500, 1040), (1300, 4096)])
 def test_norm(ctxs, dtype, rows, cols):
     rng = gen.rng_for(21, f"norm{rows}{cols}")
     x, r = (dev(rng.standard_normal((rows, cols)) * np.exp(rng.standard_normal((rows, 1))), dtype) for _ in range(2))
