@@ -78,7 +78,8 @@ inline BlockMatmulPlan plan_block_matmul(int64_t m, int64_t n, int64_t k, int n_
   int64_t whole = cost(tiles * passes, whole_splits);
   // Tiles that are left over where all SMs have as many as the others: in a launch of their own, dealt to all SMs, up to 32 rows beside the first
   // one (two CTAs fit an SM), with more than 64 behind it.  4096 columns through 22016 weights, 172 tiles: 18 rows 20.1 us as one launch (most SMs
-  // that have a CTA have two), 18.0 as 148 and 24 by five (by six, of which 22 fit beside the 148, 18.1); 64 rows, whose sums take longer, 20.9 / 21.2; 128 rows 33.8 / 26.7.
+  // that have a CTA have two), 18.0 as 148 and 24 by five (by six, of which 22 fit beside the 148, 18.1); 64
+  // rows, whose sums take longer, 20.9 / 21.2; 128 rows 33.8 / 26.7.
   const int64_t full = tiles / n_sms * n_sms, left = tiles - full;
   if ((pl.tn <= 32 || pl.tn > 64) && passes == 1 && full > 0 && left > 0) {
     const int s = splits_of(left, true);
