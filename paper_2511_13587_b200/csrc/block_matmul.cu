@@ -167,7 +167,7 @@ block_matmul_kernel(const __grid_constant__ MatmulParams p, const __grid_constan
         if (ok) {
           tc_fence_after();
           const float4* f = reinterpret_cast<const float4*>(&s_factor[half][c & 1][b][0]);
-          constexpr int kLd = CPT < 16 ? 8 : 16, kPieces = CPT / kLd;
+          constexpr int kLd = CPT % 16 ? 8 : 16, kPieces = CPT / kLd;
           float part[kPieces > 1 ? 2 : 1][kLd];
           tmem_request(t_row + buf * kCols, part[0]);
 #pragma unroll
@@ -331,6 +331,7 @@ int launch_rows(const BlockMatmulArgs& g, const MatmulParams& p, cudaStream_t s)
   switch (matmul_rows(g.m)) {
     case 16: return launch_cpt<8, T>(g, p, s);
     case 32: return launch_cpt<16, T>(g, p, s);
+    case 48: return launch_cpt<24, T>(g, p, s);
     case 64: return launch_cpt<32, T>(g, p, s);
     case 96: return launch_cpt<48, T>(g, p, s);
     default: return launch_cpt<64, T>(g, p, s);

@@ -34,9 +34,11 @@ constexpr int kMatmulColumns = TN <= 64 ? 128 : 256;
 inline int matmul_columns(int tn) { return tn <= 64 ? kMatmulColumns<64> : kMatmulColumns<128>; }
 constexpr int kMatmulPairSmem = 226 * 1024;
 
-inline int matmul_rows(int64_t m) {                               // of a pass
+// Rows of a pass: the fewest that hold what a pass has.  36 rows through passes of 48 / 64: of 4096 through 22016 weights 19.1 / 19.7 us, 11008 through
+// 4096 13.7 / 14.5, 1280 through 1280 4.0 / 4.2.
+inline int matmul_rows(int64_t m) {
   const int64_t passes = (m + 127) / 128, each = (m + passes - 1) / passes;
-  return each <= 16 ? 16 : each <= 32 ? 32 : each <= 64 ? 64 : each <= 96 ? 96 : 128;
+  return each <= 16 ? 16 : each <= 32 ? 32 : each <= 48 ? 48 : each <= 64 ? 64 : each <= 96 ? 96 : 128;
 }
 // Shared memory: blocks of K under way and, of a cluster, the sums that a CTA is sent, 128 weights of its share of the rows in fours.  Two CTAs
 // fit an SM up to 64 rows, beside their factors (64 bytes a row) and barriers.
@@ -58,7 +60,7 @@ inline BlockMatmulPlan plan_block_matmul(int64_t m, int64_t n, int64_t k, int n_
   pl.passes = (int)std::min<int64_t>(passes, 65535);
   // Microseconds x 100: blocks of K of the busiest SM (where two CTAs share it, one's loads fill the other's waits), and what a cluster's
   // exchange costs.
-  const int64_t a_block = pl.tn <= 32 ? 24 : pl.tn <= 64 ? 32 : pl.tn <= 96 ? 42 : 50;
+  const int64_t a_block = pl.tn <= 32 ? 24 : pl.tn <= 48 ? 28 : pl.tn <= 64 ? 32 : pl.tn <= 96 ? 42 : 50;
   const int per_sm = pl.tn <= 64 ? 2 : 1;
   auto cost = [&](int64_t count, int s) {
     const int64_t each = (count * s + n_sms - 1) / n_sms, rounds = (each + per_sm - 1) / per_sm, blocks = (nkb + s - 1) / s;
@@ -76,12 +78,12 @@ inline BlockMatmulPlan plan_block_matmul(int64_t m, int64_t n, int64_t k, int n_
   const int whole_splits = splits_of(tiles * passes, false);
   pl.part[0] = {0, tiles, whole_splits};
   int64_t whole = cost(tiles * passes, whole_splits);
-  // Tiles that are left over where all SMs have as many as the others: in a launch of their own, dealt to all SMs, up to 32 rows beside the first
+  // Tiles that are left over where all SMs have as many as the others: in a launch of their own, dealt to all SMs, up to 48 rows beside the first
   // one (two CTAs fit an SM), with more than 64 behind it.  4096 columns through 22016 weights, 172 tiles: 18 rows 20.1 us as one launch (most SMs
-  // that have a CTA have two), 18.0 as 148 and 24 by five (by six, of which 22 fit beside the 148, 18.1); 64
-  // rows, whose sums take longer, 20.9 / 21.2; 128 rows 33.8 / 26.7.
+  // that have a CTA have two), 18.0 as 148 and 24 by five (by six, of which 22 fit beside the 148, 18.1); 64 rows, whose sums take longer,
+  // 20.9 / 21.2; 128 rows 33.8 / 26.7.
   const int64_t full = tiles / n_sms * n_sms, left = tiles - full;
-  if ((pl.tn <= 32 || pl.tn > 64) && passes == 1 && full > 0 && left > 0) {
+  if ((pl.tn <= 48 || pl.tn > 64) && passes == 1 && full > 0 && left > 0) {
     const int s = splits_of(left, true);
     const int64_t blocks = full / n_sms * nkb + (left * s + n_sms - 1) / n_sms * ((nkb + s - 1) / s);
     const int64_t both = blocks * a_block + 530 + 20 * s + (per_sm == 1 ? full / n_sms * 350 : 0);

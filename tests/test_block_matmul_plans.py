@@ -21,7 +21,7 @@ extern "C" int pair_smem() { return vvs::kMatmulPairSmem; }
 extern "C" int room(int tn) { return vvs::matmul_room(tn) + 1024; }
 extern "C" int smem(int tn, int splits) { return vvs::matmul_smem(tn, splits); }
 """
-SIZES = [1, 2, 15, 16, 17, 32, 33, 64, 65, 96, 97, 128, 129, 191, 192, 193, 255, 256, 257, 300, 511, 512, 1000, 5460, 70001, 1 << 24]
+SIZES = [1, 2, 15, 16, 17, 32, 33, 48, 49, 64, 65, 96, 97, 128, 129, 191, 192, 193, 255, 256, 257, 300, 511, 512, 1000, 5460, 70001, 1 << 24]
 # clusters of 0 .. 8 CTAs that a device holds at once, an SM each, and of a device that holds none of more than one
 CLUSTERS = {None: [0, 148, 74, 45, 33, 26, 22, 15, 15], 0: [0, 148] + [0] * 7}
 
@@ -54,7 +54,7 @@ def test_plans_cover_their_rows_and_weights_and_fit(plan, held):
                 p = plan(m, n, k, held)
                 if p["pairs"]:
                     continue
-                assert p["tn"] in (16, 32, 64, 96, 128) and 1 <= p["passes"] <= 65535 and p["tn"] * p["passes"] >= m, (m, n, k)
+                assert p["tn"] in (16, 32, 48, 64, 96, 128) and 1 <= p["passes"] <= 65535 and p["tn"] * p["passes"] >= m, (m, n, k)
                 assert p["tn"] * (p["passes"] - 1) < m                              # no pass without rows
                 (first, count, splits), (first_2, count_2, splits_2) = p["parts"]
                 assert first == 0 and count >= 1 and count + count_2 == -(-n // 128) <= 65535
@@ -67,7 +67,7 @@ def test_plans_cover_their_rows_and_weights_and_fit(plan, held):
 
 def test_shared_memory_of_a_cta(plan):
     plan(1, 128, 128)
-    for tn in (16, 32, 64, 96, 128):
+    for tn in (16, 32, 48, 64, 96, 128):
         for splits in range(1, 9):
             stages, recv, smem = (f(tn, splits) for f in (plan.lib.stages, plan.lib.recv, plan.lib.smem))
             stage = 16384 + tn * 128
@@ -86,7 +86,7 @@ def test_shared_memory_of_a_cta(plan):
 def test_shares_of_tensor_memory(plan):
     """At least as large a share of shared memory as of tensor memory; beside a CTA that has all 512 columns nothing fits that wants 32."""
     plan(1, 128, 128)
-    for tn in (16, 32, 64, 96, 128):
+    for tn in (16, 32, 48, 64, 96, 128):
         for splits in range(1, 9):
             assert plan.lib.smem(tn, splits) + 1024 >= plan.lib.columns(tn) / 512 * 228 * 1024
     assert 228 * 1024 - (plan.lib.pair_smem() + 1024) < 32 / 512 * 228 * 1024 - 2048 and plan.lib.pair_smem() + 512 <= 227 * 1024
@@ -104,6 +104,6 @@ def test_few_rows_stay_with_the_weights_and_many_go_on_pairs(plan):
     assert plan(5460, 12288, 4096)["pairs"] and plan(1 << 24, 16, 128)["pairs"]
 
 
-@pytest.mark.parametrize("m,k,n", [(18, 4096, 19000), (3, 4000, 20001), (100, 4096, 20001)])
+@pytest.mark.parametrize("m,k,n", [(18, 4096, 19000), (3, 4000, 20001), (36, 4096, 19000), (100, 4096, 20001)])
 def test_sizes_of_the_gpu_tests_in_two_launches(plan, m, k, n):
     assert plan(m, n, k)["parts"][1][1] > 0

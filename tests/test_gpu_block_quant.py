@@ -221,7 +221,8 @@ def check_product(out, ops, rows=None):
 
 
 PRODUCTS = [(1, 16, 1), (1, 128, 128), (1, 1280, 1280), (2, 144, 127), (8, 112, 129), (15, 4096, 200), (16, 256, 640), (17, 1376, 999), (18, 2064, 384),
-            (32, 128, 3000), (33, 320, 130), (40, 5984, 4000), (64, 1280, 257), (64, 11008, 512), (30, 6000, 520), (100, 7008, 400), (10, 8016, 130), (65, 1296, 512), (96, 640, 100), (97, 256, 64), (128, 3456, 300), (129, 128, 1000),
+            (32, 128, 3000), (33, 320, 130), (40, 5984, 4000), (36, 1280, 1280), (45, 144, 1290), (48, 11008, 512), (49, 640, 300), (64, 1280, 257),
+            (64, 11008, 512), (30, 6000, 520), (100, 7008, 400), (10, 8016, 130), (65, 1296, 512), (96, 640, 100), (97, 256, 64), (128, 3456, 300), (129, 128, 1000),
             (200, 1360, 700), (257, 512, 640), (300, 2048, 1000), (513, 384, 520), (1030, 272, 650), (1500, 1040, 1290), (2100, 128, 260),
             # on pairs of CTAs: odd blocks of K, results that end anywhere, tiles of rows and weights that are not full, one tile and many
             (2100, 400, 1290), (1025, 272, 3001), (5000, 16, 1000), (1300, 1296, 2056), (300, 640, 22000), (3000, 128, 17000), (20000, 16, 1000), (9000, 272, 1288)]
@@ -244,7 +245,7 @@ def test_product(ctxs, dtype, rows, cols, outs):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
-@pytest.mark.parametrize("rows,cols,outs", [(18, 4096, 19000), (3, 4000, 20001), (100, 4096, 20001)])
+@pytest.mark.parametrize("rows,cols,outs", [(18, 4096, 19000), (3, 4000, 20001), (36, 4096, 19000), (100, 4096, 20001)])
 def test_few_rows_of_many_weights(ctxs, dtype, rows, cols, outs):
     """Two launches: tiles for all SMs, and those left over dealt to all of them.  Right behind other calls on the stream, and in a graph."""
     rng = gen.rng_for(25, f"many{rows}{cols}{outs}")
