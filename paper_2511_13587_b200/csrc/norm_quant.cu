@@ -85,12 +85,14 @@ __global__ void __launch_bounds__(512) norm_quant_kernel(NormQuantArgs a) {
     if (a.norm_out.data && there && u < units)
       store_unit(static_cast<T*>(a.norm_out.data) + row * a.norm_out.row + 8 * u, false, 0, narrow_unit(y[j], x[j]));
     float m = amax8(y[j]);
-    if (odd(m)) {
-      strange = true;
-      m = amax8_finite(y[j]);
-    }
+    const bool some = odd(m);
+    if (some) m = amax8_finite(y[j]);
     const float scale = block_scale(half_warp_max(m));
-    const uint2 c = codes8(y[j], scale_inverse(scale));
+    if (some) {
+      strange = true;
+      hold8(y[j], scale);
+    }
+    const uint2 c = codes8(y[j], scale, minus_inverse(scale));
     if (there && u < units) {
       *reinterpret_cast<uint2*>(a.codes + row * a.codes_row + 8 * u) = c;
       if ((u & 15) == 0) a.scale[(size_t)row * nb + (u >> 4)] = scale;

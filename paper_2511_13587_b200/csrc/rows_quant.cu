@@ -59,13 +59,15 @@ __global__ void __launch_bounds__(kThreads, 4) rows_quant_kernel(RowsQuantArgs a
         for (int e = 0; e < 8; ++e) y[e] = gated(z[e], y[e]);
       }
       float m = amax8(y);
-      if (odd(m)) {
-        strange = true;
-        m = amax8_finite(y);
-      }
+      const bool some = odd(m);
+      if (some) m = amax8_finite(y);
       const float scale = block_scale(half_warp_max(m));
+      if (some) {
+        strange = true;
+        hold8(y, scale);
+      }
       if (in) {
-        *reinterpret_cast<uint2*>(codes) = codes8(y, scale_inverse(scale));
+        *reinterpret_cast<uint2*>(codes) = codes8(y, scale, minus_inverse(scale));
         if ((threadIdx.x & 15) == 0) *scale_at = scale;
       }
       codes += a.codes_row;
@@ -107,15 +109,18 @@ __global__ void __launch_bounds__(kThreads, 3) weight_quant_kernel(RowsQuantArgs
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < kThreads / 32; ++i) m = fmaxf(m, s_max[i]);
-  const float scale = block_scale(m), inv = scale_inverse(scale);
+  const float scale = block_scale(m), inv = minus_inverse(scale);
   if (threadIdx.x == 0) a.scale[(size_t)blockIdx.y * gridDim.x + blockIdx.x] = scale;
 #pragma unroll
   for (int j = 0; j < kUnits; ++j) {
     const long long row = r0 + j * kRows;
     float y[8];
     widen_unit(x[j], y);
-    if (strange) amax8_finite(y);
-    if (in && row < a.n_rows) *reinterpret_cast<uint2*>(a.codes + row * a.codes_row + col) = codes8(y, inv);
+    if (strange) {
+      amax8_finite(y);
+      hold8(y, scale);
+    }
+    if (in && row < a.n_rows) *reinterpret_cast<uint2*>(a.codes + row * a.codes_row + col) = codes8(y, scale, inv);
   }
   if (strange) atomicOr(a.status, VVS_DEV_NONFINITE);
 }
