@@ -15,7 +15,10 @@ namespace vvs {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kFlight = 4;                         // rows whose elements are on their way together (four CTAs an SM 51.9 us; three, five CTAs 51.9; two, eight 54.9)
+// Rows whose elements are on their way together, at four CTAs an SM: four (two, eight CTAs: 5 % slower), of float32 with gates two, for four do not fit
+// the registers (2730 rows of 11008: 41.5 us, with four 64).
+template <typename T, bool GATE>
+constexpr int kFlight = sizeof(T) == 4 && GATE ? 2 : 4;
 
 // gate / (1 + e^-gate) * x
 __device__ __forceinline__ float gated(float gate, float x) {
@@ -27,6 +30,7 @@ __device__ __forceinline__ float gated(float gate, float x) {
 // A CTA has up to sixteen blocks of columns, a half warp each, and goes through `each` rows.
 template <typename T, bool GATE>
 __global__ void __launch_bounds__(kThreads, 4) rows_quant_kernel(RowsQuantArgs a, int each) {
+  constexpr int kAt = kFlight<T, GATE>;
   grid_dep_launch();
   grid_dep_wait();
   const int nb = qblocks(a.n_cols), block = blockIdx.x * (blockDim.x >> 4) + (threadIdx.x >> 4), col = block * kQBlock + 8 * (threadIdx.x & 15);
@@ -37,10 +41,10 @@ __global__ void __launch_bounds__(kThreads, 4) rows_quant_kernel(RowsQuantArgs a
   uint8_t* codes = a.codes + (int64_t)r0 * a.codes_row + col;
   float* scale_at = a.scale + (size_t)r0 * nb + block;
   bool strange = false;
-  for (int r = r0; r < r1; r += kFlight) {
-    Unit<T> ux[kFlight], ug[kFlight];
+  for (int r = r0; r < r1; r += kAt) {
+    Unit<T> ux[kAt], ug[kAt];
 #pragma unroll
-    for (int j = 0; j < kFlight; ++j) {
+    for (int j = 0; j < kAt; ++j) {
       const bool there = in && r + j < r1;
       ux[j] = there ? load_unit(x, false, 0) : no_unit<T>();
       if (GATE) ug[j] = there ? load_unit(g, false, 0) : no_unit<T>();
@@ -48,7 +52,7 @@ __global__ void __launch_bounds__(kThreads, 4) rows_quant_kernel(RowsQuantArgs a
       if (GATE) g += a.gate.row;
     }
 #pragma unroll
-    for (int j = 0; j < kFlight; ++j) {
+    for (int j = 0; j < kAt; ++j) {
       if (r + j >= r1) break;                      // (of all lanes)
       float y[8];
       widen_unit(ux[j], y);
@@ -133,7 +137,7 @@ int launch_rows_quant(const RowsQuantArgs& a, cudaStream_t s) {
   const int nb = qblocks(a.n_cols), groups = (nb + 15) / 16, mine = ((nb + groups - 1) / groups + 1) & ~1;
   const long long most = std::max(1LL, (long long)a.n_sms * 4 * (kThreads / (16 * mine)) / groups);
   long long each = (a.n_rows + most - 1) / most;
-  if (each > 1) each = (each + kFlight - 1) / kFlight * kFlight;
+  if (each > 1) each = (each + 3) / 4 * 4;          // (of either number in flight)
   each = std::max(each, (a.n_rows + 65534LL) / 65535);
   auto* fn = a.gate.data ? rows_quant_kernel<T, true> : rows_quant_kernel<T, false>;
   const cudaError_t e =
