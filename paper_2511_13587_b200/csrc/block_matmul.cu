@@ -45,7 +45,11 @@ block_matmul_kernel(const __grid_constant__ MatmulParams p, const __grid_constan
 
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
-  const int splits = (int)gridDim.x, rank = (int)blockIdx.x, tile = p.first + (int)blockIdx.y, tok0 = (int)blockIdx.z * TN;
+  // (of a product in two parts the first clusters have a tile of the first part in each CTA, the others a tile of the second part together)
+  const bool alone = (int)blockIdx.y < p.alone;
+  const int splits = alone ? 1 : (int)gridDim.x, rank = alone ? 0 : (int)blockIdx.x, tok0 = (int)blockIdx.z * TN;
+  const int tile = alone ? (int)(blockIdx.y * gridDim.x + blockIdx.x) : p.first + (int)blockIdx.y - p.alone;
+  if (alone && tile >= p.first) return;
   const int kb0 = (int)((long long)p.nkb * rank / splits), kb1 = (int)((long long)p.nkb * (rank + 1) / splits), n_kb = kb1 - kb0;
 
   // Rows of the call go in fours to the CTAs of a cluster, in turns: that is whose sums a CTA gets.  [CTA][four rows][weight][row] behind the stages
@@ -78,11 +82,10 @@ block_matmul_kernel(const __grid_constant__ MatmulParams p, const __grid_constan
   tc_fence_after();
   if (splits > 1) cluster_arrive_relaxed();        // this CTA's barrier is ready for the others' sums (fence_barrier_init above)
   const uint32_t tmem = tmem_slot;
-  // Of two launches the first lets the second begin once what precedes both is done, so that the second need not wait for the first; it
-  // does so in the end, for what follows waits for the second alone.
-  if (p.chain != 1) pdl_launch_dependents();
-  if (p.chain != 2) pdl_wait();
-  if (p.chain == 1) pdl_launch_dependents();
+  // (Of two launches the second waits for the first, of which it needs nothing: only behind a wait of its own does a launch see what those
+  // before it wrote.)
+  pdl_launch_dependents();
+  pdl_wait();
 
   if (warp == 0) {
     // ---- producer -------------------------------------------------------------------------------------------------------
@@ -271,7 +274,6 @@ block_matmul_kernel(const __grid_constant__ MatmulParams p, const __grid_constan
   }
   __syncwarp();
   if (warp == 2) tmem_dealloc(tmem, kTmem);
-  if (p.chain == 2) pdl_wait();
 }
 
 // The kernel set up on the current device, and how many of its clusters the device holds; asked once (a look into both tables is a tenth of what a
@@ -312,17 +314,22 @@ int launch_cpt(const BlockMatmulArgs& g, MatmulParams p, cudaStream_t s) {
   attr[1].id = cudaLaunchAttributeClusterDimension;
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  const bool both = pl.part[1].count > 0;
-  for (int i = 0; i < (both ? 2 : 1); ++i) {
-    const BlockMatmulPart& part = pl.part[i];
-    cfg.gridDim = dim3(part.splits, (unsigned)part.count, pl.passes);
-    cfg.dynamicSmemBytes = matmul_smem(TN, part.splits);
-    attr[1].val.clusterDim.x = part.splits;
-    cfg.numAttrs = part.splits > 1 ? 2 : 1;
-    p.first = (int)part.first;
-    p.chain = both ? i + 1 : 0;
-    if (cudaLaunchKernelEx(&cfg, fn, p, tm_w, tm_a, matmul_stages(TN, part.splits)) != cudaSuccess) return VVS_ERR_CUDA;
+  auto launch = [&](int splits, int64_t rows) {
+    cfg.gridDim = dim3(splits, (unsigned)rows, pl.passes);
+    cfg.dynamicSmemBytes = matmul_smem(TN, splits);
+    attr[1].val.clusterDim.x = splits;
+    cfg.numAttrs = splits > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, fn, p, tm_w, tm_a, matmul_stages(TN, splits)) == cudaSuccess;
+  };
+  const BlockMatmulPart &main = pl.part[0], &rest = pl.part[1];
+  if (rest.count && matmul_in_one_launch(TN)) {
+    p.first = (int)rest.first;
+    p.alone = (int)((main.count + rest.splits - 1) / rest.splits);
+    return launch(rest.splits, p.alone + rest.count) ? VVS_OK : VVS_ERR_CUDA;
   }
+  if (!launch(main.splits, main.count)) return VVS_ERR_CUDA;
+  p.first = (int)rest.first;
+  if (rest.count && !launch(rest.splits, rest.count)) return VVS_ERR_CUDA;
   return VVS_OK;
 }
 

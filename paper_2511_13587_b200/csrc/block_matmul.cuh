@@ -19,8 +19,8 @@ struct MatmulParams {
   void* out;
   int64_t out_row;
   int m, n, nkb;                                   // nkb: blocks of K
-  int first;                                       // tile of weights that the launch begins with
-  int chain;                                       // 1: the first of two launches of a product, 2: the second
+  int first;                                       // tile of weights that the clusters begin with whose CTAs share one
+  int alone;                                       // clusters ahead of them whose CTAs have a tile each, from 0 to `first`
   int wide;                                        // four elements of out may be written together
   int32_t* status;
 };

@@ -6,7 +6,7 @@
 
 namespace vvs {
 
-// Tiles of 128 weights of one launch; of each tile and pass the blocks of K are dealt to `splits` CTAs, a cluster.
+// Tiles of 128 weights; of each tile and pass the blocks of K are dealt to `splits` CTAs, a cluster.
 struct BlockMatmulPart {
   int64_t first, count;
   int splits;
@@ -40,6 +40,8 @@ inline int matmul_rows(int64_t m) {
   const int64_t passes = (m + 127) / 128, each = (m + passes - 1) / passes;
   return each <= 16 ? 16 : each <= 32 ? 32 : each <= 48 ? 48 : each <= 64 ? 64 : each <= 96 ? 96 : 128;
 }
+// The two parts of a plan go in one launch: clusters of the second part's size, in the first of which each CTA has a tile of the first part.
+inline bool matmul_in_one_launch(int tn) { return tn <= 64; }
 // Shared memory: blocks of K under way and, of a cluster, the sums that a CTA is sent, 128 weights of its share of the rows in fours.  Two CTAs
 // fit an SM up to 64 rows, beside their factors (64 bytes a row) and barriers.
 inline int matmul_stage_bytes(int tn) { return kMatmulTileBytes + tn * 128; }
@@ -78,10 +80,10 @@ inline BlockMatmulPlan plan_block_matmul(int64_t m, int64_t n, int64_t k, int n_
   const int whole_splits = splits_of(tiles * passes, false);
   pl.part[0] = {0, tiles, whole_splits};
   int64_t whole = cost(tiles * passes, whole_splits);
-  // Tiles that are left over where all SMs have as many as the others: in a launch of their own, dealt to all SMs, up to 48 rows beside the first
-  // one (two CTAs fit an SM), with more than 64 behind it.  4096 columns through 22016 weights, 172 tiles: 18 rows 20.1 us as one launch (most SMs
-  // that have a CTA have two), 18.0 as 148 and 24 by five (by six, of which 22 fit beside the 148, 18.1); 64 rows, whose sums take longer,
-  // 20.9 / 21.2; 128 rows 33.8 / 26.7.
+  // Tiles that are left over where all SMs have as many as the others: dealt to all SMs, up to 48 rows beside the first ones in the same launch
+  // (two CTAs fit an SM), with more than 64 in a launch behind it.  4096 columns through 22016 weights, 172 tiles: 18 rows 20.1 us alike (most SMs
+  // that have a CTA have two), 18.3 as 148 and 24 by five (21.9 in two launches, of which the second waits for the first); 64 rows, whose sums take
+  // longer, 20.9 / 21.2; 128 rows 33.8 / 26.7.
   const int64_t full = tiles / n_sms * n_sms, left = tiles - full;
   if ((pl.tn <= 48 || pl.tn > 64) && passes == 1 && full > 0 && left > 0) {
     const int s = splits_of(left, true);
