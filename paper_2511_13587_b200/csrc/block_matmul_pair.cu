@@ -155,6 +155,8 @@ block_matmul_pair_kernel(const __grid_constant__ MatmulParams p, const __grid_co
         st.next();
       }
     }
+    // The last stages' MMAs signal both CTAs too, and nobody else waits for that: no CTA leaves before it was told of them.
+    for (int i = max(issued - kStages, 0); i < issued && ok; ++i) ok = warp_wait_or_abort(&done_bar[i % kStages], (i / kStages) & 1, &s_abort);
     if (!ok && rank == 0) {                        // nothing may be in flight when the pair leaves (bounded)
       for (int i = issued > kStages ? issued - kStages : 0; i < issued; ++i) mbar_wait(&full_bar[i % kStages], (i / kStages) & 1);
       __syncwarp();
@@ -308,7 +310,7 @@ block_matmul_pair_kernel(const __grid_constant__ MatmulParams p, const __grid_co
   }
   tc_fence_before();
   __syncthreads();
-  cluster_sync();                                  // no CTA leaves while the pair's MMAs or signals may still reach it
+  cluster_sync();                                  // no CTA leaves while the other one's signals may still reach it
   tc_fence_after();
   if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
 }
