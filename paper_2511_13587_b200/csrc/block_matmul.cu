@@ -106,10 +106,10 @@ block_matmul_kernel(const __grid_constant__ MatmulParams p, const __grid_constan
     if (!ok) {
       if (lane == 0) atomicOr(p.status, VVS_DEV_TIMEOUT);
       s_abort = 1;
-      for (int i = issued > stages ? issued - stages : 0; i < issued; ++i)     // nothing may be in flight when the CTA leaves (bounded)
-        mbar_wait(&full_bar[i % stages], (i / stages) & 1);
-      __syncwarp();
     }
+    // Nothing may be in flight when the CTA leaves, also where it is another warp that gives up (bounded)
+    for (int i = max(issued - stages, 0); i < issued; ++i) mbar_wait(&full_bar[i % stages], (i / stages) & 1);
+    __syncwarp();
   } else if (warp == 1) {
     // ---- MMA issuer (a wait that ran out is reported, and nothing more is issued) -------------------------------------------
     const uint32_t idesc = idesc_e4m3_f32(128, TN), lo0 = desc_lo_sw128(smem_u32(smem));

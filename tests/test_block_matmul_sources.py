@@ -38,3 +38,16 @@ def test_the_pairs_producers_wait_for_the_last_stages_signals():
         at += 1
         if at == stages:
             at, par = 0, par ^ 1
+
+
+def test_loads_under_way_are_waited_for_whoever_gives_up():
+    """The warp that waits for loads may give up when the one that asked for them has long been through: that one waits for its last fills in any case."""
+    code = _code("block_matmul.cu")
+    producer = code[code.index("if (warp == 0) {"):code.index("else if (warp == 1)")]
+    depth, drained = 0, []
+    for i, c in enumerate(producer):
+        depth += (c == "{") - (c == "}")
+        if producer.startswith("mbar_wait(&full_bar[i % stages], (i / stages) & 1)", i):
+            drained.append(depth)
+    assert drained == [1]                                     # the warp's own block: under no condition
+    assert re.search(r"for \(int i = max\(issued - stages, 0\); i < issued; \+\+i\) mbar_wait", producer)
