@@ -482,8 +482,9 @@ int vvs_quant_cache_evict(vvs_ctx* ctx, const vvs_qcache* qc, const int32_t* cac
  * codes (as in the cache) times a float32 scale: of a row, one for each block of 128 columns; of a weight matrix, one for each block of
  * 128 x 128.  The last block of a row, and of a matrix's rows, may be short.  The calls that make them take the smallest scale by which a
  * block's largest finite magnitude is at most 448, max / 448, 2^-60 at least; an infinity is stored as the largest code, a NaN as 0:
- * VVS_DEV_NONFINITE.  Columns are multiples of 16; rows that are written do not overlap (stride >= columns).  The calls need a context for its storage type T and its status word only; calls on
- * different streams may share it. */
+ * VVS_DEV_NONFINITE.  Columns are multiples of 16; neither they nor the rows times a row's blocks are more than 2^30; rows that are
+ * written do not overlap (stride >= columns).  The calls need a context for its storage type T and its status word only; calls on different
+ * streams may share it. */
 
 /* Rows of T: row t begins at data + t * row (elements; data is 16-byte aligned, the stride of more than one row a multiple of 16 bytes). */
 typedef struct vvs_rows {
@@ -509,9 +510,9 @@ typedef struct vvs_qweight {
 
 /* s = x + residual (NULL: x), y = s / sqrt(mean(s^2) + eps) * weight (T [n_cols]), out = y in 8 bits.  sum_out = s and norm_out = y, both
  * rounded to T, where they are given.  Sums and products are float32; y comes from s before it is rounded.  sum_out and norm_out may be x
- * or residual, where address and stride are the same; other overlaps are not allowed.  A row whose squares' sum is no finite float32 sets
- * VVS_DEV_NONFINITE.  n_cols <= 32768; below 2^30 at most, and n_rows times the blocks of a row
- * at most 2^30 everywhere. */
+ * or residual, where address and stride are the same; other overlaps are not allowed.  A row whose squares' sum is beyond float32 becomes
+ * zeros, as one with a NaN does, and sets VVS_DEV_NONFINITE; small squares are taken without loss.  eps is 0 at least; a row of zeros
+ * with eps 0 is 0 / 0: codes 0, norm_out NaN, VVS_DEV_NONFINITE.  n_cols: 32768 at most. */
 int vvs_norm_quant(vvs_ctx* ctx, int32_t n_rows, int32_t n_cols, const vvs_rows* x, const vvs_rows* residual, const void* weight, float eps,
                    const vvs_rows* sum_out, const vvs_rows* norm_out, const vvs_qrows* out, void* stream);
 

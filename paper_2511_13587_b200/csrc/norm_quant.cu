@@ -13,6 +13,21 @@ namespace vvs {
 
 namespace {
 
+// Of all threads of a row: a warp, or the CTA.
+__device__ __forceinline__ float row_sum(float v, float* s_sum, int t, int threads) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  if (threads > 32) {                              // (one row a CTA then)
+    if ((t & 31) == 0) s_sum[t >> 5] = v;
+    __syncthreads();
+    v = (t & 31) < (threads >> 5) ? s_sum[t & 31] : 0.f;
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    v = __shfl_sync(0xffffffffu, v, 0);
+  }
+  return v;
+}
+
 // U: units of a thread.  blockDim (threads of a row, rows of a CTA).
 template <typename T, int U>
 __global__ void __launch_bounds__(512) norm_quant_kernel(NormQuantArgs a) {
@@ -62,17 +77,23 @@ __global__ void __launch_bounds__(512) norm_quant_kernel(NormQuantArgs a) {
       const int u = j * threads + t;
       if (u < units) store_unit(static_cast<T*>(a.sum_out.data) + row * a.sum_out.row + 8 * u, false, 0, narrow_unit(y[j], x[j]));
     }
+  ss = row_sum(ss, s_sum, t, threads);
+  float mean = ss / (float)a.n_cols + a.eps;
+  if (mean < 0x1p-100f) {                          // (of the whole row) squares that float32 does not hold well: the row times 2^96, its squares times 2^192
+    constexpr float k = 0x1p96f;
+    ss = 0.f;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-  if (threads > 32) {                              // (one row a CTA then)
-    if ((t & 31) == 0) s_sum[t >> 5] = ss;
-    __syncthreads();
-    ss = (t & 31) < (threads >> 5) ? s_sum[t & 31] : 0.f;
+    for (int j = 0; j < U; ++j)
 #pragma unroll
-    for (int o = 8; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-    ss = __shfl_sync(0xffffffffu, ss, 0);
+      for (int e = 0; e < 8; ++e) {
+        y[j][e] *= k;
+        ss = fmaf(y[j][e], y[j][e], ss);
+      }
+    if (threads > 32) __syncthreads();             // (the first sum has been read)
+    ss = row_sum(ss, s_sum, t, threads);
+    mean = ss / (float)a.n_cols + a.eps * k * k;
   }
-  const float rs = rsqrtf(ss / (float)a.n_cols + a.eps);
+  const float rs = rsqrtf(mean);
   bool strange = false;
 #pragma unroll
   for (int j = 0; j < U; ++j) {
