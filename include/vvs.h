@@ -516,7 +516,8 @@ typedef struct vvs_qweight {
 int vvs_norm_quant(vvs_ctx* ctx, int32_t n_rows, int32_t n_cols, const vvs_rows* x, const vvs_rows* residual, const void* weight, float eps,
                    const vvs_rows* sum_out, const vvs_rows* norm_out, const vvs_qrows* out, void* stream);
 
-/* out = x in 8 bits or, with gate, gate / (1 + exp(-gate)) * x (SwiGLU; gate and x may be halves of one projection's rows). */
+/* out = x in 8 bits or, with gate, gate / (1 + exp(-gate)) * x (SwiGLU; gate and x may be halves of one projection's rows).  Where exp(-gate) is
+ * 2^126 or more (gates below -87.3) the product is taken as 0; it is below 2^-119 |x|. */
 int vvs_rows_quant(vvs_ctx* ctx, int32_t n_rows, int32_t n_cols, const vvs_rows* x, const vvs_rows* gate, const vvs_qrows* out, void* stream);
 
 /* out = w (T [n_rows, n_cols]) in 8 bits; what out points to is written. */

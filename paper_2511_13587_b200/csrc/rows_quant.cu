@@ -20,7 +20,9 @@ constexpr int kThreads = 256;
 template <typename T, bool GATE>
 constexpr int kFlight = sizeof(T) == 4 && GATE ? 2 : 4;
 
-// gate / (1 + e^-gate) * x
+// gate / (1 + e^-gate) * x: within 2^-17, most of it by the exponent, whose product and constant round (1.3 * 2^-24 of 126 at most).  From e^-gate = 2^126
+// on (gates below -87.3) the reciprocal is no normal number and the result 0, |y| below 2^-119 |x|.  (What large elements leave of that by a second
+// form for such gates: 5460 rows of 11008 56.3 to 57.2 us for 53.8, whichever way they were looked for.)
 __device__ __forceinline__ float gated(float gate, float x) {
   float r;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + ex2(gate * -1.442695041f)));
