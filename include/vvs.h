@@ -524,9 +524,9 @@ int vvs_rows_quant(vvs_ctx* ctx, int32_t n_rows, int32_t n_cols, const vvs_rows*
 int vvs_weight_quant(vvs_ctx* ctx, const vvs_rows* w, const vvs_qweight* out, void* stream);
 
 /* out[m, n] = sum over blocks b of a_scale[m, b] * w_scale[n / 128, b] * sum over b's columns of a[m, k] * w[n, k]: out T [n_rows,
- * w->n_rows], a [n_rows, w->n_cols].  Any scales whose products with the sums are float32 numbers; codes that are e4m3's NaN give NaN.
- * A block's sum is taken by the tensor cores in float32, blocks are added in float32; the order is fixed for a size.  Rows of out need no
- * alignment but the first's (16 bytes). */
+ * w->n_rows], a [n_rows, w->n_cols].  Any scales of which a_scale[m, b] * w_scale[n / 128, b] is 0 or a normal float32 number (that product is
+ * formed first), and its product with b's sum a float32 number; codes that are e4m3's NaN give NaN.  A block's sum is taken by the tensor
+ * cores in float32, blocks are added in float32; the order is fixed for a size.  Rows of out need no alignment but the first's (16 bytes). */
 int vvs_block_matmul(vvs_ctx* ctx, int32_t n_rows, const vvs_qrows* a, const vvs_qweight* w, const vvs_rows* out, void* stream);
 
 /* Synchronise `stream`, copy the device status word to *out_bits (VVS_DEV_* bits) and clear
