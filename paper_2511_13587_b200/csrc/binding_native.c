@@ -795,11 +795,17 @@ static PyObject* py_matmul(FAST) {
   int32_t rows = 0;
   f.device = -1;
   if (PARSE("vvs_block_matmul", matmul_params, N(matmul_params)) < 0) return NULL;
+  /* a structure of the base class, vvs_qweight, that the caller has made, or one from make_qweight; no other object of that many bytes */
   Py_buffer b;
-  if (PyObject_GetBuffer(f.w, &b, PyBUF_SIMPLE) < 0) return NULL;
-  const int ok = b.len == (Py_ssize_t)sizeof(vvs_qweight) || PyObject_TypeCheck(f.w, (PyTypeObject*)g_qweight);
-  if (ok) memcpy(&q, b.buf, b.len == (Py_ssize_t)sizeof(vvs_qweight) ? sizeof(vvs_qweight) : sizeof(q));
-  PyBuffer_Release(&b);
+  PyTypeObject* made = (PyTypeObject*)g_qweight;
+  const Py_ssize_t bytes = PyObject_TypeCheck(f.w, made) ? (Py_ssize_t)sizeof(q) : (Py_ssize_t)sizeof(vvs_qweight);
+  int ok = PyObject_TypeCheck(f.w, made->tp_base);
+  if (ok) {
+    if (PyObject_GetBuffer(f.w, &b, PyBUF_SIMPLE) < 0) return NULL;
+    ok = b.len == bytes;
+    if (ok) memcpy(&q, b.buf, bytes);
+    PyBuffer_Release(&b);
+  }
   if (!ok) {
     PyErr_SetString(PyExc_TypeError, "w: expected a vvs_qweight");
     return NULL;
