@@ -68,9 +68,9 @@ inline BlockMatmulPlan plan_block_matmul(int64_t m, int64_t n, int64_t k, int n_
     const int64_t each = (count * s + n_sms - 1) / n_sms, rounds = (each + per_sm - 1) / per_sm, blocks = (nkb + s - 1) / s;
     return (each < per_sm ? blocks * a_block * 3 / 2 : each * blocks * a_block) + rounds * 350 + (s > 1 ? 80 + 20 * s : 0);
   };
-  // Clusters that do not all fit at once wait for others' end and gain nothing; a CTA has two blocks at least.  288 rows of 3456 through 1280
-  // weights, 30 tiles: 1 / 2 / 4 CTAs a tile 13.3 / 9.7 / 8.2 us; 18 rows of 4096 through 4096, 32 tiles, 1 / 2 / 4 / 8: 11.2 / 8.7 / 7.2 / 7.1.
-  // Numbers between are slower where all SMs have work already (96 tiles of 32 blocks, 2 / 3: 12.9 / 14.0; ten of ten, 4 / 5: 4.1 / 4.5).
+  // Clusters all fit at once, or some wait for others' end; a CTA has two blocks at least.  288 rows of 3456 through 1280 weights, 30 tiles by
+  // 1 / 2 / 4 / 8 CTAs: 12.5 / 9.4 / 7.4 / 12.3 us; 18 rows of 4096 through 4096, 32 tiles: 11.2 / 8.1 / 6.5 / 6.0 (30 of eight fit: here two that
+  // wait would do no harm).  Numbers between are slower where all SMs have work already (96 tiles of 32 blocks, 2 / 3: 12.4 / 15.5).
   auto splits_of = [&](int64_t count, bool beside) {              // beside others: a CTA an SM, any number
     int best = 1;
     for (int s = 2; s <= kMatmulMaxSplits && 2 * s <= nkb && count <= (int64_t)clusters[s] * (beside ? 1 : per_sm); s += beside ? 1 : s)
@@ -81,11 +81,12 @@ inline BlockMatmulPlan plan_block_matmul(int64_t m, int64_t n, int64_t k, int n_
   pl.part[0] = {0, tiles, whole_splits};
   int64_t whole = cost(tiles * passes, whole_splits);
   // Tiles that are left over where all SMs have as many as the others: dealt to all SMs, up to 48 rows beside the first ones in the same launch
-  // (two CTAs fit an SM), with more than 64 in a launch behind it.  4096 columns through 22016 weights, 172 tiles: 18 rows 20.1 us alike (most SMs
-  // that have a CTA have two), 18.3 as 148 and 24 by five (21.9 in two launches, of which the second waits for the first); 64 rows, whose sums take
-  // longer, 20.9 / 21.2; 128 rows 33.8 / 26.7.
+  // (two CTAs fit an SM), with more than 64 in a launch behind it.  4096 columns through 22016 weights, 172 tiles: 18 rows 18.4 to 18.8 us alike,
+  // 17.7 as 148 and 24 by five (21.9 in two launches, of which the second waits for the first); 36 rows 18.1 / 19.0, of 1280 columns 9.0 / 8.9; 64
+  // rows, whose sums take longer, 20.9 / 21.2; 72 rows 29.1 / 23.6, 128 rows 33.0 / 26.1.  In the same launch only where an SM has one of the first
+  // tiles: with more its clusters do not all fit at once (18 rows of 1280 columns, 297 tiles 12.9 / 14.0, 470 16.8 / 18.3, 600 20.2 / 22.3).
   const int64_t full = tiles / n_sms * n_sms, left = tiles - full;
-  if ((pl.tn <= 48 || pl.tn > 64) && passes == 1 && full > 0 && left > 0) {
+  if ((pl.tn <= 48 ? full == n_sms : pl.tn > 64 && full > 0) && passes == 1 && left > 0) {
     const int s = splits_of(left, true);
     const int64_t blocks = full / n_sms * nkb + (left * s + n_sms - 1) / n_sms * ((nkb + s - 1) / s);
     const int64_t both = blocks * a_block + 530 + 20 * s + (per_sm == 1 ? full / n_sms * 350 : 0);
@@ -95,9 +96,9 @@ inline BlockMatmulPlan plan_block_matmul(int64_t m, int64_t n, int64_t k, int n_
       pl.part[1] = {full, left, s};
     }
   }
-  // The pairs' kernel: rounds of pairs x blocks of K.  Measured at 9 x 9 sizes from 96 to 2048 rows, the smaller of the two numbers is the faster
-  // kernel or one within 5 %: 128 rows of 4096 through 22016 weights 35.2 us here, 34.5 on pairs; 256 53.9 / 34.5; 1024 194 / 86; 1024 rows of 1280
-  // through 1280 9.3 / 9.4, 2048 18.3 / 9.8.
+  // The pairs' kernel: rounds of pairs x blocks of K.  Measured at 12 x 8 sizes from 65 to 2048 rows, the smaller of the two numbers is the faster
+  // kernel or one within 4 %: 128 rows of 4096 through 22016 weights 26.3 us here, 33.2 on pairs; 256 49.7 / 33.7; 1024 163 / 80; 1024 rows of 1280
+  // through 1280 8.0 / 8.3, 2048 15.8 / 9.1.
   const int64_t pair_tiles = (m + 255) / 256 * ((n + 255) / 256), pairs = n_sms / 2;
   const int64_t there = (pair_tiles + pairs - 1) / pairs * (nkb + (nkb & 1)) * 46 + 500;
   pl.pairs = there < whole || passes > 65535;

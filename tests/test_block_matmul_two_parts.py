@@ -21,3 +21,9 @@ def test_parts_that_go_in_one_launch(plan):  # noqa: F811
                 alone = -(-count // size)
                 tiles = [t for t in range(alone * size) if t < begin] + [begin + y for y in range(rest)]
                 assert first == 0 and tiles == list(range(-(-n // 128))) and (alone - 1) * size < begin and alone + rest <= 65535
+
+
+@pytest.mark.parametrize("m,k,n", [(18, 1280, 38016), (18, 1280, 60160), (9, 4096, 76800), (36, 1280, 60160)])
+def test_more_tiles_than_clusters_of_one_launch_hold(plan, m, k, n):  # noqa: F811
+    """Up to 48 rows two parts are for one tile an SM: of more the clusters would not all fit at once."""
+    assert plan(m, n, k)["parts"][1][1] == 0
