@@ -1,14 +1,27 @@
 """Products in two parts whose rows, scales and weights are written by the calls right before them, into the same buffers again and again: every
 result is that of what was written last.  The scales of the sets lie far apart, so that one set's scale beside another's codes is a result far off."""
-import numpy as np
 import pytest
 import torch
 
 from paper_2511_13587_b200 import binding as vb
-from test_gpu_block_quant import BF16, EPS, F32, check_product, coded, ctxs, dev  # noqa: F401
+from test_gpu_block_quant import BF16, E4M3, EPS, F32, HALF_STEP, coded, ctxs, dev  # noqa: F401
 from vvs_synth import gen
 
 pytestmark = pytest.mark.gpu
+
+
+def product64(a, a_scale, w, w_scale):
+    """(out, sum of magnitudes) in float64, on the device: the oracle's loops take seconds for a matrix of this size."""
+    cols = a.shape[1]
+    a = a.view(E4M3).double() * a_scale.double().repeat_interleave(128, 1)[:, :cols]
+    w = w.view(E4M3).double() * w_scale.double().repeat_interleave(128, 0)[:len(w)].repeat_interleave(128, 1)[:, :cols]
+    return a @ w.T, a.abs() @ w.abs().T
+
+
+def check_product(out, ops):
+    want, room = product64(*ops)
+    off = (out.double() - want).abs()
+    assert (off <= (2.0 ** -16 + 3 * ops[1].shape[1] * 2.0 ** -24) * room + HALF_STEP[out.dtype] * want.abs()).all()
 
 
 @pytest.mark.parametrize("dtype,rows,cols,outs", [(BF16, 18, 4096, 19000), (F32, 18, 4096, 19000), (BF16, 36, 4096, 20001), (BF16, 100, 4096, 20001),

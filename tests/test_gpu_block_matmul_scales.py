@@ -5,9 +5,9 @@ import numpy as np
 import pytest
 import torch
 
-from oracle import block_quant_oracle as B
 from paper_2511_13587_b200 import binding as vb
-from test_gpu_block_quant import F32, ctxs, dev, host  # noqa: F401
+from test_gpu_block_matmul_rewritten import product64
+from test_gpu_block_quant import F32, ctxs, dev  # noqa: F401
 from vvs_synth import gen
 
 pytestmark = pytest.mark.gpu
@@ -24,11 +24,10 @@ def test_product_of_scales(ctxs, rows, cols, outs, a_power, w_power):  # noqa: F
     w_scale = (rng.uniform(1, 2, (-(-outs // 128), blocks)) * np.exp2(w_power)).astype(np.float32)
     a_scale[0], w_scale[0, 0] = 0.0, 0.0
     assert np.isfinite(a_scale).all() and np.isfinite(w_scale).all()
+    ops = [dev(t) for t in (a, a_scale, w, w_scale)]
     out = torch.full((rows, outs), float("nan"), device="cuda")
-    vb.vvs_block_matmul(ctxs[F32], dev(a), dev(a_scale), vb.make_qweight(dev(w), dev(w_scale)), out)
-    at = np.unique(np.r_[0:rows:max(1, rows // 40), rows - 1])
-    want, room = B.product(a[at], a_scale[at], w, w_scale)
-    bound = (2.0 ** -16 + 3 * blocks * 2.0 ** -24) * room + 2.0 ** -24 * np.abs(want) + blocks * 2.0 ** -150
-    got = host(out)[at]
-    assert (np.abs(got - want) <= bound).all() and (got[0] == 0).all()
+    vb.vvs_block_matmul(ctxs[F32], ops[0], ops[1], vb.make_qweight(ops[2], ops[3]), out)
+    want, room = product64(*ops)
+    bound = (2.0 ** -16 + 3 * blocks * 2.0 ** -24) * room + 2.0 ** -24 * want.abs() + blocks * 2.0 ** -150
+    assert ((out.double() - want).abs() <= bound).all() and (out[0] == 0).all()
     assert vb.vvs_device_status(ctxs[F32]) == 0
