@@ -8,8 +8,8 @@
 // dealt to the CTAs of a cluster where tiles are few; each CTA is sent the others' sums of its share of the rows and adds them in rank order.
 //
 // Bound by the weights' way from HBM, small ones by their chain of round trips (wait for what precedes, first loads, sums, exchange: a
-// microsecond each).  Rows of 4096 through 22016 weights: 18 in 18.4 us, 4.95 TB/s (77 % of a copy's rate; 94 % through 88064 weights), 128 in 26.7;
-// 288 of 3456 through 1280 7.0, one of 1280 through 1280 4.0 (2.9 in a graph).
+// microsecond each).  Rows of 4096 through 22016 weights: 18 in 18.5 us, 4.9 TB/s (76 % of a copy's rate; 94 % through 88064 weights), 128 in 26.7;
+// 288 of 3456 through 1280 7.0, one of 1280 through 1280 4.2 (2.9 in a graph).
 #include <atomic>
 
 #include "block_matmul.cuh"

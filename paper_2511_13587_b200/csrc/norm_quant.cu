@@ -6,7 +6,8 @@
 // prompts, by the launch and two dependent steps (sum over the row, maximum over a block) for a step's rows.  A thread has units of eight
 // elements; the sixteen lanes of half a warp have a block of 128 columns, so that a block's maximum is four shuffles.
 //
-// 10408 rows of 4096, residual and sum: 51 us, 5.9 TB/s (91 % of a copy's rate); 18 rows of 1280 4.2 us, as long as the call (1.7 in a graph).
+// 10408 rows of 4096, residual and sum: 54.5 us, 5.5 TB/s (85 % of a copy's rate; 48.2 for the same rows each time, some of which L2 has); 18
+// rows of 1280 4.4 us, as long as the call (1.8 in a graph).
 #include "block_quant.cuh"
 
 namespace vvs {
@@ -129,8 +130,9 @@ template <typename T>
 int launch_norm_quant(const NormQuantArgs& a, cudaStream_t s) {
   const int units = a.n_cols / 8;
   // Units of a thread: one as long as that leaves at most 2048 threads an SM, else up to four (two of float32), where whole warps do not leave
-  // more lanes idle for it.  Microseconds with 1 / 2 / 4 units: 18 rows of 1280 1.67 / 1.71 / 2.17, 288 of 4096 3.80 / 4.27 / 5.17, 10408 of 4096 60.5 /
-  // 47.1 / 45.7, 40000 of 256 14.4 / 17.7 / 30.0; float32, 5204 of 4096 42.3 / 41.9 / 47.1.  (Eight, for rows that are wider than 512 threads' four.)
+  // more lanes idle for it.  Microseconds with 1 / 2 / 4 units, of the same rows each time: 18 rows of 1280 1.76 / 1.88 / 2.39, 288 of 4096 3.05 / 3.93 / 4.63,
+  // 10408 of 4096 62.4 / 50.8 / 48.2, 40000 of 256 12.3 / 17.9 / 32.7; float32, 5204 of 4096 42.8 / 42.2 / 45.5.  (Eight, for rows that are wider than 512
+  // threads' four.)
   const long long room = (long long)a.n_sms * 2048;
   auto threads_of = [&](int per) { return ((units + per - 1) / per + 31) / 32 * 32; };
   int per = 1;

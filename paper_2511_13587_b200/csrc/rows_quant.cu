@@ -3,11 +3,11 @@
 //   y = x  or  gate / (1 + exp(-gate)) * x,  scale = max |y| / 448 over the block,  code = e4m3(y / scale)
 //
 // Bound by HBM (every element is read once and stays in registers until its code is written), small calls by the launch.  Rows: half a
-// warp has a block of 128 columns, eight elements a lane; SwiGLU's also by the exponential's and the reciprocal's pipe (64 % of its rate).
+// warp has a block of 128 columns, eight elements a lane; SwiGLU's also by the exponential's and the reciprocal's pipe (64 % of its rate at 57 us).
 // Weights: a CTA has a block of 128 x 128, eight units of eight elements a thread.
 //
-// 5460 rows of 11008, gate and up: 57 us, 5.3 TB/s (82 % of a copy's rate); 18 of 3456 3.4 us, as long as the call (1.2 in a graph).  22016 x 4096 weights 46 us, 5.8 TB/s
-// (three CTAs of 256 threads an SM; two of 512 50 us, one of 1024 88).
+// 5460 rows of 11008, gate and up: 60 us, 5.0 TB/s (78 % of a copy's rate; 53.8 for the same rows each time); 18 of 3456 3.6 us, as long as the call
+// (1.4 in a graph).  22016 x 4096 weights 49.5 us, 5.5 TB/s (46.5 for the same each time; two CTAs of 512 threads an SM 50, one of 1024 88).
 #include "block_quant.cuh"
 
 namespace vvs {

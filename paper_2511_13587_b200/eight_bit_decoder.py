@@ -1,5 +1,6 @@
 """Decoder layers whose weights and activations are 8 bits wide, over a `BoundedCache`: what a program decoding long images or video runs in
-the place of `vvs_verify`'s bf16 layers where their weights' bytes, or the products of its prompts, are what it waits for.
+the place of `vvs_verify`'s bf16 layers where their weights' bytes, or the products of its prompts, are what it waits for: for 18 rows a layer of 4096
+columns takes 81 us in the place of 97, but one of 1280 columns, whose ten launches cost more than its bytes, 41 in the place of 18.
 
 `EightBitDecoder` rounds a model's weights once, block by block (`vvs_weight_quant`).  A step takes a block's rows through all layers: norm with
 the residual's addition into 8 bits, q, k and v, append and attention of the cache, 8 bits, output projection, norm, gate and up, SwiGLU
@@ -63,7 +64,8 @@ class EightBitDecoder:
     def step(self, x: torch.Tensor, pos: torch.Tensor, mass_rows: int = 1, row_count: torch.Tensor | None = None,
              visible: torch.Tensor | None = None) -> torch.Tensor:
         """x [n_seqs, rows, d_model] of a block (embeddings), pos int32 [axes, n_seqs, rows]: its features [n_seqs, rows, d_model] (a buffer of
-        this object).  The rows lie behind the cache's fill until `cache.commit`."""
+        this object).  The rows lie behind the cache's fill until `cache.commit`.  Rows of x from row_count on go through norms and products with
+        the others: their features mean nothing, and numbers there that are not finite are told of like any."""
         b, rows, d = x.shape
         if b != self.n_seqs or d != self.d_model or rows > self.cache.max_rows:
             raise ValueError(f"expected [{self.n_seqs}, up to {self.cache.max_rows}, {self.d_model}]")
